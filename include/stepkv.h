@@ -369,6 +369,102 @@ STEPKV_API stepkv_status_t stepkv_decode_h2o(int32_t n_layers, const void* const
                                   void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * A cache held in 4 bits: the rows that a boundary keeps (Eq. 1), at 4.5 bits a channel instead of 16.  The paper
+ * compresses by leaving rows out; this is the same cache with fewer bits per row, for callers whose decode reads
+ * are bound by the bytes of the rows.
+ *
+ * Format.  A row (one token of one KV head) is cut into groups of STEPKV_Q4_GROUP channels.  A group has one fp16 scale s
+ * of at most 5 significant bits, either sign, and 32 codes n in 0..15; a code stands for s (n - 8).  With M and m the
+ * group's maximum and minimum:
+ *   x* = M if M >= -m else m
+ *   s  = fp16(r5(-x* / 8)), r5: rounded to 5 significant bits, ties to even; |s| at most 896
+ *   n  = 8 + clamp(rint(x / s), -8, 7) with the exact quotient, ties to even; 8 where s is 0
+ * so the channel of the largest magnitude gets code 0.  A group that holds a NaN or an infinity has s = NaN and codes 8:
+ * it reads back as NaN.  Magnitudes above 7168 saturate; groups below 2^-22 become 0.
+ * A value has at most 5 + 3 significant bits, so bf16 holds it exactly: reading back does not round, attention over the
+ * cache is attention over the rows read back, and quantising what was read back gives the same codes and scales (where
+ * |s| >= 2^-20: below, fp16's grid leaves a scale fewer than 5 bits).
+ * Nothing but the row enters its codes, so rows can be appended one at a time and moved by a compaction.
+ *
+ * Layout, per layer and for keys and values alike:
+ *   codes   [Hkv][rows][d / 2] uint8: byte b of a row holds channel 2b in its low and channel 2b + 1 in its high half
+ *   scales  [Hkv][rows][d / 32] fp16
+ * Codes: bases 16-byte aligned, code_head_stride (bytes) a multiple of 16.  Scales: bases aligned to d / 16 bytes (to the
+ * largest power of two that divides it), scale_head_stride (elements) a multiple of d / 32.
+ * d a multiple of 32 up to 256 (stepkv_q4_decode: 64 or 128).  Keys alone: V and V_scale NULL.
+ */
+#define STEPKV_Q4_GROUP 32
+typedef struct {
+  int32_t n_layers, Hkv, d;
+  int32_t rows;                /* capacity of a head, rows */
+  void* const* K;              /* host [n_layers]: codes of the keys */
+  void* const* K_scale;        /* host [n_layers] */
+  void* const* V;              /* host [n_layers], or NULL with V_scale: keys alone */
+  void* const* V_scale;
+  int64_t code_head_stride;    /* bytes between KV heads of codes (>= rows * d / 2) */
+  int64_t scale_head_stride;   /* fp16 elements between KV heads of scales (>= rows * d / 32) */
+} stepkv_q4_cache_t;
+
+/* Quantises rows as they are written: for every layer l, KV head h and r < n,
+ *   row row0 + r of the cache = the codes and scales of K[l][h][idx ? idx[r] : r][:]   (V alike).
+ * Appending a token is n = 1; writing what a selection kept is idx = kept_idx, n_dev = n_kept, row0 = 0.
+ *  K[l], V[l]  host arrays of device pointers, bf16 with head_stride and row_stride elements between heads and rows
+ *              (any order, so [token][head][d] serves too; both multiples of 8), T rows; bases 16-byte aligned.  V is
+ *              NULL exactly where the cache holds keys alone.
+ *  idx         [n] int32 device, or NULL.  An index outside [0, T) sets STEPKV_EDATA and its row is not written.
+ *  n           rows to write; with n_dev given, *n_dev (device) rows and n is their limit: a count above it sets
+ *              STEPKV_ENOSPACE, a negative one STEPKV_EDATA, and nothing is written.  0 is a valid count.
+ *  row0        the first row written, the same for all layers; with row0_dev given, row0_dev[l * row0_dev_stride]
+ *              (device; stride 0: one for all layers, 1: one each) takes its place.  A layer whose rows would
+ *              not all lie in [0, rows) sets STEPKV_ENOSPACE and is not written.
+ * Other rows of the cache are left as they are.
+ */
+STEPKV_API stepkv_status_t stepkv_q4_write(const stepkv_q4_cache_t* cache, const void* const* K, const void* const* V,
+                                int64_t head_stride, int64_t row_stride, int32_t T, const int32_t* idx,
+                                const int32_t* n_dev, int32_t n, const int32_t* row0_dev, int32_t row0_dev_stride,
+                                int32_t row0, int32_t* dev_status, void* stream);
+
+/* Reads rows back to bf16 (exactly, see above): for every layer l, KV head h and r < n,
+ *   K[l][h][r][:] = row (idx ? idx[r] : row0 + r) of the cache   (V alike).
+ * E.g. the saliency layers' keys for stepkv_score, or a whole cache for a prefill.
+ *  K, V        host arrays of device pointers to bf16, strides as in stepkv_q4_write; either may be NULL (not both).
+ *  idx, n, n_dev, row0, row0_dev as in stepkv_q4_write; row0 is not used with idx.  A row outside [0, rows) sets
+ *  STEPKV_EDATA and is not read: with idx that row, else the layer.
+ */
+STEPKV_API stepkv_status_t stepkv_q4_read(const stepkv_q4_cache_t* cache, const int32_t* idx, const int32_t* n_dev, int32_t n,
+                               const int32_t* row0_dev, int32_t row0_dev_stride, int32_t row0, void* const* K,
+                               void* const* V, int64_t head_stride, int64_t row_stride, int32_t* dev_status,
+                               void* stream);
+
+/* stepkv_compact over a cache held in 4 bits: retained rows move as they are (codes and scales bit for bit).  Arguments,
+ * results and errors as stepkv_compact, with the source's T rows in `in` (T <= in->rows) and kept_cap <= out->rows; `out`
+ * shares no buffer with `in` (STEPKV_EUNSUPPORTED where a base pointer is the same), and holds values where `in` does.
+ */
+STEPKV_API stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_t T, const int32_t* kept_idx,
+                                  const int32_t* n_kept, int32_t kept_cap, const stepkv_q4_cache_t* out,
+                                  const int32_t* step_id_in, const int32_t* pos_in, int32_t* step_id_out,
+                                  int32_t* pos_out, int32_t* dev_status, void* stream);
+
+/* Decode attention over a cache held in 4 bits: stepkv_decode's formula over the values the codes stand for.  The
+ * n_layers caches may be the layers of one trajectory or the trajectories of a batch, each with its own count:
+ *  q[l]        host array of device pointers, [Hq][d] bf16, 16-byte aligned.
+ *  n           keys of cache l: n_dev[l * n_dev_stride] (device; stride 0: one for all, 1: one each) where n_dev is given,
+ *              else n_host (0 <= n_host <= n_cap).  0: nothing to attend to, the output is zero.  A count above n_cap
+ *              sets STEPKV_ENOSPACE and n_cap rows are used; a negative one sets STEPKV_EDATA, the output is zero.
+ *  n_cap       at most rows; the workspace and the split of the work go by it.
+ *  out[l]      host array of device pointers, [Hq][d] fp32, 16-byte aligned.
+ *  ws          scratch of stepkv_q4_decode_workspace_size bytes (256-byte aligned): partial states.
+ *  Rows at or past the count are not used, whatever they hold.  A key or a query with a NaN or an infinity makes the
+ *  outputs of its heads NaN; a value row that reads back as NaN makes those channels NaN.
+ *  Supported: d in {64, 128}; Hq a multiple of Hkv with at most 8 query heads per KV head.
+ *  Deterministic; the last bits depend on the split, which goes by the counts, n_layers, Hkv and n_cap.
+ */
+STEPKV_API size_t stepkv_q4_decode_workspace_size(int32_t n_layers, int32_t Hkv, int32_t Hq, int32_t d, int32_t n_cap);
+STEPKV_API stepkv_status_t stepkv_q4_decode(const stepkv_q4_cache_t* cache, const void* const* q, int32_t Hq,
+                                 const int32_t* n_dev, int32_t n_dev_stride, int32_t n_host, int32_t n_cap,
+                                 float* const* out, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Step signals from evidence cues (Sec. 4.1: observation validity, evidence gain, action redundancy of
  * Eq. 2 and the similarity that drives Eq. 3).  Every field of a step (0 Thought, 1 Action,
  * 2 Observation) is given as up to STEPKV_MAX_CUES evidence cues: distinct 32-bit ids in strictly

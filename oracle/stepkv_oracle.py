@@ -373,3 +373,46 @@ def decode_attention_mass(q: np.ndarray, K: np.ndarray) -> np.ndarray:
         e = np.exp(s)
         A[h] += e / e.sum()
     return A / G
+
+
+# --------------------------------------------------------------------------------------
+# A cache held in 4 bits (no counterpart in the paper): groups of 32 channels, a scale s and codes n, value s (n - 8)
+# --------------------------------------------------------------------------------------
+Q4_GROUP = 32
+
+
+def q4_quantise(X: np.ndarray):
+    """X [..., d] bf16 bits -> (codes [..., d] int 0..15, scales [..., d / 32] float64).  Per group with maximum M and
+    minimum m: x* = M if M >= -m else m; s = -x* / 8 rounded to 5 significant bits (ties to even), then to fp16's grid
+    (multiples of 2^-24), |s| <= 896; n = 8 + clamp(rint(x / s), -8, 7), 8 where s is 0.  A group with a NaN or an infinity:
+    s NaN, codes 8."""
+    x = bf16_to_f64(X)
+    g = x.reshape(*x.shape[:-1], -1, Q4_GROUP)
+    with np.errstate(invalid="ignore", divide="ignore", over="ignore"):
+        M, m = g.max(-1), g.min(-1)
+        t = -np.where(M >= -m, M, m) / 8
+        mant, exp = np.frexp(t)                                    # t = mant 2^exp, mant in [1/2, 1)
+        s = np.clip(np.rint(mant * 32) * np.exp2(exp - 5.0), -896, 896)
+        s = np.where(np.abs(s) < 2.0 ** -14, np.rint(s * 2.0 ** 24) * 2.0 ** -24, s)
+        s = np.where(np.isfinite(t), s, np.nan)
+        n = 8 + np.clip(np.rint(g / s[..., None]), -8, 7)          # exact: ties are multiples of s / 2
+    n = np.where(np.isfinite(s)[..., None] & (s[..., None] != 0), n, 8)
+    return n.astype(np.int64).reshape(x.shape), s
+
+
+def q4_values(codes: np.ndarray, scales: np.ndarray) -> np.ndarray:
+    """float64 values s (n - 8) of codes [..., d] and scales [..., d / 32]."""
+    return (np.asarray(codes) - 8.0) * np.repeat(scales, Q4_GROUP, -1)
+
+
+def q4_decode_attention(q: np.ndarray, K: np.ndarray, V: np.ndarray) -> np.ndarray:
+    """decode_attention over values K, V [Hkv, n, d] float64 (q [Hq, d] bf16 bits); no keys: zeros."""
+    qf = bf16_to_f64(q)
+    Hq, d = qf.shape
+    G = Hq // K.shape[0]
+    out = np.zeros((Hq, d))
+    for g in range(Hq if K.shape[1] else 0):
+        s = K[g // G] @ qf[g] / math.sqrt(d)
+        e = np.exp(s - s.max())
+        out[g] = (e / e.sum()) @ V[g // G]
+    return out

@@ -66,6 +66,12 @@ class CProblem(ctypes.Structure):
                 ("sal_lse", ctypes.c_void_p)]
 
 
+class CQ4Cache(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("K", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
+                ("code_head_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64)]
+
+
 STEPKV_MEM_DEVICE = 0
 STEPKV_MEM_HOST = 1
 
@@ -101,6 +107,13 @@ SIGNATURES = {
                                  _SZ, _VP, _VP]),
     "stepkv_decode": (_I32, [_I32, _VP, _VP, _VP, _I64, _I32, _I32, _I32, _VP, _I32, _I32, _VP, _VP, _SZ, _VP,
                              _VP]),
+    "stepkv_q4_write": (_I32, [ctypes.POINTER(CQ4Cache), _VP, _VP, _I64, _I64, _I32, _VP, _VP, _I32, _VP, _I32, _I32, _VP,
+                               _VP]),
+    "stepkv_q4_read": (_I32, [ctypes.POINTER(CQ4Cache), _VP, _VP, _I32, _VP, _I32, _I32, _VP, _VP, _I64, _I64, _VP, _VP]),
+    "stepkv_q4_compact": (_I32, [ctypes.POINTER(CQ4Cache), _I32, _VP, _VP, _I32, ctypes.POINTER(CQ4Cache), _VP, _VP, _VP,
+                                 _VP, _VP, _VP]),
+    "stepkv_q4_decode_workspace_size": (_SZ, [_I32, _I32, _I32, _I32, _I32]),
+    "stepkv_q4_decode": (_I32, [ctypes.POINTER(CQ4Cache), _VP, _I32, _VP, _I32, _I32, _I32, _VP, _VP, _SZ, _VP, _VP]),
     "stepkv_compress_workspace_size": (_SZ, [ctypes.POINTER(CProblem), _I32]),
     "stepkv_compress": (_I32, [ctypes.POINTER(CProblem), _I32, ctypes.POINTER(CParams), _VP, _SZ, _VP, _VP]),
 }
@@ -714,3 +727,261 @@ def stepkv_compress(problems: Sequence[Problem], params: Params, ws=None, status
     code = lib.stepkv_compress(arr, len(probs), ctypes.byref(cp), wp, wn, status.data_ptr(), _stream_handle(stream))
     _check(code, "stepkv_compress")
     return status
+
+
+# ----------------------------------------------------------------------------- a cache held in 4 bits
+Q4_GROUP = 32  # channels that share a scale (STEPKV_Q4_GROUP in the header)
+
+
+class _PerLayer:
+    """Per-layer tensors of one layout: a list, or one tensor with the layers in front (whose pointers need no look at
+    each layer)."""
+    __slots__ = ("ptrs", "shape", "strides", "device", "n", "keep")
+
+    def __init__(self, x, dtype, ndim, name):
+        torch = _torch()
+        if isinstance(x, torch.Tensor):
+            _need(x, dtype, name, ndim + 1)
+            self.n, self.shape, self.strides = x.shape[0], tuple(x.shape[1:]), tuple(x.stride()[1:])
+            base, step = x.data_ptr(), x.stride(0) * x.element_size()
+            self.ptrs = (ctypes.c_void_p * max(1, self.n))(*[base + l * step for l in range(self.n)])
+            self.device = x.device
+        else:
+            x = list(x)
+            self.n = len(x)
+            if self.n:
+                _need_all(x, lambda t, nm: _need(t, dtype, nm, ndim), name)
+                self.shape, self.strides, self.device = tuple(x[0].shape), tuple(x[0].stride()), x[0].device
+                lay = _layout(torch, x[0])
+                if any(_layout(torch, t) != lay or t.device != self.device for t in x[1:]):
+                    raise ValueError(f"all {name} tensors must be laid out alike, on one device")
+            self.ptrs = _ptr_array(x)
+        if self.n < 1:
+            raise ValueError(f"{name} needs at least one layer")
+        self.keep = x
+
+    @property
+    def arg(self):
+        return ctypes.cast(self.ptrs, ctypes.c_void_p)
+
+
+def _same_device(dev, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != dev:
+            raise ValueError(f"{name} is on {t.device}, the cache on {dev}")
+
+
+def _call_on(dev, stream, where, call):
+    """call(stream handle) with `dev` as the current device (the library launches on the current one), on `stream` or
+    the device's current stream."""
+    torch = _torch()
+    if stream is not None and stream.device != dev:
+        raise ValueError(f"{where}: the stream is on {stream.device}, the tensors on {dev}")
+    if dev.index == torch.cuda.current_device():
+        _check(call(_stream_handle(stream)), where)
+    else:
+        with torch.cuda.device(dev):
+            _check(call(_stream_handle(stream)), where)
+
+
+def _int32_vector(t, name, dev, least=1):
+    _need(t, _torch().int32, name)
+    if t.dim() > 1 or not t.is_contiguous() or t.numel() < least:
+        raise ValueError(f"{name} must be a contiguous int32 vector of at least {least}")
+    _same_device(dev, **{name: t})
+    return t
+
+
+class Q4Cache:
+    """A KV cache held in 4 bits (format in include/stepkv.h).  K, V: codes, per layer [Hkv, rows, d / 2] uint8;
+    K_scale, V_scale: [Hkv, rows, d / 32] float16; each a list of per-layer tensors or one tensor with the layers in
+    front.  V and V_scale None: keys alone.  The checked C struct is built once: the tensors must not be replaced."""
+
+    def __init__(self, K, K_scale, V=None, V_scale=None):
+        torch = _torch()
+        if (V is None) != (V_scale is None):
+            raise ValueError("V and V_scale go together")
+        self.K, self.K_scale, self.V, self.V_scale = K, K_scale, V, V_scale
+        parts = [(K, torch.uint8, "K"), (K_scale, torch.float16, "K_scale")]
+        if V is not None:
+            parts += [(V, torch.uint8, "V"), (V_scale, torch.float16, "V_scale")]
+        self._parts = [_PerLayer(x, t, 3, name) for x, t, name in parts]
+        codes, scales = self._parts[0], self._parts[1]
+        self.n_layers, (self.Hkv, self.rows, half) = codes.n, codes.shape
+        self.d, self.device = 2 * half, codes.device
+        if self.rows < 1 or self.d < Q4_GROUP or self.d % Q4_GROUP:
+            raise ValueError("codes must be [Hkv, rows >= 1, d / 2] with d a multiple of 32")
+        width = {torch.uint8: half, torch.float16: self.d // Q4_GROUP}
+        for p, (_, t, name), like in zip(self._parts, parts, (codes, scales) * 2):
+            w = width[t]
+            if p.n != self.n_layers or p.shape != (self.Hkv, self.rows, w) or p.device != self.device:
+                raise ValueError(f"{name} must be {self.n_layers} x [{self.Hkv}, {self.rows}, {w}] on {self.device}")
+            if p.strides[2] != 1 or (self.rows > 1 and p.strides[1] != w):
+                raise ValueError(f"{name} rows must be dense")
+            if self.Hkv > 1 and p.strides[0] != like.strides[0]:
+                raise ValueError(f"{name} must share the head stride of {'K' if t == torch.uint8 else 'K_scale'}")
+        stride = [p.strides[0] if self.Hkv > 1 else self.rows * p.shape[2] for p in (codes, scales)]
+        args = [p.arg for p in self._parts] + [None, None]
+        self._c = CQ4Cache(self.n_layers, self.Hkv, self.d, self.rows, *args[:4], *stride)
+
+    @staticmethod
+    def allocate(n_layers: int, Hkv: int, rows: int, d: int, device="cuda", values: bool = True) -> "Q4Cache":
+        """An empty cache (zeroed: every row reads back as 0)."""
+        torch = _torch()
+        z = lambda w, t: torch.zeros((n_layers, Hkv, rows, w), dtype=t, device=device)
+        kv = [x for _ in range(1 + values) for x in (z(d // 2, torch.uint8), z(d // Q4_GROUP, torch.float16))]
+        return Q4Cache(*kv)
+
+    def layers(self, lo: int, hi: Optional[int] = None) -> "Q4Cache":
+        """Layers lo .. hi of this cache (as a slice of a list takes them), sharing its memory."""
+        part = lambda x: None if x is None else x[lo:hi]
+        return Q4Cache(part(self.K), part(self.K_scale), part(self.V), part(self.V_scale))
+
+    def c(self):
+        return ctypes.byref(self._c)
+
+
+def _q4_rows(cache, row0, n, limit):
+    """(n_dev, n, row0_dev, stride, row0) as the C calls take them, device vectors as tensors (the caller holds them until
+    the launch: freed earlier, their memory would go to its next allocation); n None: the limit."""
+    n_dev = row0_dev = None
+    if n is None:
+        n = limit
+    elif not isinstance(n, int):
+        n_dev, n = _int32_vector(n, "n", cache.device), limit
+    elif not 0 <= n <= limit:
+        raise ValueError(f"n = {n} rows, at most {limit} here")
+    stride = 0
+    if not isinstance(row0, int):
+        row0_dev, row0 = _int32_vector(row0, "row0", cache.device), 0
+        if row0_dev.numel() not in (1, cache.n_layers):
+            raise ValueError("row0 must hold one row, or one for each layer")
+        stride = int(row0_dev.numel() > 1)
+    return n_dev, n, row0_dev, stride, row0
+
+
+def _q4_bf16(cache, K, V, what):
+    """The bf16 side of a write or read: per layer [Hkv, rows, d] with unit stride in d, K and V laid out alike."""
+    torch = _torch()
+    p = [None if x is None else _PerLayer(x, torch.bfloat16, 3, name) for x, name in ((K, "K"), (V, "V"))]
+    some = p[0] or p[1]
+    if some is None:
+        raise ValueError(f"{what} needs K or V")
+    H, rows, d = some.shape
+    if (some.n, H, d) != (cache.n_layers, cache.Hkv, cache.d):
+        raise ValueError(f"{what}: {some.n} x [{H}, {rows}, {d}] does not fit {cache.n_layers} layers of {cache.Hkv} heads "
+                         f"of {cache.d}")
+    if some.strides[2] != 1:
+        raise ValueError(f"{what}: the channels of a row must be contiguous")
+    for x in p:
+        if x is not None and (x.shape, x.strides, x.n, x.device) != (some.shape, some.strides, some.n, cache.device):
+            raise ValueError(f"{what}: K and V must be laid out alike, on the cache's device")
+    return p[0], p[1], rows, some.strides[0] if H > 1 else rows * d, some.strides[1] if rows > 1 else d
+
+
+def stepkv_q4_write(cache: Q4Cache, K, V, row0, n=None, idx=None, status=None, stream=None):
+    """Quantises rows of K and V (per layer [Hkv, T, d] bf16, any head and row strides; V None for a cache of keys) into
+    rows row0, row0 + 1, ... of the cache: rows idx[0], idx[1], ... of K and V, or all of them in order.  row0: an int, or
+    a device int32 tensor of one row or one per layer; n: how many rows (default all), an int or a device int32
+    tensor.  Returns the status word."""
+    lib = load_library()
+    k, v, T, hs, rs = _q4_bf16(cache, K, V, "stepkv_q4_write")
+    if k is None or (v is None) != (cache.V is None):
+        raise ValueError("stepkv_q4_write needs K, and V exactly where the cache holds values")
+    if idx is not None:
+        _int32_vector(idx, "idx", cache.device, 0)
+    n_dev, n, row0_dev, stride, row0 = _q4_rows(cache, row0, n, T if idx is None else idx.numel())
+    status = status if status is not None else new_status(cache.device)
+    _same_device(cache.device, status=status)
+    _call_on(cache.device, stream, "stepkv_q4_write", lambda s: lib.stepkv_q4_write(
+        cache.c(), k.arg, None if v is None else v.arg, hs, rs, T, _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev), stride, row0,
+        status.data_ptr(), s))
+    return status
+
+
+def stepkv_q4_read(cache: Q4Cache, row0=0, n=None, idx=None, K=None, V=None, status=None, stream=None):
+    """Rows row0, row0 + 1, ... (or idx[0], idx[1], ...) of the cache as bf16, exactly: returns (K, V), per layer
+    [Hkv, >= n, d].  n: an int or a device int32 tensor, default as many as K and V (or idx, or the cache from an int row0
+    on) hold.  Give K or V alone to read only that; neither: both are allocated as [n_layers, Hkv, n, d] (a device n: with
+    room for all, zero past n)."""
+    torch = _torch()
+    lib = load_library()
+    if idx is not None:
+        _int32_vector(idx, "idx", cache.device, 0)
+    if K is None and V is None:
+        room = idx.numel() if idx is not None else cache.rows - (row0 if isinstance(row0, int) else 0)
+        new = torch.empty if n is None or isinstance(n, int) else torch.zeros
+        shape = (cache.n_layers, cache.Hkv, n if isinstance(n, int) else max(room, 0), cache.d)
+        K = new(shape, dtype=torch.bfloat16, device=cache.device)
+        V = None if cache.V is None else new(shape, dtype=torch.bfloat16, device=cache.device)
+    if V is not None and cache.V is None:
+        raise ValueError("stepkv_q4_read: the cache holds no values")
+    k, v, rows, hs, rs = _q4_bf16(cache, K, V, "stepkv_q4_read")
+    n_dev, n, row0_dev, stride, row0 = _q4_rows(cache, row0, n, rows if idx is None else min(rows, idx.numel()))
+    status = status if status is not None else new_status(cache.device)
+    _same_device(cache.device, status=status)
+    _call_on(cache.device, stream, "stepkv_q4_read", lambda s: lib.stepkv_q4_read(
+        cache.c(), _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev), stride, row0, None if k is None else k.arg,
+        None if v is None else v.arg, hs, rs, status.data_ptr(), s))
+    return K, V
+
+
+def stepkv_q4_compact(cache: Q4Cache, T: int, kept_idx, n_kept, kept_cap: int, out: Q4Cache, step_id_in=None, pos_in=None,
+                      step_id_out=None, pos_out=None, status=None, stream=None):
+    """stepkv_compact over a cache held in 4 bits: row r of `out` = row kept_idx[r] of `cache`, bit for bit.  Returns the
+    status word."""
+    lib = load_library()
+    dev = cache.device
+    _int32_vector(kept_idx, "kept_idx", dev, kept_cap)
+    _int32_vector(n_kept, "n_kept", dev)
+    for t, name, least in ((step_id_in, "step_id_in", T), (pos_in, "pos_in", T), (step_id_out, "step_id_out", kept_cap),
+                           (pos_out, "pos_out", kept_cap)):
+        if t is not None:
+            _int32_vector(t, name, dev, least)
+    status = status if status is not None else new_status(dev)
+    _same_device(dev, status=status, out=out)
+    _call_on(dev, stream, "stepkv_q4_compact", lambda s: lib.stepkv_q4_compact(
+        cache.c(), T, kept_idx.data_ptr(), n_kept.data_ptr(), kept_cap, out.c(), _ptr(step_id_in), _ptr(pos_in),
+        _ptr(step_id_out), _ptr(pos_out), status.data_ptr(), s))
+    return status
+
+
+def q4_decode_workspace(cache: Q4Cache, Hq: int):
+    """A workspace for stepkv_q4_decode calls over this cache (one call at a time may use it)."""
+    torch = _torch()
+    need = load_library().stepkv_q4_decode_workspace_size(cache.n_layers, cache.Hkv, Hq, cache.d, cache.rows)
+    return torch.empty(need + 512, dtype=torch.uint8, device=cache.device)
+
+
+def stepkv_q4_decode(q, cache: Q4Cache, n, out=None, ws=None, status=None, stream=None):
+    """One query token per layer (or per trajectory of a batch) over a cache held in 4 bits: stepkv_decode's formula.
+
+    q: per layer [Hq, d] bf16; n: an int, or a device int32 tensor of one count or one per layer (0: the output is
+    zero).  Returns out, per layer [Hq, d] fp32, as a list or (where q is one tensor) one tensor."""
+    torch = _torch()
+    lib = load_library()
+    qs = _PerLayer(q, torch.bfloat16, 2, "q")
+    Hq = qs.shape[0]
+    if qs.n != cache.n_layers or qs.shape[1] != cache.d or cache.V is None:
+        raise ValueError("stepkv_q4_decode needs one [Hq, d] query per layer of a cache with keys and values")
+    if out is None:
+        out = torch.empty((cache.n_layers, Hq, cache.d), dtype=torch.float32, device=cache.device)
+        out = out if isinstance(q, torch.Tensor) else list(out)
+    outs = _PerLayer(out, torch.float32, 2, "out")
+    for x, name in ((qs, "q"), (outs, "out")):
+        if x.n != cache.n_layers or x.shape != qs.shape or x.strides != (cache.d, 1) or x.device != cache.device:
+            raise ValueError(f"{name} must be contiguous [Hq, d] per layer, on the cache's device")
+    n_dev, stride = None, 0
+    if not isinstance(n, int):
+        n_dev, n = _int32_vector(n, "n", cache.device), 0
+        if n_dev.numel() not in (1, cache.n_layers):
+            raise ValueError("n must hold one count, or one for each layer")
+        stride = int(n_dev.numel() > 1)
+    if ws is None:
+        ws = q4_decode_workspace(cache, Hq)
+    wp, wn = _aligned_ws(ws)
+    status = status if status is not None else new_status(cache.device)
+    _same_device(cache.device, ws=ws, status=status)
+    _call_on(cache.device, stream, "stepkv_q4_decode", lambda s: lib.stepkv_q4_decode(
+        cache.c(), qs.arg, Hq, _ptr(n_dev), stride, n, cache.rows, outs.arg, wp, wn, status.data_ptr(), s))
+    return out

@@ -416,6 +416,117 @@ stepkv_status_t stepkv_decode(int32_t n_layers, const void* const* q, const void
                     static_cast<cudaStream_t>(stream));
 }
 
+// ---- a cache held in 4 bits
+// `values`: 1 where the call needs the cache's values, 0 where it does not use them, -1 where the cache may hold keys alone.
+static stepkv_status_t check_q4_cache(const stepkv_q4_cache_t* c, int values) {
+  if (!c || c->n_layers < 1 || c->Hkv < 1 || c->d < 1 || c->rows < 1) return STEPKV_EINVAL;
+  if (c->d % STEPKV_Q4_GROUP || c->d > 256) return STEPKV_EUNSUPPORTED;
+  if (!c->K || !c->K_scale || (c->V == nullptr) != (c->V_scale == nullptr)) return STEPKV_EINVAL;
+  if (values > 0 && !c->V) return STEPKV_EINVAL;
+  const int groups = c->d / STEPKV_Q4_GROUP;
+  if (c->code_head_stride < (int64_t)c->rows * (c->d / 2) || c->scale_head_stride < (int64_t)c->rows * groups)
+    return STEPKV_EINVAL;
+  if (c->code_head_stride % 16 || c->scale_head_stride % groups) return STEPKV_EUNSUPPORTED;
+  // a row's scales are read as one word where their number is a power of two
+  const uintptr_t scale_mask = 2u * (groups & -groups) - 1u;
+  for (int l = 0; l < c->n_layers; ++l) {
+    if (!c->K[l] || !c->K_scale[l]) return STEPKV_EINVAL;
+    if (!aligned16(c->K[l]) || (reinterpret_cast<uintptr_t>(c->K_scale[l]) & scale_mask)) return STEPKV_EUNSUPPORTED;
+    if (c->V && values != 0) {
+      if (!c->V[l] || !c->V_scale[l]) return STEPKV_EINVAL;
+      if (!aligned16(c->V[l]) || (reinterpret_cast<uintptr_t>(c->V_scale[l]) & scale_mask)) return STEPKV_EUNSUPPORTED;
+    }
+  }
+  return STEPKV_OK;
+}
+
+// bf16 rows at any order of heads and rows: pointers present and aligned, strides that keep every row aligned.
+static stepkv_status_t check_q4_rows(int n_layers, const void* const* K, const void* const* V, int64_t head_stride,
+                                     int64_t row_stride, const Q4Rows& r) {
+  if (r.n < 0 || head_stride < 0 || row_stride < 0) return STEPKV_EINVAL;
+  if (r.row0_dev && r.row0_stride != 0 && r.row0_stride != 1) return STEPKV_EINVAL;
+  if (head_stride % 8 || row_stride % 8) return STEPKV_EUNSUPPORTED;
+  for (int l = 0; l < (r.n > 0 ? n_layers : 0); ++l) {  // (no rows: an empty tensor has no address)
+    if ((K && !K[l]) || (V && !V[l])) return STEPKV_EINVAL;
+    if ((K && !aligned16(K[l])) || (V && !aligned16(V[l]))) return STEPKV_EUNSUPPORTED;
+  }
+  return STEPKV_OK;
+}
+
+stepkv_status_t stepkv_q4_write(const stepkv_q4_cache_t* cache, const void* const* K, const void* const* V,
+                                int64_t head_stride, int64_t row_stride, int32_t T, const int32_t* idx,
+                                const int32_t* n_dev, int32_t n, const int32_t* row0_dev, int32_t row0_dev_stride,
+                                int32_t row0, int32_t* dev_status, void* stream) {
+  stepkv_status_t st = check_q4_cache(cache, -1);
+  if (st != STEPKV_OK) return st;
+  if (!K || (V == nullptr) != (cache->V == nullptr) || T < 0) return STEPKV_EINVAL;
+  const Q4Rows r{idx, n_dev, n, row0_dev, row0_dev_stride, row0};
+  st = check_q4_rows(cache->n_layers, K, V, head_stride, row_stride, r);
+  if (st != STEPKV_OK) return st;
+  if (!idx && n > T) return STEPKV_EINVAL;
+  if (!row0_dev && !n_dev && (row0 < 0 || (int64_t)row0 + n > cache->rows)) return STEPKV_ENOSPACE;
+  if (n == 0) return STEPKV_OK;
+  return q4_write_run(*cache, K, V, head_stride, row_stride, T, r, dev_status, static_cast<cudaStream_t>(stream));
+}
+
+stepkv_status_t stepkv_q4_read(const stepkv_q4_cache_t* cache, const int32_t* idx, const int32_t* n_dev, int32_t n,
+                               const int32_t* row0_dev, int32_t row0_dev_stride, int32_t row0, void* const* K,
+                               void* const* V, int64_t head_stride, int64_t row_stride, int32_t* dev_status,
+                               void* stream) {
+  stepkv_status_t st = check_q4_cache(cache, V != nullptr);
+  if (st != STEPKV_OK) return st;
+  if (!K && !V) return STEPKV_EINVAL;
+  const Q4Rows r{idx, n_dev, n, row0_dev, row0_dev_stride, row0};
+  st = check_q4_rows(cache->n_layers, K, V, head_stride, row_stride, r);
+  if (st != STEPKV_OK) return st;
+  if ((head_stride < cache->d && cache->Hkv > 1) || (row_stride < cache->d && n > 1)) return STEPKV_EINVAL;  // rows apart
+  if (!idx && !row0_dev && !n_dev && (row0 < 0 || (int64_t)row0 + n > cache->rows)) return STEPKV_EINVAL;
+  if (n == 0) return STEPKV_OK;
+  return q4_read_run(*cache, r, K, V, head_stride, row_stride, dev_status, static_cast<cudaStream_t>(stream));
+}
+
+stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_t T, const int32_t* kept_idx, const int32_t* n_kept,
+                                  int32_t kept_cap, const stepkv_q4_cache_t* out, const int32_t* step_id_in,
+                                  const int32_t* pos_in, int32_t* step_id_out, int32_t* pos_out, int32_t* dev_status,
+                                  void* stream) {
+  stepkv_status_t st = check_q4_cache(in, -1);
+  if (st == STEPKV_OK) st = check_q4_cache(out, -1);
+  if (st != STEPKV_OK) return st;
+  if (in->n_layers != out->n_layers || in->Hkv != out->Hkv || in->d != out->d) return STEPKV_EINVAL;
+  if ((in->V == nullptr) != (out->V == nullptr)) return STEPKV_EINVAL;
+  if (T < 1 || T > in->rows || kept_cap < 0 || kept_cap > out->rows || !kept_idx || !n_kept) return STEPKV_EINVAL;
+  for (int l = 0; l < in->n_layers; ++l) {
+    if (in->K[l] == out->K[l] || in->K_scale[l] == out->K_scale[l]) return STEPKV_EUNSUPPORTED;
+    if (in->V && (in->V[l] == out->V[l] || in->V_scale[l] == out->V_scale[l])) return STEPKV_EUNSUPPORTED;
+  }
+  return q4_compact_run(*in, T, kept_idx, n_kept, kept_cap, *out, step_id_in, pos_in, step_id_out, pos_out, dev_status,
+                        static_cast<cudaStream_t>(stream));
+}
+
+size_t stepkv_q4_decode_workspace_size(int32_t n_layers, int32_t Hkv, int32_t Hq, int32_t d, int32_t n_cap) {
+  if (n_layers < 1 || Hkv < 1 || Hq < Hkv || n_cap < 1 || (d != 64 && d != 128)) return 0;
+  return q4_decode_ws_bytes(std::min(n_layers, kQ4Layers), Hkv, Hq, d, n_cap);
+}
+
+stepkv_status_t stepkv_q4_decode(const stepkv_q4_cache_t* cache, const void* const* q, int32_t Hq, const int32_t* n_dev,
+                                 int32_t n_dev_stride, int32_t n_host, int32_t n_cap, float* const* out, void* ws,
+                                 size_t ws_bytes, int32_t* dev_status, void* stream) {
+  stepkv_status_t st = check_q4_cache(cache, 1);
+  if (st != STEPKV_OK) return st;
+  if (!q || !out || !ws || Hq < 1 || Hq % cache->Hkv != 0 || n_cap < 1 || n_cap > cache->rows) return STEPKV_EINVAL;
+  if (cache->d != 64 && cache->d != 128) return STEPKV_EUNSUPPORTED;
+  if (Hq / cache->Hkv > 8) return STEPKV_EUNSUPPORTED;
+  if (n_dev ? (n_dev_stride != 0 && n_dev_stride != 1) : (n_host < 0 || n_host > n_cap)) return STEPKV_EINVAL;
+  if (ws_bytes < stepkv_q4_decode_workspace_size(cache->n_layers, cache->Hkv, Hq, cache->d, n_cap)) return STEPKV_ENOSPACE;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return STEPKV_EINVAL;
+  for (int l = 0; l < cache->n_layers; ++l) {
+    if (!q[l] || !out[l]) return STEPKV_EINVAL;
+    if (!aligned16(q[l]) || !aligned16(out[l])) return STEPKV_EUNSUPPORTED;
+  }
+  return q4_decode_run(*cache, q, Hq, n_dev, n_dev_stride, n_host, n_cap, out, ws, dev_status,
+                       static_cast<cudaStream_t>(stream));
+}
+
 stepkv_status_t stepkv_step_signals(const uint32_t* cues, const int32_t* n_cues, int32_t n_steps, int32_t k0,
                                     float* gain, float* red, float* obs_sim, int32_t* dev_status, void* stream) {
   if (!cues || !n_cues || n_steps < 1 || n_steps > 65535 || k0 < 0 || k0 > n_steps) return STEPKV_EINVAL;

@@ -90,6 +90,28 @@ stepkv_status_t decode_run(int n_layers, const void* const* q, const void* const
                            float* const* out, void* ws, int32_t* status, cudaStream_t stream,
                            float* const* mass = nullptr, int64_t mass_stride = 0);
 
+// ---- a cache held in 4 bits (q4.cu, q4_decode.cu)
+constexpr int kQ4Layers = 64;  // layers per launch (pointer arrays travel in the kernel parameters)
+// The rows of one call: r < n (n_dev: *n_dev, n its limit), cache rows row0 + r (row0_dev: row0_dev[layer * row0_stride]).
+struct Q4Rows {
+  const int32_t* idx;
+  const int32_t* n_dev;
+  int n;
+  const int32_t* row0_dev;
+  int row0_stride;
+  int row0;
+};
+stepkv_status_t q4_write_run(const stepkv_q4_cache_t& c, const void* const* K, const void* const* V, int64_t head_stride,
+                             int64_t row_stride, int T, const Q4Rows& rows, int32_t* status, cudaStream_t stream);
+stepkv_status_t q4_read_run(const stepkv_q4_cache_t& c, const Q4Rows& rows, void* const* K, void* const* V,
+                            int64_t head_stride, int64_t row_stride, int32_t* status, cudaStream_t stream);
+stepkv_status_t q4_compact_run(const stepkv_q4_cache_t& in, int T, const int32_t* kept_idx, const int32_t* n_kept,
+                               int kept_cap, const stepkv_q4_cache_t& out, const int32_t* step_id_in, const int32_t* pos_in,
+                               int32_t* step_id_out, int32_t* pos_out, int32_t* status, cudaStream_t stream);
+size_t q4_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap);
+stepkv_status_t q4_decode_run(const stepkv_q4_cache_t& c, const void* const* q, int Hq, const int32_t* n_dev, int n_stride,
+                              int n_host, int n_cap, float* const* out, void* ws, int32_t* status, cudaStream_t stream);
+
 // ---- step signals from evidence cues (signals.cu)
 stepkv_status_t signals_run(const uint32_t* cues, const int32_t* n_cues, int n_steps, int k0, float* gain, float* red,
                             float* obs_sim, int32_t* status, cudaStream_t stream);
