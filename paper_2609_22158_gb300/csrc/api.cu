@@ -516,6 +516,9 @@ stepkv_status_t stepkv_q4_decode(const stepkv_q4_cache_t* cache, const void* con
   if (!q || !out || !ws || Hq < 1 || Hq % cache->Hkv != 0 || n_cap < 1 || n_cap > cache->rows) return STEPKV_EINVAL;
   if (cache->d != 64 && cache->d != 128) return STEPKV_EUNSUPPORTED;
   if (Hq / cache->Hkv > 8) return STEPKV_EUNSUPPORTED;
+  // the blocks of a launch are counted in 32 bits
+  if ((int64_t)std::min(cache->n_layers, kQ4Layers) * cache->Hkv * ((int64_t)n_cap / 32 + 1) >= ((int64_t)1 << 30))
+    return STEPKV_EUNSUPPORTED;
   if (n_dev ? (n_dev_stride != 0 && n_dev_stride != 1) : (n_host < 0 || n_host > n_cap)) return STEPKV_EINVAL;
   if (ws_bytes < stepkv_q4_decode_workspace_size(cache->n_layers, cache->Hkv, Hq, cache->d, n_cap)) return STEPKV_ENOSPACE;
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return STEPKV_EINVAL;
