@@ -7,8 +7,8 @@
 // Five bits of scale times three of code fit bf16's eight, so reading back is exact, and so is quantising what was read
 // back.  Everything is row-local, so a compaction moves codes and scales as they are.
 //
-// All three kernels stream: a warp takes chunks of a few rows of one row set (layer, tensor, head), a lane 8 channels
-// (16 bytes of bf16, one 32-bit word of codes), a quad of lanes a group.
+// All three kernels stream: a warp takes chunks of a few rows of one row set (layer, tensor, head), loads everything a
+// chunk needs before it uses any of it, and steps to its next chunk without a division.
 #include <cuda_fp16.h>
 
 #include <algorithm>
@@ -20,7 +20,6 @@
 namespace stepkv {
 
 constexpr int kQ4Threads = 256;
-constexpr int kQ4Unroll = 4;       // row groups of a warp's chunk
 
 struct Q4Args {
   const void* src[2 * kQ4Layers];  // per (layer, tensor): bf16 rows, or the codes where they are read
@@ -58,44 +57,71 @@ __device__ __forceinline__ void q4_st_stream(void* p, const uint4& v) {
   asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-// max / min that give NaN where either is one
-__device__ __forceinline__ float max_nan(float a, float b) {
+// The larger halves of two bf16 pairs, NaN where either is one.
+__device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ float rcp_approx(float x) {
   float r;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(r) : "f"(a), "f"(b));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(x));
   return r;
 }
 
-// The scale of a group from its maximum and minimum.
-__device__ __forceinline__ __half q4_scale(float hi, float lo) {
-  const float x = hi >= -lo ? hi : lo;
+// The scale of a group whose maximum is hi and minimum -neg_lo.
+__device__ __forceinline__ __half q4_scale(float hi, float neg_lo) {
+  const float x = hi >= neg_lo ? hi : -neg_lo;
   if (!(fabsf(x) < INFINITY)) return __ushort_as_half(0x7FFF);
   uint32_t b = __float_as_uint(x * -0.125f);
   b = (b + 0x3FFFFu + ((b >> 19) & 1u)) & ~0x7FFFFu;  // 4 of the 23 explicit bits, ties to even
   return __float2half_rn(fminf(fmaxf(__uint_as_float(b), -896.f), 896.f));
 }
 
-// The codes of 8 channels as one word, channel i in bits 4i .. 4i + 3.
-__device__ __forceinline__ uint32_t q4_codes(const float (&x)[8], __half s) {
-  const float step = __half2float(s);
-  uint32_t w = 0;
-#pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    const float q = step == 0.f || step != step ? 0.f : fminf(fmaxf(rintf(x[i] / step), -8.f), 7.f);
-    w |= (uint32_t)((int)q + 8) << (4 * i);
-  }
-  return w;
-}
-
-__device__ __forceinline__ void bf16x8_to_float(const uint4& v, float (&x)[8]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+// The codes of 8 channels (four bf16 pairs) as one word, channel i in bits 4i .. 4i + 3; inv: 1 / s (0 where s is 0).
+// rint(x / s) with the exact quotient's ties: x has 8 bits and s 5, so a quotient near a tie k + 1/2 (k < 8) is the tie or
+// at least 2^-8.95 from it, and x inv is off by 2^-19 at most.  Added to 6144 it is rounded to multiples of 2^-11, a tie to
+// itself and nothing else to a tie; the next sum rounds that to an integer, ties to even, which lies in the low bits.
+__device__ __forceinline__ uint32_t q4_codes(const uint32_t (&v)[4], float inv) {
+  constexpr float kMagic = 12582912.f;  // 1.5 2^23: the last place is 1
+  const uint64_t inv2 = f2_pack(inv, inv), c0 = f2_pack(6144.f, 6144.f), c1 = f2_pack(kMagic + 8.f - 6144.f, kMagic + 8.f - 6144.f);
+  float u[8];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
-    x[2 * i] = __uint_as_float(w[i] << 16);
-    x[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+    const uint64_t x = f2_pack(__uint_as_float(v[i] << 16), __uint_as_float(v[i] & 0xFFFF0000u));
+    f2_unpack(f2_add(f2_fma(x, inv2, c0), c1), u[2 * i], u[2 * i + 1]);
   }
+  uint32_t w = 0;
+#pragma unroll
+  for (int i = 7; i >= 0; --i)  // 16 w + bits of u: what the constant's bits add up to is taken off at the end
+    w = w * 16u + __float_as_uint(fminf(fmaxf(u[i], kMagic), kMagic + 15.f));
+  return w - (0x4B400000u * 0x11111111u);
 }
 
-// Where a warp's chunk lies: row set -> (layer, tensor) entry, layer and head.
+// The chunks of a warp: chunk `pos` of row set `set`, every `step`-th of the list of all sets' chunks.
+struct Q4Chunks {
+  int chunks, sets;         // of a set; sets in all
+  int set, pos;
+  int d_set, d_pos;
+  __device__ __forceinline__ Q4Chunks(int n, int per_chunk, int n_sets) : chunks((n + per_chunk - 1) / per_chunk), sets(n_sets) {
+    const int step = gridDim.x * (kQ4Threads / 32), first = blockIdx.x * (kQ4Threads / 32) + (threadIdx.x >> 5);
+    set = first / chunks;
+    pos = first - set * chunks;
+    d_set = step / chunks;
+    d_pos = step - d_set * chunks;
+  }
+  __device__ __forceinline__ bool any() const { return set < sets; }
+  __device__ __forceinline__ void next() {
+    set += d_set;
+    pos += d_pos;
+    if (pos >= chunks) {
+      pos -= chunks;
+      ++set;
+    }
+  }
+};
+
+// Where a row set lies: (layer, tensor) entry, layer and head.
 struct Q4Set {
   int lt, layer, h;
 };
@@ -106,68 +132,85 @@ __device__ __forceinline__ Q4Set q4_set(const Q4Args& a, int set) {
   return s;
 }
 
+// A lane takes 16 channels of a row, vectors (8 channels) v and v + 2 of a group with v = lane & 1, so that a pair of lanes has
+// a group and reads 32 consecutive bytes at a time.
+constexpr int kQ4WriteUnroll = 2;
+
 __global__ void __launch_bounds__(kQ4Threads) q4_write_kernel(const __grid_constant__ Q4Args a) {
   pdl_wait();
   pdl_launch_dependents();
   const int n = q4_count(a.r, a.status);
   if (n <= 0) return;
-  const int lpr = a.d >> 3, rpi = 32 / lpr;  // lanes a row, rows an instruction
+  const int lpr = a.d >> 4, rpi = 32 / lpr;  // lanes a row, rows an instruction
   const int lane = threadIdx.x & 31, sub = lane / lpr, col = lane - sub * lpr;
-  const int per_chunk = rpi * kQ4Unroll, chunks = (n + per_chunk - 1) / per_chunk;
-  const int total = a.sets * chunks;
-  const int warps = gridDim.x * (kQ4Threads / 32);
-  for (int c = blockIdx.x * (kQ4Threads / 32) + (threadIdx.x >> 5); c < total; c += warps) {
-    const int set = c / chunks, r0 = (c - set * chunks) * per_chunk;
-    const Q4Set s = q4_set(a, set);
+  const int vec = (col >> 1) * 4 + (col & 1);
+  const int per_chunk = rpi * kQ4WriteUnroll;
+  for (Q4Chunks c(n, per_chunk, a.sets); c.any(); c.next()) {
+    const Q4Set s = q4_set(a, c.set);
     const int row0 = a.r.row0_dev ? a.r.row0_dev[(a.layer0 + s.layer) * a.r.row0_stride] : a.r.row0;
     if (row0 < 0 || (int64_t)row0 + n > a.rows) {
       if (lane == 0) record_status(a.status, STEPKV_ENOSPACE);
       continue;
     }
-    const uint16_t* src = static_cast<const uint16_t*>(a.src[s.lt]) + (int64_t)s.h * a.head_stride + col * 8;
-    uint8_t* codes = static_cast<uint8_t*>(a.dst[s.lt]) + (int64_t)s.h * a.code_head_stride;
-    __half* scales = static_cast<__half*>(a.scale[s.lt]) + (int64_t)s.h * a.scale_head_stride;
-    uint4 v[kQ4Unroll];
-    bool ok[kQ4Unroll];
+    const uint16_t* src = static_cast<const uint16_t*>(a.src[s.lt]) + (int64_t)s.h * a.head_stride + vec * 8;
+    uint8_t* codes = static_cast<uint8_t*>(a.dst[s.lt]) + (int64_t)s.h * a.code_head_stride + vec * 4;
+    __half* scales = static_cast<__half*>(a.scale[s.lt]) + (int64_t)s.h * a.scale_head_stride + (col >> 1);
+    const int r0 = c.pos * per_chunk + sub;
+    uint4 v[kQ4WriteUnroll][2];
+    bool ok[kQ4WriteUnroll];
 #pragma unroll
-    for (int u = 0; u < kQ4Unroll; ++u) {
-      const int r = r0 + u * rpi + sub;
+    for (int u = 0; u < kQ4WriteUnroll; ++u) {
+      const int r = r0 + u * rpi;
       ok[u] = sub < rpi && r < n;
-      v[u] = make_uint4(0, 0, 0, 0);
+      const int t = ok[u] && a.r.idx ? a.r.idx[r] : r;
+      if (ok[u] && (t < 0 || t >= a.T)) {
+        record_status(a.status, STEPKV_EDATA);
+        ok[u] = false;
+      }
+      v[u][0] = v[u][1] = make_uint4(0, 0, 0, 0);
       if (ok[u]) {
-        const int t = a.r.idx ? a.r.idx[r] : r;
-        if (t < 0 || t >= a.T) {
-          record_status(a.status, STEPKV_EDATA);
-          ok[u] = false;
-        } else {
-          v[u] = q4_ld_stream(src + (int64_t)t * a.row_stride);
-        }
+        v[u][0] = q4_ld_stream(src + (int64_t)t * a.row_stride);
+        v[u][1] = q4_ld_stream(src + (int64_t)t * a.row_stride + 16);
       }
     }
 #pragma unroll
-    for (int u = 0; u < kQ4Unroll; ++u) {
-      float x[8];
-      bf16x8_to_float(v[u], x);
-      float hi = x[0], lo = x[0];
+    for (int u = 0; u < kQ4WriteUnroll; ++u) {
+      const uint32_t x[2][4] = {{v[u][0].x, v[u][0].y, v[u][0].z, v[u][0].w}, {v[u][1].x, v[u][1].y, v[u][1].z, v[u][1].w}};
+      // (maximum, -minimum) of the group as a bf16 pair
+      uint32_t hi = x[0][0], lo = x[0][0] ^ 0x80008000u;
 #pragma unroll
       for (int i = 1; i < 8; ++i) {
-        hi = max_nan(hi, x[i]);
-        lo = min_nan(lo, x[i]);
+        hi = max2_nan(hi, x[i >> 2][i & 3]);
+        lo = max2_nan(lo, x[i >> 2][i & 3] ^ 0x80008000u);
       }
+      uint32_t both = max2_nan(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
+      both = max2_nan(both, __shfl_xor_sync(0xffffffffu, both, 1));
+      const __half sc = q4_scale(__uint_as_float(both << 16), __uint_as_float(both & 0xFFFF0000u));
+      const float step = __half2float(sc);
+      const float inv = step == 0.f ? 0.f : rcp_approx(step);
+      uint32_t w[2];
 #pragma unroll
-      for (int o = 1; o < 4; o <<= 1) {
-        hi = max_nan(hi, __shfl_xor_sync(0xffffffffu, hi, o));
-        lo = min_nan(lo, __shfl_xor_sync(0xffffffffu, lo, o));
-      }
-      const __half sc = q4_scale(hi, lo);
-      const uint32_t w = q4_codes(x, sc);
+      for (int k = 0; k < 2; ++k) w[k] = step == step ? q4_codes(x[k], inv) : 0x88888888u;
       if (ok[u]) {
-        const int64_t row = (int64_t)row0 + r0 + u * rpi + sub;
-        *reinterpret_cast<uint32_t*>(codes + row * (a.d >> 1) + col * 4) = w;
-        if ((col & 3) == 0) scales[row * (a.d >> 5) + (col >> 2)] = sc;
+        const int64_t row = (int64_t)row0 + r0 + u * rpi;
+        uint32_t* dst = reinterpret_cast<uint32_t*>(codes + row * (a.d >> 1));
+        dst[0] = w[0];
+        dst[2] = w[1];
+        if ((col & 1) == 0) scales[row * (a.d >> 5)] = sc;
       }
     }
   }
+}
+
+// A lane takes a word of codes (8 channels).  The codes of a pair of channels become bf16 by a mask, s (n - 8) by one sum and
+// one product, both exact.
+constexpr int kQ4ReadUnroll = 8;
+
+__device__ __forceinline__ uint32_t q4_bf16_pair(uint32_t x, uint32_t s) {
+  uint32_t y, z;
+  asm("add.rn.bf16x2 %0, %1, %2;" : "=r"(y) : "r"((x & 0x000F000Fu) | 0x43004300u), "r"(0xC308C308u));  // (128 + n) - 136
+  asm("mul.rn.bf16x2 %0, %1, %2;" : "=r"(z) : "r"(y), "r"(s));
+  return z;
 }
 
 __global__ void __launch_bounds__(kQ4Threads) q4_read_kernel(const __grid_constant__ Q4Args a) {
@@ -177,12 +220,9 @@ __global__ void __launch_bounds__(kQ4Threads) q4_read_kernel(const __grid_consta
   if (n <= 0) return;
   const int lpr = a.d >> 3, rpi = 32 / lpr;
   const int lane = threadIdx.x & 31, sub = lane / lpr, col = lane - sub * lpr;
-  const int per_chunk = rpi * kQ4Unroll, chunks = (n + per_chunk - 1) / per_chunk;
-  const int total = a.sets * chunks;
-  const int warps = gridDim.x * (kQ4Threads / 32);
-  for (int c = blockIdx.x * (kQ4Threads / 32) + (threadIdx.x >> 5); c < total; c += warps) {
-    const int set = c / chunks, r0 = (c - set * chunks) * per_chunk;
-    const Q4Set s = q4_set(a, set);
+  const int per_chunk = rpi * kQ4ReadUnroll;
+  for (Q4Chunks c(n, per_chunk, a.sets); c.any(); c.next()) {
+    const Q4Set s = q4_set(a, c.set);
     int row0 = 0;
     if (!a.r.idx) {
       row0 = a.r.row0_dev ? a.r.row0_dev[(a.layer0 + s.layer) * a.r.row0_stride] : a.r.row0;
@@ -191,27 +231,39 @@ __global__ void __launch_bounds__(kQ4Threads) q4_read_kernel(const __grid_consta
         continue;
       }
     }
-    const uint8_t* codes = static_cast<const uint8_t*>(a.src[s.lt]) + (int64_t)s.h * a.code_head_stride;
-    const __half* scales = static_cast<const __half*>(a.scale[s.lt]) + (int64_t)s.h * a.scale_head_stride;
+    const uint8_t* codes = static_cast<const uint8_t*>(a.src[s.lt]) + (int64_t)s.h * a.code_head_stride + col * 4;
+    const __half* scales = static_cast<const __half*>(a.scale[s.lt]) + (int64_t)s.h * a.scale_head_stride + (col >> 2);
     uint16_t* dst = static_cast<uint16_t*>(a.dst[s.lt]) + (int64_t)s.h * a.head_stride + col * 8;
+    const int r0 = c.pos * per_chunk + sub;
+    uint32_t w[kQ4ReadUnroll];
+    __half sc[kQ4ReadUnroll];
+    bool ok[kQ4ReadUnroll];
 #pragma unroll
-    for (int u = 0; u < kQ4Unroll; ++u) {
-      const int r = r0 + u * rpi + sub;
-      if (sub >= rpi || r >= n) continue;
-      const int64_t row = a.r.idx ? a.r.idx[r] : (int64_t)row0 + r;
-      if (row < 0 || row >= a.rows) {
+    for (int u = 0; u < kQ4ReadUnroll; ++u) {
+      const int r = r0 + u * rpi;
+      ok[u] = sub < rpi && r < n;
+      const int64_t row = ok[u] && a.r.idx ? a.r.idx[r] : (int64_t)row0 + r;
+      if (ok[u] && (row < 0 || row >= a.rows)) {
         record_status(a.status, STEPKV_EDATA);
-        continue;
+        ok[u] = false;
       }
-      const uint32_t w = *reinterpret_cast<const uint32_t*>(codes + row * (a.d >> 1) + col * 4);
-      const float step = __half2float(scales[row * (a.d >> 5) + (col >> 2)]);
-      uint32_t o[4];
+      w[u] = 0;
+      sc[u] = __ushort_as_half(0);
+      if (ok[u]) {
+        w[u] = __ldg(reinterpret_cast<const uint32_t*>(codes + row * (a.d >> 1)));
+        sc[u] = __ldg(scales + row * (a.d >> 5));
+      }
+    }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {  // exact in bf16: the upper halves of the fp32 values
-        const float x = (float)((int)((w >> (8 * i)) & 15u) - 8) * step, y = (float)((int)((w >> (8 * i + 4)) & 15u) - 8) * step;
-        o[i] = __byte_perm(__float_as_uint(x), __float_as_uint(y), 0x7632);
-      }
-      q4_st_stream(dst + (int64_t)r * a.row_stride, make_uint4(o[0], o[1], o[2], o[3]));
+    for (int u = 0; u < kQ4ReadUnroll; ++u) {
+      const uint32_t f = __float_as_uint(__half2float(sc[u])), s2 = __byte_perm(f, f, 0x3232);  // exact in bf16
+      uint32_t x[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[i] = q4_bf16_pair(w[u] >> (4 * i), s2);  // channels i and i + 4
+      if (ok[u])
+        q4_st_stream(dst + (int64_t)(r0 + u * rpi) * a.row_stride,
+                     make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410),
+                                __byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632)));
     }
   }
 }
@@ -238,6 +290,10 @@ struct Q4CompactArgs {
 };
 static_assert(sizeof(Q4CompactArgs) <= 32000, "kernel parameter space");
 
+// A lane takes 16 bytes of a row's codes; its first lanes also the scales, in words as wide as a row of them allows (T).
+constexpr int kQ4CompactUnroll = 4;
+
+template <typename T>
 __global__ void __launch_bounds__(kQ4Threads) q4_compact_kernel(const __grid_constant__ Q4CompactArgs a) {
   pdl_wait();
   pdl_launch_dependents();
@@ -256,31 +312,47 @@ __global__ void __launch_bounds__(kQ4Threads) q4_compact_kernel(const __grid_con
     }
   }
   if (n == 0) return;
-  const int row_bytes = a.d >> 1, groups = a.d >> 5;
+  const int row_bytes = a.d >> 1, words = (a.d >> 5) * 2 / (int)sizeof(T);  // words: of a row's scales
   const int lpr = row_bytes >> 4, rpi = 32 / lpr;
   const int lane = threadIdx.x & 31, sub = lane / lpr, col = lane - sub * lpr;
-  const int per_chunk = rpi * kQ4Unroll, chunks = (n + per_chunk - 1) / per_chunk;
-  const int total = a.sets * chunks;
-  const int warps = gridDim.x * (kQ4Threads / 32);
-  for (int c = blockIdx.x * (kQ4Threads / 32) + (threadIdx.x >> 5); c < total; c += warps) {
-    const int set = c / chunks, r0 = (c - set * chunks) * per_chunk;
+  const int per_chunk = rpi * kQ4CompactUnroll;
+  for (Q4Chunks c(n, per_chunk, a.sets); c.any(); c.next()) {
     int h;
-    const int lt = fdivmod(set, a.by_heads, h);
+    const int lt = fdivmod(c.set, a.by_heads, h);
     const uint8_t* src = a.src[lt] + (int64_t)h * a.in_code_stride + col * 16;
-    const __half* ss = a.src_scale[lt] + (int64_t)h * a.in_scale_stride;
+    const T* ss = reinterpret_cast<const T*>(a.src_scale[lt] + (int64_t)h * a.in_scale_stride) + col;
     uint8_t* dst = a.dst[lt] + (int64_t)h * a.out_code_stride + col * 16;
-    __half* ds = a.dst_scale[lt] + (int64_t)h * a.out_scale_stride;
+    T* ds = reinterpret_cast<T*>(a.dst_scale[lt] + (int64_t)h * a.out_scale_stride) + col;
+    const int r0 = c.pos * per_chunk + sub;
+    int t[kQ4CompactUnroll];
+    uint4 v[kQ4CompactUnroll];
+    T sc[kQ4CompactUnroll];
 #pragma unroll
-    for (int u = 0; u < kQ4Unroll; ++u) {
-      const int r = r0 + u * rpi + sub;
-      if (sub >= rpi || r >= n) continue;
-      const int t = a.kept_idx[r];
-      if (t < 0 || t >= a.T) {
-        record_status(a.status, STEPKV_EDATA);
-        continue;
+    for (int u = 0; u < kQ4CompactUnroll; ++u) {
+      const int r = r0 + u * rpi;
+      t[u] = -1;
+      if (sub < rpi && r < n) {
+        t[u] = __ldg(a.kept_idx + r);
+        if (t[u] < 0 || t[u] >= a.T) {
+          record_status(a.status, STEPKV_EDATA);
+          t[u] = -1;
+        }
       }
-      q4_st_stream(dst + (int64_t)r * row_bytes, q4_ld_stream(src + (int64_t)t * row_bytes));
-      for (int g = col; g < groups; g += lpr) ds[(int64_t)r * groups + g] = ss[(int64_t)t * groups + g];
+    }
+#pragma unroll
+    for (int u = 0; u < kQ4CompactUnroll; ++u) {
+      sc[u] = T();
+      if (t[u] >= 0) {
+        v[u] = q4_ld_stream(src + (int64_t)t[u] * row_bytes);
+        if (col < words) sc[u] = __ldg(ss + (int64_t)t[u] * words);
+      }
+    }
+#pragma unroll
+    for (int u = 0; u < kQ4CompactUnroll; ++u) {
+      if (t[u] < 0) continue;
+      const int64_t r = r0 + u * rpi;
+      q4_st_stream(dst + r * row_bytes, v[u]);
+      if (col < words) ds[r * words] = sc[u];
     }
   }
 }
@@ -333,7 +405,7 @@ static stepkv_status_t q4_rows_run(bool write, const stepkv_q4_cache_t& c, const
     a.rows = c.rows;
     a.r = rows;
     a.status = status;
-    const int grid = q4_grid(n_sm, a.sets, rows.n, 32 / (c.d >> 3) * kQ4Unroll);
+    const int grid = q4_grid(n_sm, a.sets, rows.n, write ? 32 / (c.d >> 4) * kQ4WriteUnroll : 32 / (c.d >> 3) * kQ4ReadUnroll);
     e = launch_kernel(write ? q4_write_kernel : q4_read_kernel, dim3(grid), dim3(kQ4Threads), 0, stream, a, true);
   }
   return q4_done(e);
@@ -385,8 +457,11 @@ stepkv_status_t q4_compact_run(const stepkv_q4_cache_t& in, int T, const int32_t
     a.step_id_out = step_id_out;
     a.pos_out = pos_out;
     a.status = status;
-    const int grid = q4_grid(n_sm, a.sets, kept_cap, 32 / (in.d >> 5) * kQ4Unroll);
-    e = launch_kernel(q4_compact_kernel, dim3(grid), dim3(kQ4Threads), 0, stream, a, true);
+    const int grid = q4_grid(n_sm, a.sets, kept_cap, 32 / (in.d >> 5) * kQ4CompactUnroll);
+    const int groups = in.d >> 5;
+    auto kern = groups % 4 == 0 ? q4_compact_kernel<unsigned long long>
+                                : groups % 2 == 0 ? q4_compact_kernel<unsigned int> : q4_compact_kernel<unsigned short>;
+    e = launch_kernel(kern, dim3(grid), dim3(kQ4Threads), 0, stream, a, true);
   }
   return q4_done(e);
 }
