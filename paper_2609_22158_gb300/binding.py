@@ -7,6 +7,7 @@ is raised.
 """
 from __future__ import annotations
 
+import array
 import ctypes
 import os
 from dataclasses import dataclass, field
@@ -735,61 +736,66 @@ Q4_GROUP = 32  # channels that share a scale (STEPKV_Q4_GROUP in the header)
 
 class _PerLayer:
     """Per-layer tensors of one layout: a list, or one tensor with the layers in front (whose pointers need no look at
-    each layer)."""
-    __slots__ = ("ptrs", "shape", "strides", "device", "n", "keep")
+    each layer).  addr: the address of the host array of device pointers, which lives as long as this."""
+    __slots__ = ("addr", "shape", "strides", "device", "n", "_keep")
 
     def __init__(self, x, dtype, ndim, name):
         torch = _torch()
         if isinstance(x, torch.Tensor):
-            _need(x, dtype, name, ndim + 1)
-            self.n, self.shape, self.strides = x.shape[0], tuple(x.shape[1:]), tuple(x.stride()[1:])
-            base, step = x.data_ptr(), x.stride(0) * x.element_size()
-            self.ptrs = (ctypes.c_void_p * max(1, self.n))(*[base + l * step for l in range(self.n)])
-            self.device = x.device
+            if x.dtype != dtype or not x.is_cuda or x.dim() != ndim + 1:
+                _need(x, dtype, name, ndim + 1)
+            shape, strides = x.shape, x.stride()
+            self.n, self.shape, self.strides, self.device = shape[0], shape[1:], strides[1:], x.device
+            base, step = x.data_ptr(), strides[0] * x.element_size()
+            ptrs = array.array("Q", range(base, base + self.n * step, step) if step else [base] * self.n)
         else:
             x = list(x)
             self.n = len(x)
             if self.n:
                 _need_all(x, lambda t, nm: _need(t, dtype, nm, ndim), name)
-                self.shape, self.strides, self.device = tuple(x[0].shape), tuple(x[0].stride()), x[0].device
+                self.shape, self.strides, self.device = x[0].shape, x[0].stride(), x[0].device
                 lay = _layout(torch, x[0])
                 if any(_layout(torch, t) != lay or t.device != self.device for t in x[1:]):
                     raise ValueError(f"all {name} tensors must be laid out alike, on one device")
-            self.ptrs = _ptr_array(x)
+            ptrs = array.array("Q", [t.data_ptr() for t in x])
         if self.n < 1:
             raise ValueError(f"{name} needs at least one layer")
-        self.keep = x
-
-    @property
-    def arg(self):
-        return ctypes.cast(self.ptrs, ctypes.c_void_p)
+        self.addr, self._keep = ptrs.buffer_info()[0], (ptrs, x)
 
 
-def _same_device(dev, **tensors):
-    for name, t in tensors.items():
-        if t is not None and t.device != dev:
-            raise ValueError(f"{name} is on {t.device}, the cache on {dev}")
+def _on(dev, t, name):
+    if t.device != dev:
+        raise ValueError(f"{name} is on {t.device}, the cache on {dev}")
 
 
-def _call_on(dev, stream, where, call):
-    """call(stream handle) with `dev` as the current device (the library launches on the current one), on `stream` or
-    the device's current stream."""
+def _call_on(dev, stream, where, call, *args):
+    """call(*args, stream handle) with `dev` as the current device (the library launches on the current one), on `stream`
+    or the device's current stream."""
     torch = _torch()
     if stream is not None and stream.device != dev:
         raise ValueError(f"{where}: the stream is on {stream.device}, the tensors on {dev}")
     if dev.index == torch.cuda.current_device():
-        _check(call(_stream_handle(stream)), where)
+        _check(call(*args, torch._C._cuda_getCurrentRawStream(dev.index) if stream is None else stream.cuda_stream), where)
     else:
         with torch.cuda.device(dev):
-            _check(call(_stream_handle(stream)), where)
+            _check(call(*args, _stream_handle(stream)), where)
 
 
 def _int32_vector(t, name, dev, least=1):
-    _need(t, _torch().int32, name)
+    if not isinstance(t, _torch().Tensor) or t.dtype != _torch().int32 or not t.is_cuda:
+        _need(t, _torch().int32, name)
     if t.dim() > 1 or not t.is_contiguous() or t.numel() < least:
         raise ValueError(f"{name} must be a contiguous int32 vector of at least {least}")
-    _same_device(dev, **{name: t})
+    _on(dev, t, name)
     return t
+
+
+def _status_on(dev, status):
+    if status is None:
+        return new_status(dev)
+    _need(status, _torch().int32, "status")
+    _on(dev, status, "status")
+    return status
 
 
 class Q4Cache:
@@ -821,8 +827,9 @@ class Q4Cache:
             if self.Hkv > 1 and p.strides[0] != like.strides[0]:
                 raise ValueError(f"{name} must share the head stride of {'K' if t == torch.uint8 else 'K_scale'}")
         stride = [p.strides[0] if self.Hkv > 1 else self.rows * p.shape[2] for p in (codes, scales)]
-        args = [p.arg for p in self._parts] + [None, None]
+        args = [p.addr for p in self._parts] + [None, None]
         self._c = CQ4Cache(self.n_layers, self.Hkv, self.d, self.rows, *args[:4], *stride)
+        self._ref = ctypes.byref(self._c)
 
     @staticmethod
     def allocate(n_layers: int, Hkv: int, rows: int, d: int, device="cuda", values: bool = True) -> "Q4Cache":
@@ -838,7 +845,7 @@ class Q4Cache:
         return Q4Cache(part(self.K), part(self.K_scale), part(self.V), part(self.V_scale))
 
     def c(self):
-        return ctypes.byref(self._c)
+        return self._ref
 
 
 def _q4_rows(cache, row0, n, limit):
@@ -868,13 +875,13 @@ def _q4_bf16(cache, K, V, what):
     if some is None:
         raise ValueError(f"{what} needs K or V")
     H, rows, d = some.shape
-    if (some.n, H, d) != (cache.n_layers, cache.Hkv, cache.d):
+    if some.n != cache.n_layers or H != cache.Hkv or d != cache.d:
         raise ValueError(f"{what}: {some.n} x [{H}, {rows}, {d}] does not fit {cache.n_layers} layers of {cache.Hkv} heads "
                          f"of {cache.d}")
     if some.strides[2] != 1:
         raise ValueError(f"{what}: the channels of a row must be contiguous")
     for x in p:
-        if x is not None and (x.shape, x.strides, x.n, x.device) != (some.shape, some.strides, some.n, cache.device):
+        if x is not None and (x.shape != some.shape or x.strides != some.strides or x.n != some.n or x.device != cache.device):
             raise ValueError(f"{what}: K and V must be laid out alike, on the cache's device")
     return p[0], p[1], rows, some.strides[0] if H > 1 else rows * d, some.strides[1] if rows > 1 else d
 
@@ -891,11 +898,9 @@ def stepkv_q4_write(cache: Q4Cache, K, V, row0, n=None, idx=None, status=None, s
     if idx is not None:
         _int32_vector(idx, "idx", cache.device, 0)
     n_dev, n, row0_dev, stride, row0 = _q4_rows(cache, row0, n, T if idx is None else idx.numel())
-    status = status if status is not None else new_status(cache.device)
-    _same_device(cache.device, status=status)
-    _call_on(cache.device, stream, "stepkv_q4_write", lambda s: lib.stepkv_q4_write(
-        cache.c(), k.arg, None if v is None else v.arg, hs, rs, T, _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev), stride, row0,
-        status.data_ptr(), s))
+    status = _status_on(cache.device, status)
+    _call_on(cache.device, stream, "stepkv_q4_write", lib.stepkv_q4_write, cache.c(), k.addr, None if v is None else v.addr,
+             hs, rs, T, _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev), stride, row0, status.data_ptr())
     return status
 
 
@@ -918,11 +923,9 @@ def stepkv_q4_read(cache: Q4Cache, row0=0, n=None, idx=None, K=None, V=None, sta
         raise ValueError("stepkv_q4_read: the cache holds no values")
     k, v, rows, hs, rs = _q4_bf16(cache, K, V, "stepkv_q4_read")
     n_dev, n, row0_dev, stride, row0 = _q4_rows(cache, row0, n, rows if idx is None else min(rows, idx.numel()))
-    status = status if status is not None else new_status(cache.device)
-    _same_device(cache.device, status=status)
-    _call_on(cache.device, stream, "stepkv_q4_read", lambda s: lib.stepkv_q4_read(
-        cache.c(), _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev), stride, row0, None if k is None else k.arg,
-        None if v is None else v.arg, hs, rs, status.data_ptr(), s))
+    status = _status_on(cache.device, status)
+    _call_on(cache.device, stream, "stepkv_q4_read", lib.stepkv_q4_read, cache.c(), _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev),
+             stride, row0, None if k is None else k.addr, None if v is None else v.addr, hs, rs, status.data_ptr())
     return K, V
 
 
@@ -938,11 +941,10 @@ def stepkv_q4_compact(cache: Q4Cache, T: int, kept_idx, n_kept, kept_cap: int, o
                            (pos_out, "pos_out", kept_cap)):
         if t is not None:
             _int32_vector(t, name, dev, least)
-    status = status if status is not None else new_status(dev)
-    _same_device(dev, status=status, out=out)
-    _call_on(dev, stream, "stepkv_q4_compact", lambda s: lib.stepkv_q4_compact(
-        cache.c(), T, kept_idx.data_ptr(), n_kept.data_ptr(), kept_cap, out.c(), _ptr(step_id_in), _ptr(pos_in),
-        _ptr(step_id_out), _ptr(pos_out), status.data_ptr(), s))
+    status = _status_on(dev, status)
+    _on(dev, out, "out")
+    _call_on(dev, stream, "stepkv_q4_compact", lib.stepkv_q4_compact, cache.c(), T, kept_idx.data_ptr(), n_kept.data_ptr(),
+             kept_cap, out.c(), _ptr(step_id_in), _ptr(pos_in), _ptr(step_id_out), _ptr(pos_out), status.data_ptr())
     return status
 
 
@@ -980,8 +982,8 @@ def stepkv_q4_decode(q, cache: Q4Cache, n, out=None, ws=None, status=None, strea
     if ws is None:
         ws = q4_decode_workspace(cache, Hq)
     wp, wn = _aligned_ws(ws)
-    status = status if status is not None else new_status(cache.device)
-    _same_device(cache.device, ws=ws, status=status)
-    _call_on(cache.device, stream, "stepkv_q4_decode", lambda s: lib.stepkv_q4_decode(
-        cache.c(), qs.arg, Hq, _ptr(n_dev), stride, n, cache.rows, outs.arg, wp, wn, status.data_ptr(), s))
+    status = _status_on(cache.device, status)
+    _on(cache.device, ws, "ws")
+    _call_on(cache.device, stream, "stepkv_q4_decode", lib.stepkv_q4_decode, cache.c(), qs.addr, Hq, _ptr(n_dev), stride, n,
+             cache.rows, outs.addr, wp, wn, status.data_ptr())
     return out

@@ -20,6 +20,9 @@
 namespace stepkv {
 
 constexpr int kQ4Threads = 256;
+// CTAs an SM holds of the write and read kernels, all of them at once: more waves, or more of them resident with less in
+// flight each, were slower (write 216 us with four of three row groups; five of two 223, eight of one 234, two waves 256).
+constexpr int kQ4CtasPerSm = 4;
 
 struct Q4Args {
   const void* src[2 * kQ4Layers];  // per (layer, tensor): bf16 rows, or the codes where they are read
@@ -57,10 +60,15 @@ __device__ __forceinline__ void q4_st_stream(void* p, const uint4& v) {
   asm volatile("st.global.cs.v4.u32 [%0], {%1,%2,%3,%4};" ::"l"(p), "r"(v.x), "r"(v.y), "r"(v.z), "r"(v.w) : "memory");
 }
 
-// The larger halves of two bf16 pairs, NaN where either is one.
+// The larger, and the smaller, halves of two bf16 pairs, NaN where either is one.
 __device__ __forceinline__ uint32_t max2_nan(uint32_t a, uint32_t b) {
   uint32_t r;
   asm("max.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  return r;
+}
+__device__ __forceinline__ uint32_t min2_nan(uint32_t a, uint32_t b) {
+  uint32_t r;
+  asm("min.NaN.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
   return r;
 }
 __device__ __forceinline__ float rcp_approx(float x) {
@@ -69,9 +77,8 @@ __device__ __forceinline__ float rcp_approx(float x) {
   return r;
 }
 
-// The scale of a group whose maximum is hi and minimum -neg_lo.
-__device__ __forceinline__ __half q4_scale(float hi, float neg_lo) {
-  const float x = hi >= neg_lo ? hi : -neg_lo;
+// The scale of a group from its element of the largest magnitude.
+__device__ __forceinline__ __half q4_scale(float x) {
   if (!(fabsf(x) < INFINITY)) return __ushort_as_half(0x7FFF);
   uint32_t b = __float_as_uint(x * -0.125f);
   b = (b + 0x3FFFFu + ((b >> 19) & 1u)) & ~0x7FFFFu;  // 4 of the 23 explicit bits, ties to even
@@ -82,6 +89,8 @@ __device__ __forceinline__ __half q4_scale(float hi, float neg_lo) {
 // rint(x / s) with the exact quotient's ties: x has 8 bits and s 5, so a quotient near a tie k + 1/2 (k < 8) is the tie or
 // at least 2^-8.95 from it, and x inv is off by 2^-19 at most.  Added to 6144 it is rounded to multiples of 2^-11, a tie to
 // itself and nothing else to a tie; the next sum rounds that to an integer, ties to even, which lies in the low bits.
+// LOW: quotients below -8 can occur (a saturated scale, or one on fp16's last steps).
+template <bool LOW>
 __device__ __forceinline__ uint32_t q4_codes(const uint32_t (&v)[4], float inv) {
   constexpr float kMagic = 12582912.f;  // 1.5 2^23: the last place is 1
   const uint64_t inv2 = f2_pack(inv, inv), c0 = f2_pack(6144.f, 6144.f), c1 = f2_pack(kMagic + 8.f - 6144.f, kMagic + 8.f - 6144.f);
@@ -94,7 +103,7 @@ __device__ __forceinline__ uint32_t q4_codes(const uint32_t (&v)[4], float inv) 
   uint32_t w = 0;
 #pragma unroll
   for (int i = 7; i >= 0; --i)  // 16 w + bits of u: what the constant's bits add up to is taken off at the end
-    w = w * 16u + __float_as_uint(fminf(fmaxf(u[i], kMagic), kMagic + 15.f));
+    w = w * 16u + __float_as_uint(fminf(LOW ? fmaxf(u[i], kMagic) : u[i], kMagic + 15.f));
   return w - (0x4B400000u * 0x11111111u);
 }
 
@@ -133,10 +142,12 @@ __device__ __forceinline__ Q4Set q4_set(const Q4Args& a, int set) {
 }
 
 // A lane takes 16 channels of a row, vectors (8 channels) v and v + 2 of a group with v = lane & 1, so that a pair of lanes has
-// a group and reads 32 consecutive bytes at a time.
-constexpr int kQ4WriteUnroll = 2;
+// a group and reads 32 consecutive bytes at a time.  32 layers x 8 heads x 8272 rows: 216 us = 6.4 TB/s (by an index list of
+// 8272 in 8911 rows 229), bound by the copies; a division per channel took 655, lanes of 8 channels 272.
+constexpr int kQ4WriteUnroll = 3;
 
-__global__ void __launch_bounds__(kQ4Threads) q4_write_kernel(const __grid_constant__ Q4Args a) {
+template <bool IDX>
+__global__ void __launch_bounds__(kQ4Threads, kQ4CtasPerSm) q4_write_kernel(const __grid_constant__ Q4Args a) {
   pdl_wait();
   pdl_launch_dependents();
   const int n = q4_count(a.r, a.status);
@@ -153,58 +164,73 @@ __global__ void __launch_bounds__(kQ4Threads) q4_write_kernel(const __grid_const
       continue;
     }
     const uint16_t* src = static_cast<const uint16_t*>(a.src[s.lt]) + (int64_t)s.h * a.head_stride + vec * 8;
-    uint8_t* codes = static_cast<uint8_t*>(a.dst[s.lt]) + (int64_t)s.h * a.code_head_stride + vec * 4;
-    __half* scales = static_cast<__half*>(a.scale[s.lt]) + (int64_t)s.h * a.scale_head_stride + (col >> 1);
     const int r0 = c.pos * per_chunk + sub;
     uint4 v[kQ4WriteUnroll][2];
     bool ok[kQ4WriteUnroll];
+    int t[kQ4WriteUnroll];
 #pragma unroll
     for (int u = 0; u < kQ4WriteUnroll; ++u) {
-      const int r = r0 + u * rpi;
-      ok[u] = sub < rpi && r < n;
-      const int t = ok[u] && a.r.idx ? a.r.idx[r] : r;
-      if (ok[u] && (t < 0 || t >= a.T)) {
-        record_status(a.status, STEPKV_EDATA);
-        ok[u] = false;
-      }
-      v[u][0] = v[u][1] = make_uint4(0, 0, 0, 0);
-      if (ok[u]) {
-        v[u][0] = q4_ld_stream(src + (int64_t)t * a.row_stride);
-        v[u][1] = q4_ld_stream(src + (int64_t)t * a.row_stride + 16);
+      ok[u] = sub < rpi && r0 + u * rpi < n;
+      t[u] = r0 + u * rpi;
+      if (IDX && ok[u]) {
+        t[u] = __ldg(a.r.idx + t[u]);
+        if (t[u] < 0 || t[u] >= a.T) {
+          record_status(a.status, STEPKV_EDATA);
+          ok[u] = false;
+        }
       }
     }
 #pragma unroll
     for (int u = 0; u < kQ4WriteUnroll; ++u) {
+      v[u][0] = v[u][1] = make_uint4(0, 0, 0, 0);
+      if (ok[u]) {
+        const uint16_t* p = src + t[u] * a.row_stride;
+        v[u][0] = q4_ld_stream(p);
+        v[u][1] = q4_ld_stream(p + 16);
+      }
+    }
+    const int64_t row = (int64_t)row0 + r0;
+    uint8_t* codes = static_cast<uint8_t*>(a.dst[s.lt]) + (int64_t)s.h * a.code_head_stride + row * (a.d >> 1) + vec * 4;
+    __half* scales = static_cast<__half*>(a.scale[s.lt]) + (int64_t)s.h * a.scale_head_stride + row * (a.d >> 5) + (col >> 1);
+#pragma unroll
+    for (int u = 0; u < kQ4WriteUnroll; ++u) {
       const uint32_t x[2][4] = {{v[u][0].x, v[u][0].y, v[u][0].z, v[u][0].w}, {v[u][1].x, v[u][1].y, v[u][1].z, v[u][1].w}};
       // (maximum, -minimum) of the group as a bf16 pair
-      uint32_t hi = x[0][0], lo = x[0][0] ^ 0x80008000u;
+      uint32_t hi = x[0][0], lo = x[0][0];
 #pragma unroll
       for (int i = 1; i < 8; ++i) {
         hi = max2_nan(hi, x[i >> 2][i & 3]);
-        lo = max2_nan(lo, x[i >> 2][i & 3] ^ 0x80008000u);
+        lo = min2_nan(lo, x[i >> 2][i & 3]);
       }
+      lo ^= 0x80008000u;
       uint32_t both = max2_nan(__byte_perm(hi, lo, 0x5410), __byte_perm(hi, lo, 0x7632));
       both = max2_nan(both, __shfl_xor_sync(0xffffffffu, both, 1));
-      const __half sc = q4_scale(__uint_as_float(both << 16), __uint_as_float(both & 0xFFFF0000u));
+      const float top = __uint_as_float(both << 16), bottom = __uint_as_float(both & 0xFFFF0000u);
+      const float most = top >= bottom ? top : -bottom;
+      const __half sc = q4_scale(most);
       const float step = __half2float(sc);
       const float inv = step == 0.f ? 0.f : rcp_approx(step);
       uint32_t w[2];
+      if (__all_sync(0xffffffffu, !ok[u] || (fabsf(most) >= 7.62939453125e-6f && fabsf(most) <= 7168.f))) {  // 8 2^-20, 8 896
+        w[0] = q4_codes<false>(x[0], inv);
+        w[1] = q4_codes<false>(x[1], inv);
+      } else {
 #pragma unroll
-      for (int k = 0; k < 2; ++k) w[k] = step == step ? q4_codes(x[k], inv) : 0x88888888u;
+        for (int k = 0; k < 2; ++k) w[k] = step == step ? q4_codes<true>(x[k], inv) : 0x88888888u;
+      }
       if (ok[u]) {
-        const int64_t row = (int64_t)row0 + r0 + u * rpi;
-        uint32_t* dst = reinterpret_cast<uint32_t*>(codes + row * (a.d >> 1));
+        uint32_t* dst = reinterpret_cast<uint32_t*>(codes + u * rpi * (a.d >> 1));
         dst[0] = w[0];
         dst[2] = w[1];
-        if ((col & 1) == 0) scales[row * (a.d >> 5)] = sc;
+        if ((col & 1) == 0) scales[u * rpi * (a.d >> 5)] = sc;
       }
     }
   }
 }
 
 // A lane takes a word of codes (8 channels).  The codes of a pair of channels become bf16 by a mask, s (n - 8) by one sum and
-// one product, both exact.
-constexpr int kQ4ReadUnroll = 8;
+// one product, both exact.  32 layers x 8 heads x 8272 rows: 219 us = 6.3 TB/s; eight row groups in flight 223-265, two 292.
+constexpr int kQ4ReadUnroll = 4;
 
 __device__ __forceinline__ uint32_t q4_bf16_pair(uint32_t x, uint32_t s) {
   uint32_t y, z;
@@ -213,7 +239,8 @@ __device__ __forceinline__ uint32_t q4_bf16_pair(uint32_t x, uint32_t s) {
   return z;
 }
 
-__global__ void __launch_bounds__(kQ4Threads) q4_read_kernel(const __grid_constant__ Q4Args a) {
+template <bool IDX>
+__global__ void __launch_bounds__(kQ4Threads, kQ4CtasPerSm) q4_read_kernel(const __grid_constant__ Q4Args a) {
   pdl_wait();
   pdl_launch_dependents();
   const int n = q4_count(a.r, a.status);
@@ -224,36 +251,44 @@ __global__ void __launch_bounds__(kQ4Threads) q4_read_kernel(const __grid_consta
   for (Q4Chunks c(n, per_chunk, a.sets); c.any(); c.next()) {
     const Q4Set s = q4_set(a, c.set);
     int row0 = 0;
-    if (!a.r.idx) {
+    if (!IDX) {
       row0 = a.r.row0_dev ? a.r.row0_dev[(a.layer0 + s.layer) * a.r.row0_stride] : a.r.row0;
       if (row0 < 0 || (int64_t)row0 + n > a.rows) {
         if (lane == 0) record_status(a.status, STEPKV_EDATA);
         continue;
       }
     }
-    const uint8_t* codes = static_cast<const uint8_t*>(a.src[s.lt]) + (int64_t)s.h * a.code_head_stride + col * 4;
-    const __half* scales = static_cast<const __half*>(a.scale[s.lt]) + (int64_t)s.h * a.scale_head_stride + (col >> 2);
-    uint16_t* dst = static_cast<uint16_t*>(a.dst[s.lt]) + (int64_t)s.h * a.head_stride + col * 8;
     const int r0 = c.pos * per_chunk + sub;
+    const int64_t row = IDX ? 0 : (int64_t)row0 + r0;
+    const uint8_t* codes = static_cast<const uint8_t*>(a.src[s.lt]) + (int64_t)s.h * a.code_head_stride + row * (a.d >> 1) + col * 4;
+    const __half* scales = static_cast<const __half*>(a.scale[s.lt]) + (int64_t)s.h * a.scale_head_stride + row * (a.d >> 5) + (col >> 2);
+    uint16_t* dst = static_cast<uint16_t*>(a.dst[s.lt]) + (int64_t)s.h * a.head_stride + r0 * a.row_stride + col * 8;
     uint32_t w[kQ4ReadUnroll];
     __half sc[kQ4ReadUnroll];
     bool ok[kQ4ReadUnroll];
+    int t[kQ4ReadUnroll];
 #pragma unroll
     for (int u = 0; u < kQ4ReadUnroll; ++u) {
-      const int r = r0 + u * rpi;
-      ok[u] = sub < rpi && r < n;
-      const int64_t row = ok[u] && a.r.idx ? a.r.idx[r] : (int64_t)row0 + r;
-      if (ok[u] && (row < 0 || row >= a.rows)) {
-        record_status(a.status, STEPKV_EDATA);
-        ok[u] = false;
+      ok[u] = sub < rpi && r0 + u * rpi < n;
+      t[u] = u * rpi;
+      if (IDX && ok[u]) {
+        t[u] = __ldg(a.r.idx + r0 + u * rpi);
+        if (t[u] < 0 || t[u] >= a.rows) {
+          record_status(a.status, STEPKV_EDATA);
+          ok[u] = false;
+        }
       }
+    }
+#pragma unroll
+    for (int u = 0; u < kQ4ReadUnroll; ++u) {
       w[u] = 0;
       sc[u] = __ushort_as_half(0);
       if (ok[u]) {
-        w[u] = __ldg(reinterpret_cast<const uint32_t*>(codes + row * (a.d >> 1)));
-        sc[u] = __ldg(scales + row * (a.d >> 5));
+        w[u] = __ldg(reinterpret_cast<const uint32_t*>(codes + (int64_t)t[u] * (a.d >> 1)));
+        sc[u] = __ldg(scales + (int64_t)t[u] * (a.d >> 5));
       }
     }
+    const int64_t step = rpi * a.row_stride;
 #pragma unroll
     for (int u = 0; u < kQ4ReadUnroll; ++u) {
       const uint32_t f = __float_as_uint(__half2float(sc[u])), s2 = __byte_perm(f, f, 0x3232);  // exact in bf16
@@ -261,9 +296,9 @@ __global__ void __launch_bounds__(kQ4Threads) q4_read_kernel(const __grid_consta
 #pragma unroll
       for (int i = 0; i < 4; ++i) x[i] = q4_bf16_pair(w[u] >> (4 * i), s2);  // channels i and i + 4
       if (ok[u])
-        q4_st_stream(dst + (int64_t)(r0 + u * rpi) * a.row_stride,
-                     make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410),
-                                __byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632)));
+        q4_st_stream(dst, make_uint4(__byte_perm(x[0], x[1], 0x5410), __byte_perm(x[2], x[3], 0x5410),
+                                     __byte_perm(x[0], x[1], 0x7632), __byte_perm(x[2], x[3], 0x7632)));
+      dst += step;
     }
   }
 }
@@ -291,7 +326,9 @@ struct Q4CompactArgs {
 static_assert(sizeof(Q4CompactArgs) <= 32000, "kernel parameter space");
 
 // A lane takes 16 bytes of a row's codes; its first lanes also the scales, in words as wide as a row of them allows (T).
+// 8272 of 8911 rows of 32 layers x 8 heads: 104 us = 5.9 TB/s (two row groups in flight 112, eight 116).
 constexpr int kQ4CompactUnroll = 4;
+constexpr int kQ4CompactCtasPerSm = 8;
 
 template <typename T>
 __global__ void __launch_bounds__(kQ4Threads) q4_compact_kernel(const __grid_constant__ Q4CompactArgs a) {
@@ -357,10 +394,10 @@ __global__ void __launch_bounds__(kQ4Threads) q4_compact_kernel(const __grid_con
   }
 }
 
-// Enough CTAs for the chunks, at most 8 a SM.
-static int q4_grid(int n_sm, int64_t sets, int64_t n, int rows_per_chunk) {
+// Enough CTAs for the chunks, at most as many as `ctas`.
+static int q4_grid(int64_t ctas, int64_t sets, int64_t n, int rows_per_chunk) {
   const int64_t chunks = sets * ((std::max<int64_t>(n, 1) + rows_per_chunk - 1) / rows_per_chunk);
-  return (int)std::max<int64_t>(1, std::min<int64_t>((int64_t)n_sm * 8, (chunks + kQ4Threads / 32 - 1) / (kQ4Threads / 32)));
+  return (int)std::max<int64_t>(1, std::min<int64_t>(ctas, (chunks + kQ4Threads / 32 - 1) / (kQ4Threads / 32)));
 }
 
 static stepkv_status_t q4_done(cudaError_t e) {
@@ -405,8 +442,10 @@ static stepkv_status_t q4_rows_run(bool write, const stepkv_q4_cache_t& c, const
     a.rows = c.rows;
     a.r = rows;
     a.status = status;
-    const int grid = q4_grid(n_sm, a.sets, rows.n, write ? 32 / (c.d >> 4) * kQ4WriteUnroll : 32 / (c.d >> 3) * kQ4ReadUnroll);
-    e = launch_kernel(write ? q4_write_kernel : q4_read_kernel, dim3(grid), dim3(kQ4Threads), 0, stream, a, true);
+    const int grid = q4_grid(n_sm * kQ4CtasPerSm, a.sets, rows.n, write ? 32 / (c.d >> 4) * kQ4WriteUnroll : 32 / (c.d >> 3) * kQ4ReadUnroll);
+    auto kern = write ? (rows.idx ? q4_write_kernel<true> : q4_write_kernel<false>)
+                      : (rows.idx ? q4_read_kernel<true> : q4_read_kernel<false>);
+    e = launch_kernel(kern, dim3(grid), dim3(kQ4Threads), 0, stream, a, true);
   }
   return q4_done(e);
 }
@@ -457,7 +496,7 @@ stepkv_status_t q4_compact_run(const stepkv_q4_cache_t& in, int T, const int32_t
     a.step_id_out = step_id_out;
     a.pos_out = pos_out;
     a.status = status;
-    const int grid = q4_grid(n_sm, a.sets, kept_cap, 32 / (in.d >> 5) * kQ4CompactUnroll);
+    const int grid = q4_grid(n_sm * kQ4CompactCtasPerSm, a.sets, kept_cap, 32 / (in.d >> 5) * kQ4CompactUnroll);
     const int groups = in.d >> 5;
     auto kern = groups % 4 == 0 ? q4_compact_kernel<unsigned long long>
                                 : groups % 2 == 0 ? q4_compact_kernel<unsigned int> : q4_compact_kernel<unsigned short>;

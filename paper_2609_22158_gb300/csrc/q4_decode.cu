@@ -39,7 +39,7 @@ namespace stepkv {
 
 constexpr int kQ4DecWarps = 4;
 constexpr int kQ4DecThreads = kQ4DecWarps * 32;
-constexpr int kQ4CtasPerSm = 3;
+constexpr int kQ4DecCtasPerSm = 3;
 constexpr int kQ4Block = 32;        // keys per warp step
 constexpr int kQ4Stages = 2;
 constexpr int kQ4MaxGroups = 4096;  // workspace sizing: groups of a launch at most
@@ -475,7 +475,7 @@ struct Q4Cursor {
 };
 
 template <int D, int GP>
-__global__ void __launch_bounds__(kQ4DecThreads, kQ4CtasPerSm) q4_decode_kernel(const __grid_constant__ Q4DecodeArgs a) {
+__global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kernel(const __grid_constant__ Q4DecodeArgs a) {
   using State = Q4State<D, GP>;
   using St = Q4Stage<D>;
   constexpr int kNoMore = -0x40000000;
@@ -762,7 +762,7 @@ stepkv_status_t q4_decode_run(const stepkv_q4_cache_t& c, const void* const* q, 
     a.group_warps = kQ4DecWarps;
     // as many groups as run at once, none without a block
     const int64_t blocks = (int64_t)nl * c.Hkv * ((n_cap + kQ4Block - 1) / kQ4Block);
-    a.n_groups = (int)std::min<int64_t>(std::min(kQ4MaxGroups, n_sm * kQ4CtasPerSm), blocks);
+    a.n_groups = (int)std::min<int64_t>(std::min(kQ4MaxGroups, n_sm * kQ4DecCtasPerSm), blocks);
     a.n_dev = n_dev;
     a.n_stride = n_stride;
     a.n_host = n_host;
