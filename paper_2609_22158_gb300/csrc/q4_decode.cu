@@ -33,16 +33,17 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "fastdiv.h"
 #include "internal.h"
 
 namespace stepkv {
 
-constexpr int kQ4DecWarps = 4;
+constexpr int kQ4DecWarps = 4;      // of a CTA: a group, unless the pairs are many and short
 constexpr int kQ4DecThreads = kQ4DecWarps * 32;
 constexpr int kQ4DecCtasPerSm = 3;
 constexpr int kQ4Block = 32;        // keys per warp step
 constexpr int kQ4Stages = 2;
-constexpr int kQ4MaxGroups = 4096;  // workspace sizing: groups of a launch at most
+constexpr int kQ4MaxGroups = 4096;  // workspace sizing: groups (single warps) of a launch at most
 constexpr float kQ4WeightLog2 = 14.f;  // the largest weight is held as 2^14 (fp16 reaches 65504)
 
 struct Q4DecodeArgs {
@@ -55,8 +56,10 @@ struct Q4DecodeArgs {
   int64_t code_head_stride, scale_head_stride;
   int n_layers, layer0;
   int Hkv, G;
-  int group_warps;  // W: warps of a group
-  int n_groups;
+  int n_groups;     // CTAs
+  // with groups of kQ4DecWarps warps, and of one: divisors groups and k = groups / pairs (1 where there are more pairs)
+  FastDiv by_groups[2], by_k[2];
+  FastDiv by_heads, by_G;
   const int32_t* n_dev;
   int n_stride;
   int n_host;
@@ -70,18 +73,20 @@ static_assert(sizeof(Q4DecodeArgs) <= 32000, "kernel parameter space");
 // The keys of a cache of this launch.
 __device__ __forceinline__ int q4_keys(const Q4DecodeArgs& a, int layer, bool tell = false) {
   if (!a.n_dev) return a.n_host;
-  const int n = a.n_dev[(a.layer0 + layer) * a.n_stride];
+  const int n = __ldcg(a.n_dev + (a.layer0 + layer) * a.n_stride);  // (the merge reads it early: not from L1)
   if (tell && n > a.n_cap) record_status(a.status, STEPKV_ENOSPACE);
   if (tell && n < 0) record_status(a.status, STEPKV_EDATA);
   return max(0, min(n, a.n_cap));
 }
 
 // Keys of every cache and the first block of each in the list of all pairs' blocks; first[n_layers]: all blocks.  By the
-// first warp of a CTA; the caller synchronises.
+// first warp of a CTA; the caller synchronises.  Not used where all caches have one count.
 struct Q4Lists {
   int n[kQ4Layers];
   int first[kQ4Layers + 1];
 };
+__device__ __forceinline__ int q4_blocks(int n) { return (n + kQ4Block - 1) / kQ4Block; }
+__device__ __forceinline__ bool q4_uniform(const Q4DecodeArgs& a) { return !a.n_dev || a.n_stride == 0 || a.n_layers == 1; }
 __device__ __forceinline__ void q4_lists(const Q4DecodeArgs& a, Q4Lists& s, bool tell) {
   const int lane = threadIdx.x & 31;
   int sum[2];
@@ -90,7 +95,7 @@ __device__ __forceinline__ void q4_lists(const Q4DecodeArgs& a, Q4Lists& s, bool
     const int l = 2 * lane + i;
     const int n = l < a.n_layers ? q4_keys(a, l, tell) : 0;
     s.n[l] = n;
-    sum[i] = (n + kQ4Block - 1) / kQ4Block * a.Hkv;
+    sum[i] = q4_blocks(n) * a.Hkv;
   }
   int total = sum[0] + sum[1];
 #pragma unroll
@@ -101,6 +106,32 @@ __device__ __forceinline__ void q4_lists(const Q4DecodeArgs& a, Q4Lists& s, bool
   s.first[2 * lane + 2] = total;
   s.first[2 * lane + 1] = total - sum[1];
   if (lane == 0) s.first[0] = 0;
+}
+
+// How the list of blocks is cut.  Ranges of `per` blocks of the list, one after another; or (k > 0: one count for all, and k
+// ranges a pair are nearly as even) ranges that each lie in one pair, which spares a second start and end to those that would
+// reach over.  Groups are single warps where there are more pairs than CTAs and the pairs are short: a warp then takes a
+// pair by itself instead of waiting for three others at its end.
+struct Q4Split {
+  int W, per, k;
+};
+__device__ __forceinline__ Q4Split q4_split(const Q4DecodeArgs& a, bool uniform, int nb, int total) {
+  Q4Split p;
+  const int pairs = a.n_layers * a.Hkv;
+  const int single = pairs > a.n_groups && total <= 16 * pairs;
+  p.W = single ? 1 : kQ4DecWarps;
+  const FastDiv groups = a.by_groups[single], ks = a.by_k[single];
+  p.per = fdiv(total + groups.d - 1, groups);
+  p.k = 0;
+  if (uniform && pairs <= groups.d) {
+    // rounded up to whole rounds: a part of one takes as long, and fewer ranges are joined faster
+    const int per = fdiv(nb + ks.d - 1, ks), whole = (per + p.W - 1) & -p.W;
+    if (per <= p.per + 2 * p.W) {
+      p.k = ks.d;
+      p.per = whole;
+    }
+  }
+  return p;
 }
 
 // Copies of N bytes, and with fewer to read (then zeros).
@@ -483,37 +514,65 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   __shared__ Q4Lists s_list;
   __shared__ float s_ml[kQ4DecWarps][2 * GP];
   __shared__ Q4Cursor s_cursor[kQ4DecWarps];  // where each warp's copies are, out of its registers
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const bool uniform = q4_uniform(a);
   pdl_wait();
   pdl_launch_dependents();
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  if (warp == 0) q4_lists(a, s_list, blockIdx.x == 0);
-  __syncthreads();
-  const int W = a.group_warps, rank = warp & (W - 1), wbase = warp - rank;
-  const int group = (blockIdx.x * kQ4DecWarps + warp) / W;
-  const int total = s_list.first[a.n_layers];
-  const int per = (total + a.n_groups - 1) / a.n_groups;
-  const int lo = min(total, group * per), hi = min(total, lo + per);
-  if (lo >= hi) return;  // whole groups
+  int n_all = 0, total;
+  if (uniform) {
+    n_all = q4_keys(a, 0, blockIdx.x == 0 && threadIdx.x == 0);
+    total = q4_blocks(n_all) * a.n_layers * a.Hkv;
+  } else {
+    if (warp == 0) q4_lists(a, s_list, blockIdx.x == 0);
+    __syncthreads();
+    total = s_list.first[a.n_layers];
+  }
+  auto keys_of = [&](int layer) { return uniform ? n_all : s_list.n[layer]; };
+  auto blocks_of = [&](int layer) { return q4_blocks(keys_of(layer)); };
+  const Q4Split sp = q4_split(a, uniform, q4_blocks(n_all), total);
+  const int W = sp.W, rank = warp & (W - 1), wbase = warp - rank;
+  const int group = W == 1 ? blockIdx.x * kQ4DecWarps + warp : blockIdx.x;
   float* s_vals = reinterpret_cast<float*>(q4_smem + kQ4DecWarps * kQ4Stages * St::kBytes);
   uint8_t* s_q = reinterpret_cast<uint8_t*>(s_vals + kQ4DecWarps * GP * D) + warp * State::NG * 512;
   const uint32_t ring = smem_u32(q4_smem + warp * kQ4Stages * St::kBytes), q_at = smem_u32(s_q) + 16 * lane;
   const int G = a.G;
 
-  // the first pair
-  int l0 = 0;
-  while (s_list.first[l0 + 1] <= lo) ++l0;
-  auto blocks_of = [&](int layer) { return (s_list.n[layer] + kQ4Block - 1) / kQ4Block; };
+  // the range and its first pair
   Q4Cursor ci;
-  {
-    const int nb = blocks_of(l0), at = lo - s_list.first[l0];
-    ci.layer = l0;
-    ci.h = at / nb;
-    ci.pair = l0 * a.Hkv + ci.h;
-    const int b0 = at - ci.h * nb;
-    ci.blk = b0;
-    ci.left = hi - lo + b0;
-    ci.end = min(nb, ci.left);
+  ci.layer = a.n_layers;
+  if (sp.k > 0) {
+    const int nb = q4_blocks(n_all);
+    ci.pair = fdiv(group, a.by_k[W == 1]);
+    ci.blk = (group - ci.pair * sp.k) * sp.per;
+    if (ci.pair < a.n_layers * a.Hkv && ci.blk < nb) {
+      ci.layer = fdivmod(ci.pair, a.by_heads, ci.h);
+      ci.end = min(nb, ci.blk + sp.per);
+      ci.left = ci.end;
+    }
+  } else {
+    const int lo = min(total, group * sp.per), hi = min(total, lo + sp.per);
+    if (lo < hi) {
+      int at, nb;
+      if (uniform) {
+        nb = q4_blocks(n_all);
+        ci.pair = (unsigned)lo / (unsigned)nb;
+        ci.layer = fdivmod(ci.pair, a.by_heads, ci.h);
+        at = lo - ci.pair * nb;
+      } else {
+        ci.layer = 0;
+        while (s_list.first[ci.layer + 1] <= lo) ++ci.layer;
+        nb = blocks_of(ci.layer);
+        at = lo - s_list.first[ci.layer];
+        ci.h = (unsigned)at / (unsigned)nb;
+        ci.pair = ci.layer * a.Hkv + ci.h;
+        at -= ci.h * nb;
+      }
+      ci.blk = at;
+      ci.left = hi - lo + at;
+      ci.end = min(nb, ci.left);
+    }
   }
+  if (ci.layer == a.n_layers) return;  // whole groups
   const Q4Cursor start = ci;
   auto next_pair = [&](Q4Cursor& c) {
     c.left -= c.end;
@@ -525,7 +584,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     if (++c.h == a.Hkv) {
       c.h = 0;
       ++c.layer;
-      while (s_list.n[c.layer] == 0) {
+      while (keys_of(c.layer) == 0) {
         ++c.layer;
         c.pair += a.Hkv;
       }
@@ -555,7 +614,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   auto enter = [&](Q4Cursor& c) {  // c: a pair's, its first block
     c.blk += rank;
     ahead = (c.end - c.blk + W - 1) / W;  // (<= 0: none)
-    rows = s_list.n[c.layer] - c.blk * kQ4Block;
+    rows = keys_of(c.layer) - c.blk * kQ4Block;
     bases(c);
   };
   {
@@ -618,7 +677,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     else named_bar_sync(1 + wbase / W, W * 32);
   };
   for (ci = start; ci.layer < a.n_layers; next_pair(ci)) {
-    const int n = s_list.n[ci.layer], first = ci.blk;
+    const int n = keys_of(ci.layer), first = ci.blk;
     st.clear();
     if (ci.blk + rank < ci.end) st.load_q(a.q[ci.layer] + (size_t)ci.h * G * D, G, a.c, s_q, lane);
     for (int blk = ci.blk + rank; blk < ci.end; blk += W) {
@@ -644,7 +703,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
         *reinterpret_cast<float4*>(a.out[ci.layer] + (size_t)(ci.h * G + g) * D + e0) =
             make_float4(v[0] / ll, v[1] / ll, v[2] / ll, v[3] / ll);
       } else {
-        float* dst = a.part + ((size_t)(group + ci.pair) * G + g) * (D + 4);
+        float* dst = a.part + ((size_t)(sp.k > 0 ? group : group + ci.pair) * G + g) * (D + 4);
         if (e0 == 0) {
           dst[0] = mm;
           dst[1] = ll;
@@ -658,64 +717,87 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
 
 // The partial states of a pair joined in key order; one (pair, head) a block.  Pairs that one range held whole are
 // written already; those without keys are set to zero.
-constexpr int kQ4MergeThreads = 128;
-
-template <int D>
-__global__ void __launch_bounds__(kQ4MergeThreads) q4_merge_kernel(const __grid_constant__ Q4DecodeArgs a) {
-  constexpr int PER = D / 32, NW = kQ4MergeThreads / 32, kInFlight = 4;
+// Which slots a pair has follows from the counts, which are final once the kernel before has passed its own wait: they are
+// read before this one's, as is the code that comes after it, run once with nothing to join (its blocks lie idle then).
+// Many slots a pair: eight warps with eight slots each in flight (57 slots of 8 pairs: 10.6 -> 10.2 us a call, 228 of 2: 9.1 ->
+// 8.3); few: four of four (the wide form holds back 32 layers by 3 us).
+template <int D, int NW>
+__global__ void __launch_bounds__(NW * 32) q4_merge_kernel(const __grid_constant__ Q4DecodeArgs a) {
+  constexpr int PER = D / 32, kInFlight = NW;
   __shared__ Q4Lists s_list;
   __shared__ float s_ml[NW][2];
   __shared__ float s_v[NW][D];
-  pdl_wait();
-  pdl_launch_dependents();
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const int pair = blockIdx.x / a.G, g = blockIdx.x - pair * a.G;
-  const int layer = pair / a.Hkv, h = pair - layer * a.Hkv;
-  if (warp == 0) q4_lists(a, s_list, false);
-  __syncthreads();
-  const int nb = (s_list.n[layer] + kQ4Block - 1) / kQ4Block;
+  int g, h;
+  const int pair = fdivmod(blockIdx.x, a.by_G, g), layer = fdivmod(pair, a.by_heads, h);
+  const bool uniform = q4_uniform(a);
+  int n, first, total;  // keys of the pair's cache, its first block in the list, all blocks
+  if (uniform) {
+    n = q4_keys(a, 0);
+    first = layer * a.Hkv * q4_blocks(n);
+    total = a.n_layers * a.Hkv * q4_blocks(n);
+  } else {
+    if (warp == 0) q4_lists(a, s_list, false);
+    __syncthreads();
+    n = s_list.n[layer];
+    first = s_list.first[layer];
+    total = s_list.first[a.n_layers];
+  }
+  const int nb = q4_blocks(n);
+  const Q4Split sp = q4_split(a, uniform, nb, total);
+  int slot = 0, count = 0;
+  if (nb > 0 && sp.k > 0) {
+    slot = pair * sp.k;
+    count = (unsigned)(nb + sp.per - 1) / (unsigned)sp.per;
+  } else if (nb > 0) {
+    const int b0 = first + h * nb, g0 = (unsigned)b0 / (unsigned)sp.per;
+    slot = g0 + pair;
+    count = (unsigned)(b0 + nb - 1) / (unsigned)sp.per - g0 + 1;
+  }
   float* out = a.out[layer] + (size_t)(h * a.G + g) * D;
-  if (nb == 0) {
-    if ((int)threadIdx.x < D) out[threadIdx.x] = 0.f;
-    return;
-  }
-  const int per = (s_list.first[a.n_layers] + a.n_groups - 1) / a.n_groups;
-  const int b0 = s_list.first[layer] + h * nb;
-  const int g0 = b0 / per, count = (b0 + nb - 1) / per - g0 + 1;
-  if (count == 1) return;
-  float mm = -INFINITY, ll = 0.f, aa[PER];
-#pragma unroll
-  for (int e = 0; e < PER; ++e) aa[e] = 0.f;
 #pragma unroll 1
-  for (int i0 = warp; i0 < count; i0 += kInFlight * NW) {
-    float2 ml[kInFlight];
-    float a2[kInFlight][PER];
+  for (int live = 0; live < 2; ++live) {
+    if (live) {
+      pdl_wait();
+      pdl_launch_dependents();
+      if (nb == 0 && (int)threadIdx.x < D) out[threadIdx.x] = 0.f;
+      if (count <= 1) return;
+    }
+    float mm = -INFINITY, ll = 0.f, aa[PER];
 #pragma unroll
-    for (int u = 0; u < kInFlight; ++u) {
-      const float* src = a.part + ((size_t)(g0 + pair + i0 + u * NW) * a.G + g) * (D + 4);
-      const bool ok = i0 + u * NW < count;
-      ml[u] = ok ? __ldcg(reinterpret_cast<const float2*>(src)) : make_float2(-INFINITY, 0.f);
+    for (int e = 0; e < PER; ++e) aa[e] = 0.f;
+#pragma unroll 1
+    for (int i0 = warp; i0 < max(count, NW); i0 += kInFlight * NW) {
+      float2 ml[kInFlight];
+      float a2[kInFlight][PER];
 #pragma unroll
-      for (int e = 0; e < PER; ++e) a2[u][e] = ok ? __ldcg(src + 4 + e * 32 + lane) : 0.f;
+      for (int u = 0; u < kInFlight; ++u) {
+        const float* src = a.part + ((size_t)(slot + i0 + u * NW) * a.G + g) * (D + 4);
+        const bool ok = live && i0 + u * NW < count;
+        ml[u] = ok ? __ldcg(reinterpret_cast<const float2*>(src)) : make_float2(-INFINITY, 0.f);
+#pragma unroll
+        for (int e = 0; e < PER; ++e) a2[u][e] = ok ? __ldcg(src + 4 + e * 32 + lane) : 0.f;
+      }
+#pragma unroll
+      for (int u = 0; u < kInFlight; ++u) q4_merge_state<PER>(mm, ll, aa, ml[u].x, ml[u].y, a2[u]);
+    }
+    if (lane == 0) {
+      s_ml[warp][0] = mm;
+      s_ml[warp][1] = ll;
     }
 #pragma unroll
-    for (int u = 0; u < kInFlight; ++u) q4_merge_state<PER>(mm, ll, aa, ml[u].x, ml[u].y, a2[u]);
-  }
-  if (lane == 0) {
-    s_ml[warp][0] = mm;
-    s_ml[warp][1] = ll;
-  }
-#pragma unroll
-  for (int e = 0; e < PER; ++e) s_v[warp][e * 32 + lane] = aa[e];
-  __syncthreads();
-  if ((int)threadIdx.x < D) {
-    float m1 = -INFINITY, l1 = 0.f, v1[1] = {0.f};
-#pragma unroll
-    for (int w = 0; w < NW; ++w) {
-      const float v2[1] = {s_v[w][threadIdx.x]};
-      q4_merge_state<1>(m1, l1, v1, s_ml[w][0], s_ml[w][1], v2);
+    for (int e = 0; e < PER; ++e) s_v[warp][e * 32 + lane] = aa[e];
+    __syncthreads();
+    if ((int)threadIdx.x < D) {
+      float m1 = -INFINITY, l1 = 0.f, v1[1] = {0.f};
+#pragma unroll 1
+      for (int w = 0; w < NW; ++w) {
+        const float v2[1] = {s_v[w][threadIdx.x]};
+        q4_merge_state<1>(m1, l1, v1, s_ml[w][0], s_ml[w][1], v2);
+      }
+      if (live) out[threadIdx.x] = v1[0] / l1;
     }
-    out[threadIdx.x] = v1[0] / l1;
+    __syncthreads();
   }
 }
 
@@ -730,10 +812,11 @@ static cudaError_t q4_decode_launch(const Q4DecodeArgs& a, cudaStream_t stream) 
   void (*kern)(Q4DecodeArgs) = q4_decode_kernel<D, GP>;
   const int smem = kQ4DecWarps * (kQ4Stages * Q4Stage<D>::kBytes + GP * D * (int)sizeof(float) + D / 32 * 512);
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), smem);
-  const int grid = (a.n_groups * a.group_warps + kQ4DecWarps - 1) / kQ4DecWarps;
-  if (e == cudaSuccess) e = launch_kernel(kern, dim3(grid), dim3(kQ4DecThreads), smem, stream, a, true);
+  const int pairs = a.n_layers * a.Hkv;
+  if (e == cudaSuccess) e = launch_kernel(kern, dim3(a.n_groups), dim3(kQ4DecThreads), smem, stream, a, true);
+  const int wide = a.n_groups >= 16 * pairs;
   if (e == cudaSuccess)
-    e = launch_kernel(q4_merge_kernel<D>, dim3(a.n_layers * a.Hkv * a.G), dim3(kQ4MergeThreads), 0, stream, a, true);
+    e = launch_kernel(wide ? q4_merge_kernel<D, 8> : q4_merge_kernel<D, 4>, dim3(pairs * a.G), dim3(wide ? 256 : 128), 0, stream, a, true);
   return e;
 }
 
@@ -759,10 +842,16 @@ stepkv_status_t q4_decode_run(const stepkv_q4_cache_t& c, const void* const* q, 
     a.layer0 = l0;
     a.Hkv = c.Hkv;
     a.G = Hq / c.Hkv;
-    a.group_warps = kQ4DecWarps;
     // as many groups as run at once, none without a block
     const int64_t blocks = (int64_t)nl * c.Hkv * ((n_cap + kQ4Block - 1) / kQ4Block);
-    a.n_groups = (int)std::min<int64_t>(std::min(kQ4MaxGroups, n_sm * kQ4DecCtasPerSm), blocks);
+    a.n_groups = (int)std::min<int64_t>(std::min(kQ4MaxGroups / kQ4DecWarps, n_sm * kQ4DecCtasPerSm), blocks);
+    for (int i = 0; i < 2; ++i) {
+      const int groups = a.n_groups * (i ? kQ4DecWarps : 1);
+      a.by_groups[i] = make_fastdiv(groups);
+      a.by_k[i] = make_fastdiv(std::max(1, groups / (nl * c.Hkv)));
+    }
+    a.by_heads = make_fastdiv(c.Hkv);
+    a.by_G = make_fastdiv(a.G);
     a.n_dev = n_dev;
     a.n_stride = n_stride;
     a.n_host = n_host;
