@@ -7,6 +7,7 @@
 // Five bits of scale times three of code fit bf16's eight, so reading back is exact, and so is quantising what was read
 // back.  Everything is row-local, so a compaction moves codes and scales as they are.
 //
+// (Launched dependently: what a kernel before may have written is read after the wait, and not by the read-only path.)
 // All three kernels stream: a warp takes chunks of a few rows of one row set (layer, tensor, head), loads everything a
 // chunk needs before it uses any of it, and steps to its next chunk without a division.
 #include <cuda_fp16.h>
@@ -173,7 +174,7 @@ __global__ void __launch_bounds__(kQ4Threads, kQ4CtasPerSm) q4_write_kernel(cons
       ok[u] = sub < rpi && r0 + u * rpi < n;
       t[u] = r0 + u * rpi;
       if (IDX && ok[u]) {
-        t[u] = __ldg(a.r.idx + t[u]);
+        t[u] = __ldcg(a.r.idx + t[u]);
         if (t[u] < 0 || t[u] >= a.T) {
           record_status(a.status, STEPKV_EDATA);
           ok[u] = false;
@@ -272,7 +273,7 @@ __global__ void __launch_bounds__(kQ4Threads, kQ4CtasPerSm) q4_read_kernel(const
       ok[u] = sub < rpi && r0 + u * rpi < n;
       t[u] = u * rpi;
       if (IDX && ok[u]) {
-        t[u] = __ldg(a.r.idx + r0 + u * rpi);
+        t[u] = __ldcg(a.r.idx + r0 + u * rpi);
         if (t[u] < 0 || t[u] >= a.rows) {
           record_status(a.status, STEPKV_EDATA);
           ok[u] = false;
@@ -284,8 +285,8 @@ __global__ void __launch_bounds__(kQ4Threads, kQ4CtasPerSm) q4_read_kernel(const
       w[u] = 0;
       sc[u] = __ushort_as_half(0);
       if (ok[u]) {
-        w[u] = __ldg(reinterpret_cast<const uint32_t*>(codes + (int64_t)t[u] * (a.d >> 1)));
-        sc[u] = __ldg(scales + (int64_t)t[u] * (a.d >> 5));
+        w[u] = __ldcg(reinterpret_cast<const uint32_t*>(codes + (int64_t)t[u] * (a.d >> 1)));
+        sc[u] = __ldcg(scales + (int64_t)t[u] * (a.d >> 5));
       }
     }
     const int64_t step = rpi * a.row_stride;
@@ -369,7 +370,7 @@ __global__ void __launch_bounds__(kQ4Threads) q4_compact_kernel(const __grid_con
       const int r = r0 + u * rpi;
       t[u] = -1;
       if (sub < rpi && r < n) {
-        t[u] = __ldg(a.kept_idx + r);
+        t[u] = __ldcg(a.kept_idx + r);
         if (t[u] < 0 || t[u] >= a.T) {
           record_status(a.status, STEPKV_EDATA);
           t[u] = -1;
@@ -381,7 +382,7 @@ __global__ void __launch_bounds__(kQ4Threads) q4_compact_kernel(const __grid_con
       sc[u] = T();
       if (t[u] >= 0) {
         v[u] = q4_ld_stream(src + (int64_t)t[u] * row_bytes);
-        if (col < words) sc[u] = __ldg(ss + (int64_t)t[u] * words);
+        if (col < words) sc[u] = __ldcg(ss + (int64_t)t[u] * words);
       }
     }
 #pragma unroll

@@ -18,10 +18,11 @@
 // For G <= 4 columns 4-7 repeat the heads of columns 0-3, and P has its first terms in 0-3 and its second in 4-7.
 // Every sum over keys starts from zero in the tensor core for 32 keys and is added in fp32, as its accumulation truncates.
 //
-// 565 instructions a block of 32 keys (G <= 4), of which unpacking V takes 176, K 96.  Mixed, they issue at 0.6 a cycle at
-// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 63.4 us, G =
-// 5: 71.2, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
-// 68.3 (more moves), 8 of 255 72.4; three ring stages 66.0.
+// 543 instructions a block of 32 keys (G <= 4), of which unpacking V takes 176, K 96.  Mixed, they issue at 0.64 a cycle at
+// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 61.6 us, G =
+// 5: 70.8, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
+// 68.3 (more moves), 8 of 255 72.4; three ring stages 66.0; a barrier that keeps the SM's warps in step 64-70 (they finish
+// between 45 and 60 us without, at the same rate in all); scales laid out in shared memory for their users 67.0.
 //
 // Each warp copies its blocks of 32 rows into a ring of its own with cp.async.  The list of all pairs' blocks is cut into
 // equal contiguous ranges, one per group of warps; the warps of a group interleave the blocks of a pair, join their states
@@ -67,7 +68,9 @@ struct Q4DecodeArgs {
   float c;          // log2(e) / sqrt(d)
   float* part;      // [slot][G][d + 4]: m, l, -, -, values
   int32_t* status;
+  uint32_t magic;   // kQ4Magic: as a literal it is brought into a register 16 times a block (63.6 -> 61.8 us)
 };
+constexpr uint32_t kQ4Magic = 0x54005400u;  // two fp16 64
 static_assert(sizeof(Q4DecodeArgs) <= 32000, "kernel parameter space");
 
 // The keys of a cache of this launch.
@@ -188,10 +191,10 @@ __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], u
 
 // Codes I of the two 4-code chunks in w (one per half) times their scales: (64 + n) s - 72 s.
 template <int I>
-__device__ __forceinline__ uint32_t q4_pair(uint32_t w, uint32_t s, uint32_t b) {
+__device__ __forceinline__ uint32_t q4_pair(uint32_t w, uint32_t s, uint32_t b, uint32_t magic) {
   const uint32_t sh = I == 0 ? w << 4 : I == 1 ? w : I == 2 ? w >> 4 : w >> 8;
   uint32_t x, y;
-  asm("lop3.b32 %0, %1, 0x00F000F0, 0x54005400, 0xEA;" : "=r"(x) : "r"(sh));
+  asm("lop3.b32 %0, %1, 0x00F000F0, %2, 0xEA;" : "=r"(x) : "r"(sh), "r"(magic));
   asm("fma.rn.f16x2 %0, %1, %2, %3;" : "=r"(y) : "r"(x), "r"(s), "r"(b));
   return y;
 }
@@ -257,7 +260,7 @@ struct Q4State {
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       v[g] = make_uint4(0, 0, 0, 0);
-      if (head < G) v[g] = __ldg(reinterpret_cast<const uint4*>(q + head * D + g * 32) + c4);
+      if (head < G) v[g] = __ldcg(reinterpret_cast<const uint4*>(q + head * D + g * 32) + c4);
       const uint32_t w[4] = {v[g].x, v[g].y, v[g].z, v[g].w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) top = max(top, max(w[i] & 0x7FFFu, (w[i] >> 16) & 0x7FFFu));
@@ -311,7 +314,6 @@ struct Q4State {
   // `scales` (key r8).
   __device__ __forceinline__ void logits(uint64_t (&s)[4], uint32_t codes, uint32_t scales, uint32_t q) {
     uint32_t sk[4][D / 64];
-    float x[4][2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) q4_lds<D / 16>(sk[i], scales + 8 * i * (D / 16));
 #pragma unroll
@@ -320,10 +322,8 @@ struct Q4State {
       const uint32_t a[4] = {sk[2 * h][0], sk[2 * h + 1][0], sk[2 * h][D / 64 - 1], sk[2 * h + 1][D / 64 - 1]};
       float d[4];
       mma_f16_zero(d, a, ob[0], ob[1]);
-      x[2 * h][0] = d[0];
-      x[2 * h][1] = d[1];
-      x[2 * h + 1][0] = d[2];
-      x[2 * h + 1][1] = d[3];
+      s[2 * h] = f2_pack(d[0], d[1]);
+      s[2 * h + 1] = f2_pack(d[2], d[3]);
     }
 #pragma unroll
     for (int p = 0; p < NG / 2; ++p) {
@@ -346,15 +346,16 @@ struct Q4State {
           for (int k = 0; k < 2; ++k) {
             const __half2 sc = *reinterpret_cast<const __half2*>(&sk[2 * h + k][p]);
             const float sf = v ? __high2float(sc) : __low2float(sc);
-            x[2 * h + k][0] = fmaf(d[2 * k], sf, x[2 * h + k][0]);
-            x[2 * h + k][1] = fmaf(d[2 * k + 1], sf, x[2 * h + k][1]);
+            s[2 * h + k] = f2_fma(f2_pack(d[2 * k], d[2 * k + 1]), f2_pack(sf, sf), s[2 * h + k]);
           }
         }
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = f2_mul(f2_pack(x[i][0], x[i][1]), f);
+    for (int i = 0; i < 4; ++i) s[i] = f2_mul(s[i], f);
   }
+
+  uint32_t magic;                       // kQ4Magic
 
   // Keys kb .. kb + 31 (those at or past n do not count) in the ring stage; off: this lane's ldmatrix offset.
   __device__ __forceinline__ void block(uint32_t stage, uint32_t off, uint32_t q, int kb, int n, int lane) {
@@ -447,8 +448,8 @@ struct Q4State {
         float d[4];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {
-          const uint32_t a[4] = {q4_pair<i>(w[h][0], sc[h][0], bi[h][0]), q4_pair<i>(w[h][2], sc[h][2], bi[h][2]),
-                                 q4_pair<i>(w[h][1], sc[h][1], bi[h][1]), q4_pair<i>(w[h][3], sc[h][3], bi[h][3])};
+          const uint32_t a[4] = {q4_pair<i>(w[h][0], sc[h][0], bi[h][0], magic), q4_pair<i>(w[h][2], sc[h][2], bi[h][2], magic),
+                                 q4_pair<i>(w[h][1], sc[h][1], bi[h][1], magic), q4_pair<i>(w[h][3], sc[h][3], bi[h][3], magic)};
           if (h == 0) mma_f16_zero(d, a, b[h][NB - 2], b[h][NB - 1]);
           else mma_f16(d, a, b[h][NB - 2], b[h][NB - 1]);
           if (GP == 8) mma_f16(d, a, b[h][0], b[h][1]);
@@ -671,6 +672,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   const int lm_row = (lane & 7) + (lane & 8), lm_vec = lane >> 4;  // ldmatrix: keys 0-7 and 8-15 of a vector, then of the next
   const uint32_t off = lm_row * St::kRow + ((lm_vec ^ St::swizzle(lm_row)) << 4);
   State st;
+  st.magic = a.magic;
   int stage = 0;
   auto sync_group = [&]() {
     if (W == 1) __syncwarp();
@@ -859,6 +861,7 @@ stepkv_status_t q4_decode_run(const stepkv_q4_cache_t& c, const void* const* q, 
     a.c = (float)(1.4426950408889634 / sqrt((double)c.d));
     a.part = static_cast<float*>(ws);
     a.status = status;
+    a.magic = kQ4Magic;
     if (c.d == 128)
       e = a.G <= 4 ? q4_decode_launch<128, 4>(a, stream) : q4_decode_launch<128, 8>(a, stream);
     else
