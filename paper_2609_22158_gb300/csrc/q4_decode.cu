@@ -19,9 +19,9 @@
 // Every sum over keys starts from zero in the tensor core for 32 keys and is added in fp32, as its accumulation truncates.
 //
 // 543 instructions a block of 32 keys (G <= 4), of which unpacking V takes 176, K 96.  Mixed, they issue at 0.64 a cycle at
-// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 61.6 us, G =
-// 5: 70.8, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
-// 68.3 (more moves), 8 of 255 72.4; three ring stages 66.0; a barrier that keeps the SM's warps in step 64-70 (they finish
+// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 61.0 us, G =
+// 5: 68.5, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
+// 66.0 (more moves), 8 of 255 72.4; three ring stages 66.0; a barrier that keeps the SM's warps in step 64-70 (they finish
 // between 45 and 60 us without, at the same rate in all); scales laid out in shared memory for their users 67.0.
 //
 // Each warp copies its blocks of 32 rows into a ring of its own with cp.async.  The list of all pairs' blocks is cut into
@@ -42,6 +42,7 @@ namespace stepkv {
 constexpr int kQ4DecWarps = 4;      // of a CTA: a group, unless the pairs are many and short
 constexpr int kQ4DecThreads = kQ4DecWarps * 32;
 constexpr int kQ4DecCtasPerSm = 3;
+constexpr int kQ4DecMinSmem = 228 * 1024 / (kQ4DecCtasPerSm + 1);
 constexpr int kQ4Block = 32;        // keys per warp step
 constexpr int kQ4Stages = 2;
 constexpr int kQ4MaxGroups = 4096;  // workspace sizing: groups (single warps) of a launch at most
@@ -236,8 +237,7 @@ struct Q4State {
   static constexpr int NT = D / 16;     // 16-channel tiles of a value row
   static constexpr int NB = GP == 4 ? 2 : 4;
   // (Q itself lies in shared memory, a lane's B operand [group][b0, b1 of both k-steps] at q + 512 group + 16 lane.)
-  uint32_t ob[2];                       // B operand of the offsets -8 sum(q), in three terms
-  uint64_t f;                           // logit per sum, of the lane's columns
+  // (and at q + 512 NG + 16 lane its B operand of the offsets -8 sum(q), in three terms, and the logit per sum of its columns)
   float m[2];                           // largest logit so far (log2 units)
   uint64_t nm;                          // 14 - m, 0 before the first key
   uint64_t l;
@@ -299,6 +299,7 @@ struct Q4State {
       }
     }
     // k of the offsets' product: groups 0 and 1 in the lower eight, term c4 in lane c4; groups 2 and 3 in the upper
+    uint32_t ob[2];
 #pragma unroll
     for (int k = 0; k < 2; ++k) {
       __half2 o = __half2half2(__ushort_as_half(0));
@@ -307,13 +308,15 @@ struct Q4State {
         if (c4 == t && 2 * k < NG) o = __halves2half2(off[(2 * k) % NG][t], off[(2 * k) % NG + 1][t]);
       ob[k] = *reinterpret_cast<const uint32_t*>(&o);
     }
-    f = f2_pack(__shfl_sync(0xffffffffu, per_sum, 8 * c4), __shfl_sync(0xffffffffu, per_sum, 8 * c4 + 4));
+    *reinterpret_cast<uint4*>(q_smem + 512 * NG + 16 * lane) =
+        make_uint4(ob[0], ob[1], __float_as_uint(__shfl_sync(0xffffffffu, per_sum, 8 * c4)), __float_as_uint(__shfl_sync(0xffffffffu, per_sum, 8 * c4 + 4)));
   }
 
   // The logits (log2 units) of keys r8 + 8 i of the 32 whose codes this lane's ldmatrix address is `codes` in, their scales at
   // `scales` (key r8).
   __device__ __forceinline__ void logits(uint64_t (&s)[4], uint32_t codes, uint32_t scales, uint32_t q) {
-    uint32_t sk[4][D / 64];
+    uint32_t sk[4][D / 64], of[4];
+    q4_lds<16>(of, q + 512 * NG);
 #pragma unroll
     for (int i = 0; i < 4; ++i) q4_lds<D / 16>(sk[i], scales + 8 * i * (D / 16));
 #pragma unroll
@@ -321,7 +324,7 @@ struct Q4State {
       // the offsets of all groups in one product: scales (k = group, again for each term) times -8 sum(q)
       const uint32_t a[4] = {sk[2 * h][0], sk[2 * h + 1][0], sk[2 * h][D / 64 - 1], sk[2 * h + 1][D / 64 - 1]};
       float d[4];
-      mma_f16_zero(d, a, ob[0], ob[1]);
+      mma_f16_zero(d, a, of[0], of[1]);
       s[2 * h] = f2_pack(d[0], d[1]);
       s[2 * h + 1] = f2_pack(d[2], d[3]);
     }
@@ -352,7 +355,7 @@ struct Q4State {
       }
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = f2_mul(s[i], f);
+    for (int i = 0; i < 4; ++i) s[i] = f2_mul(s[i], f2_pack(__uint_as_float(of[2]), __uint_as_float(of[3])));
   }
 
   uint32_t magic;                       // kQ4Magic
@@ -514,7 +517,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   extern __shared__ __align__(128) uint8_t q4_smem[];  // per-warp rings, then per-warp states, then per-warp queries
   __shared__ Q4Lists s_list;
   __shared__ float s_ml[kQ4DecWarps][2 * GP];
-  __shared__ Q4Cursor s_cursor[kQ4DecWarps];  // where each warp's copies are, out of its registers
+  __shared__ Q4Cursor s_cursor[kQ4DecWarps], s_here[kQ4DecWarps];  // where each warp's copies and its arithmetic are, out of its registers
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool uniform = q4_uniform(a);
   pdl_wait();
@@ -534,9 +537,8 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   const int W = sp.W, rank = warp & (W - 1), wbase = warp - rank;
   const int group = W == 1 ? blockIdx.x * kQ4DecWarps + warp : blockIdx.x;
   float* s_vals = reinterpret_cast<float*>(q4_smem + kQ4DecWarps * kQ4Stages * St::kBytes);
-  uint8_t* s_q = reinterpret_cast<uint8_t*>(s_vals + kQ4DecWarps * GP * D) + warp * State::NG * 512;
+  uint8_t* s_q = reinterpret_cast<uint8_t*>(s_vals + kQ4DecWarps * GP * D) + warp * (State::NG + 1) * 512;
   const uint32_t ring = smem_u32(q4_smem + warp * kQ4Stages * St::kBytes), q_at = smem_u32(s_q) + 16 * lane;
-  const int G = a.G;
 
   // the range and its first pair
   Q4Cursor ci;
@@ -574,7 +576,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     }
   }
   if (ci.layer == a.n_layers) return;  // whole groups
-  const Q4Cursor start = ci;
+  if (lane == 0) s_here[warp] = ci;
   auto next_pair = [&](Q4Cursor& c) {
     c.left -= c.end;
     if (c.left <= 0) {
@@ -678,18 +680,27 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     if (W == 1) __syncwarp();
     else named_bar_sync(1 + wbase / W, W * 32);
   };
-  for (ci = start; ci.layer < a.n_layers; next_pair(ci)) {
-    const int n = keys_of(ci.layer), first = ci.blk;
-    st.clear();
-    if (ci.blk + rank < ci.end) st.load_q(a.q[ci.layer] + (size_t)ci.h * G * D, G, a.c, s_q, lane);
-    for (int blk = ci.blk + rank; blk < ci.end; blk += W) {
-      q4_cp_wait<kQ4Stages - 1>();
-      __syncwarp();
-      st.block(ring + stage * St::kBytes, off, q_at, blk * kQ4Block, n, lane);
-      __syncwarp();
-      issue_next(ring + stage * St::kBytes);
-      stage = stage + 1 == kQ4Stages ? 0 : stage + 1;
+  for (;;) {
+    __syncwarp();
+    {
+      const Q4Cursor c = s_here[warp];
+      const int n = keys_of(c.layer);
+      int kb = (c.blk + rank) * kQ4Block;
+      const int k_end = c.end * kQ4Block;
+      st.clear();
+      if (kb < k_end) st.load_q(a.q[c.layer] + (size_t)c.h * a.G * D, a.G, a.c, s_q, lane);
+#pragma unroll 1
+      for (; kb < k_end; kb += W * kQ4Block) {
+        q4_cp_wait<kQ4Stages - 1>();
+        __syncwarp();
+        st.block(ring + stage * St::kBytes, off, q_at, kb, n, lane);
+        __syncwarp();
+        issue_next(ring + stage * St::kBytes);
+        stage = stage + 1 == kQ4Stages ? 0 : stage + 1;
+      }
     }
+    Q4Cursor ci = s_here[warp];
+    const int first = ci.blk, G = a.G;
     st.store(s_ml[warp], s_vals + warp * GP * D, G, lane);
     sync_group();
     const bool whole = first == 0 && ci.end == blocks_of(ci.layer);
@@ -714,6 +725,9 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
       }
     }
     sync_group();
+    next_pair(ci);
+    if (ci.layer == a.n_layers) break;
+    if (lane == 0) s_here[warp] = ci;
   }
 }
 
@@ -812,7 +826,9 @@ size_t q4_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap) {
 template <int D, int GP>
 static cudaError_t q4_decode_launch(const Q4DecodeArgs& a, cudaStream_t stream) {
   void (*kern)(Q4DecodeArgs) = q4_decode_kernel<D, GP>;
-  const int smem = kQ4DecWarps * (kQ4Stages * Q4Stage<D>::kBytes + GP * D * (int)sizeof(float) + D / 32 * 512);
+  // (at least what lets no more than kQ4DecCtasPerSm on an SM: a fourth where registers allow one leaves other SMs without,
+  // d = 64: 41 -> 51 us)
+  const int smem = std::max(kQ4DecMinSmem, kQ4DecWarps * (kQ4Stages * Q4Stage<D>::kBytes + GP * D * (int)sizeof(float) + (D / 32 + 1) * 512));
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), smem);
   const int pairs = a.n_layers * a.Hkv;
   if (e == cudaSuccess) e = launch_kernel(kern, dim3(a.n_groups), dim3(kQ4DecThreads), smem, stream, a, true);
