@@ -391,7 +391,7 @@ STEPKV_API stepkv_status_t stepkv_decode_h2o(int32_t n_layers, const void* const
  *   scales  [Hkv][rows][d / 32] fp16
  * Codes: bases 16-byte aligned, code_head_stride (bytes) a multiple of 16.  Scales: bases aligned to d / 16 bytes (to the
  * largest power of two that divides it), scale_head_stride (elements) a multiple of d / 32.
- * d a multiple of 32 up to 256 (stepkv_q4_decode: 64 or 128).  Keys alone: V and V_scale NULL.
+ * d a multiple of 32 up to 256 (stepkv_q4_decode: 64 or 128).  Keys alone: V and V_scale NULL.  At most 2^30 rows.
  */
 #define STEPKV_Q4_GROUP 32
 typedef struct {
@@ -457,6 +457,8 @@ STEPKV_API stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_
  *  Rows at or past the count are not used, whatever they hold.  A key or a query with a NaN or an infinity makes the
  *  outputs of its heads NaN; a value row that reads back as NaN makes those channels NaN.
  *  Supported: d in {64, 128}; Hq a multiple of Hkv with at most 8 query heads per KV head.
+ *  Accuracy is fp32's for groups whose scale is a normal fp16 number (2^-14: a largest channel of 2^-11); the logits
+ *  and values of groups below that lose a bit for each halving.
  *  Deterministic; the last bits depend on the split, which goes by the counts, n_layers, Hkv and n_cap.
  */
 STEPKV_API size_t stepkv_q4_decode_workspace_size(int32_t n_layers, int32_t Hkv, int32_t Hq, int32_t d, int32_t n_cap);

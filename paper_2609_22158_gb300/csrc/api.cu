@@ -421,6 +421,7 @@ stepkv_status_t stepkv_decode(int32_t n_layers, const void* const* q, const void
 static stepkv_status_t check_q4_cache(const stepkv_q4_cache_t* c, int values) {
   if (!c || c->n_layers < 1 || c->Hkv < 1 || c->d < 1 || c->rows < 1) return STEPKV_EINVAL;
   if (c->d % STEPKV_Q4_GROUP || c->d > 256) return STEPKV_EUNSUPPORTED;
+  if (c->rows > kQ4MaxRows || c->Hkv > 65535) return STEPKV_EUNSUPPORTED;
   if (!c->K || !c->K_scale || (c->V == nullptr) != (c->V_scale == nullptr)) return STEPKV_EINVAL;
   if (values > 0 && !c->V) return STEPKV_EINVAL;
   const int groups = c->d / STEPKV_Q4_GROUP;
@@ -444,6 +445,7 @@ static stepkv_status_t check_q4_cache(const stepkv_q4_cache_t* c, int values) {
 static stepkv_status_t check_q4_rows(int n_layers, const void* const* K, const void* const* V, int64_t head_stride,
                                      int64_t row_stride, const Q4Rows& r) {
   if (r.n < 0 || head_stride < 0 || row_stride < 0) return STEPKV_EINVAL;
+  if (r.n > kQ4MaxRows) return STEPKV_EUNSUPPORTED;
   if (r.row0_dev && r.row0_stride != 0 && r.row0_stride != 1) return STEPKV_EINVAL;
   if (head_stride % 8 || row_stride % 8) return STEPKV_EUNSUPPORTED;
   for (int l = 0; l < (r.n > 0 ? n_layers : 0); ++l) {  // (no rows: an empty tensor has no address)

@@ -92,6 +92,7 @@ stepkv_status_t decode_run(int n_layers, const void* const* q, const void* const
 
 // ---- a cache held in 4 bits (q4.cu, q4_decode.cu)
 constexpr int kQ4Layers = 64;  // layers per launch (pointer arrays travel in the kernel parameters)
+constexpr int kQ4MaxRows = 1 << 30;  // of a head, and of one call: row and chunk numbers are 32-bit (offsets 64-bit)
 // The rows of one call: r < n (n_dev: *n_dev, n its limit), cache rows row0 + r (row0_dev: row0_dev[layer * row0_stride]).
 struct Q4Rows {
   const int32_t* idx;

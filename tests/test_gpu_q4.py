@@ -460,6 +460,77 @@ def test_decode_matches_oracle(B, L, Hkv, G, d, n, rows, ks):
             _check(a[l], q[l % some], K[l % some], V[l % some], n, f"layer {l}")
 
 
+@pytest.mark.parametrize("L,Hkv,G,d,n", [(16, 32, 1, 128, 1), (16, 32, 4, 128, 33), (20, 32, 2, 64, 150), (33, 16, 5, 128, 500),
+                                          (64, 40, 1, 64, 70), (64, 32, 8, 128, 17)])
+def test_decode_more_pairs_than_ctas(B, L, Hkv, G, d, n):
+    """512 to 2560 (cache, KV head) pairs of few rows, which single warps take, one count for all; then a count for each cache,
+    zero among them.  Rows at or past a count hold NaN scales."""
+    import torch
+    rng = np.random.default_rng(L + n)
+    rows = n + 3
+    K, V, q = _keys(rng, (Hkv, n, d)), _bits(rng, (Hkv, n, d)), _bits(rng, (Hkv * G, d), 2.0)
+    cache = B.Q4Cache.allocate(L, Hkv, rows, d)
+    _stale(cache, rng)
+    st = B.new_status()
+    Kd, Vd = (TL.bf16_dev(x).expand(L, -1, -1, -1) for x in (K, V))
+    B.stepkv_q4_write(cache, Kd, Vd, 0, status=st)
+    qd = TL.bf16_dev(q).expand(L, -1, -1).contiguous()
+    out = B.stepkv_q4_decode(qd, cache, n, status=st)
+    counts = rng.integers(0, n + 1, L)
+    counts[0], counts[L // 2], counts[-1] = n, 0, 1
+    ragged = B.stepkv_q4_decode(qd, cache, _dev(counts.astype(np.int32)), status=st)
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    _check(out[0], q, K, V, n, "one count")
+    bound = 2 * _dev(_decode_bound(q, _values(K), _values(V)))
+    for l in range(L):  # caches that hold the same: the split cuts them differently, each within its bound of the oracle's
+        assert ((out[l] - out[0]).abs() <= bound).all()
+    for l in (0, L // 2, L - 1, 1, L // 3):
+        _check(ragged[l], q, K, V, int(counts[l]), f"cache {l} of {counts[l]}")
+
+
+@pytest.mark.parametrize("magnitude", [2.0 ** -9, 1.0, 2.0 ** 9])
+def test_decode_keys_of_any_magnitude(B, magnitude):
+    """Keys as small and as large as normal scales hold, with queries that make up for it."""
+    import torch
+    rng = np.random.default_rng(9)
+    K, V, q = _bits(rng, (2, 300, 128), magnitude), _bits(rng, (2, 300, 128)), _bits(rng, (6, 128), 1 / magnitude)
+    out = B.stepkv_q4_decode([TL.bf16_dev(q)], _filled(B, [K], [V]), 300)[0]
+    torch.cuda.synchronize()
+    _check(out, q, K, V, 300, "")
+
+
+def test_offsets_past_32_bits(B):
+    """68 million rows of one head: 4.4 GB of codes.  All but the last 40 are zero keys and values, so the output is known; the
+    last rows are written, read back, moved and attended where offsets need more than 32 bits."""
+    import torch
+    rng = np.random.default_rng(41)
+    rows, n, d = 68_000_000, 40, 128
+    assert rows * d // 2 > 2 ** 32
+    cache = B.Q4Cache.allocate(1, 1, rows, d)
+    cache.K.fill_(0x88), cache.V.fill_(0x88)  # (code 8 with scale 0: the value 0)
+    K, V, q = _bits(rng, (1, n, d)), _bits(rng, (1, n, d)), _bits(rng, (4, d))
+    st = B.stepkv_q4_write(cache, TL.bf16_dev(K)[None], TL.bf16_dev(V)[None], rows - n)
+    Kb, Vb = B.stepkv_q4_read(cache, rows - n, n, status=st)
+    by_idx, _ = B.stepkv_q4_read(cache, idx=torch.arange(rows - n, rows, dtype=torch.int32, device="cuda"), status=st)
+    small = B.Q4Cache.allocate(1, 1, n, d)
+    kept = torch.arange(rows - n, rows, dtype=torch.int32, device="cuda")
+    B.stepkv_q4_compact(cache, rows, kept, torch.tensor([n], dtype=torch.int32, device="cuda"), n, small, status=st)
+    out = B.stepkv_q4_decode([TL.bf16_dev(q)], cache, rows, status=st)[0]
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    for got, X in ((Kb, K), (Vb, V), (by_idx, K)):
+        _same_bits(got[0], _back_bits(X))
+    assert torch.equal(small.K[0], cache.K[0][:, rows - n:]) and torch.equal(small.V_scale[0], cache.V_scale[0][:, rows - n:])
+    k, v = _values(K)[0], _values(V)[0]
+    w = np.exp(O.bf16_to_f64(q) @ k.T / math.sqrt(d))
+    want = w @ v / (rows - n + w.sum(1, keepdims=True))
+    # the weights of a lane are summed one after another: rows / 8 / (warps of a wave) of them at least on one GPU; half an
+    # ulp each of the running sum, and the same of the values' sums
+    terms = rows / 8 / 1824 + 100
+    assert (np.abs(out.cpu().numpy() - want) <= 2 * terms * 2.0 ** -24 * (w @ np.abs(v)) / rows + 2.0 ** -38 * np.abs(v).sum(0)).all()
+
+
 RAGGED = [  # Hkv, G, d, counts, rows
     (2, 4, 64, [8191, 0, 1, 17, 5000, 333, 0, 16, 4096, 2], 8192), (8, 4, 128, [0, 0, 0], 100), (1, 8, 128, [0, 3001], 3001),
     (8, 5, 128, [1] * 40 + [900], 900), (2, 1, 64, list(range(0, 64)), 70), (16, 2, 128, [31, 700, 32, 0, 33], 701),
@@ -689,6 +760,41 @@ def test_captured_steps_replay_with_new_counts(B):
             _check(got[t][l], q[l], K[l], V[l], n0 + t + 1, f"step {t}, layer {l}")
     for l in range(L):
         _check(other[l], q[l], K[l], V[l], 33, f"other graph, layer {l}")
+
+
+def test_captured_boundary(B):
+    """Write by an index list, compaction and reading back in one graph, replayed with other counts, indices and data."""
+    import torch
+    rng = np.random.default_rng(33)
+    L, Hkv, d, T = 2, 2, 64, 80
+    i32 = lambda n: torch.zeros(n, dtype=torch.int32, device="cuda")
+    src = torch.zeros((L, Hkv, T, d), dtype=torch.bfloat16, device="cuda")
+    cache, left = B.Q4Cache.allocate(L, Hkv, T, d), B.Q4Cache.allocate(L, Hkv, T, d)
+    idx, n, kept, n_kept, st = i32(T), i32(1), i32(T), i32(1), B.new_status()
+    back = torch.zeros((L, Hkv, T, d), dtype=torch.bfloat16, device="cuda")
+
+    def boundary():
+        B.stepkv_q4_write(cache, src, src, 0, n=n, idx=idx, status=st)
+        B.stepkv_q4_compact(cache, T, kept, n_kept, T, left, status=st)
+        B.stepkv_q4_read(left, 0, n_kept, K=back, status=st)
+
+    boundary()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        boundary()
+    for t in range(3):
+        X = _bits(rng, (L, Hkv, T, d))
+        a, b = int(rng.integers(2, T + 1)), int(rng.integers(1, T // 2))
+        i, j = rng.integers(0, T, T).astype(np.int32), np.sort(rng.integers(0, a, T)).astype(np.int32)
+        src.copy_(TL.bf16_dev(X))
+        for dst, v in ((idx, i), (n, [a]), (kept, j), (n_kept, [b])):
+            dst.copy_(torch.as_tensor(np.asarray(v, np.int32)))
+        back.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert st.item() == 0
+        _same_bits(back[:, :, :b], _back_bits(X)[:, :, i[j[:b]]])
+        assert (back[:, :, b:] == 7).all()
 
 
 def test_trajectory_on_a_4_bit_cache(B):

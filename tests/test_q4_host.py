@@ -133,7 +133,8 @@ OK, EINVAL, ENOSPACE, EUNSUPPORTED = 0, 1, 3, 4
 BAD_CACHE = [(dict(n_layers=0), EINVAL), (dict(Hkv=0), EINVAL), (dict(rows=0), EINVAL), (dict(d=48), EUNSUPPORTED),
              (dict(d=288), EUNSUPPORTED), (dict(K=None), EINVAL), (dict(K_scale=None), EINVAL), (dict(V=None), EINVAL),
              (dict(V_scale=None), EINVAL), (dict(code=6399), EINVAL), (dict(code=6408), EUNSUPPORTED),
-             (dict(scale=399), EINVAL), (dict(scale=402), EUNSUPPORTED)]
+             (dict(scale=399), EINVAL), (dict(scale=402), EUNSUPPORTED),
+             (dict(rows=2 ** 30 + 1, code=2 ** 37, scale=2 ** 33), EUNSUPPORTED), (dict(Hkv=65536), EUNSUPPORTED)]
 
 
 @pytest.mark.parametrize("over,code", BAD_CACHE)
@@ -160,7 +161,7 @@ def test_bad_layer_pointers(lib):
 @pytest.mark.parametrize("over,code", [
     (dict(src=None), EINVAL), (dict(val=None), EINVAL), (dict(T=-1), EINVAL), (dict(n=-1), EINVAL), (dict(n=101), EINVAL),
     (dict(hs=-8), EINVAL), (dict(rs=-8), EINVAL), (dict(hs=12804), EUNSUPPORTED), (dict(rs=132), EUNSUPPORTED),
-    (dict(row0=-1), ENOSPACE), (dict(row0=91), ENOSPACE), (dict(row0=2 ** 31 - 1), ENOSPACE), (dict(row0_dev=4096, rstride=2), EINVAL),
+    (dict(n=2 ** 30 + 1, T=2 ** 31 - 1, n_dev=4096), EUNSUPPORTED), (dict(row0=-1), ENOSPACE), (dict(row0=91), ENOSPACE), (dict(row0=2 ** 31 - 1), ENOSPACE), (dict(row0_dev=4096, rstride=2), EINVAL),
     (dict(V=None, V_scale=None), EINVAL), (dict(n=0), OK), (dict(n=0, V=None, V_scale=None, val=None), OK)])
 def test_write_refusals(lib, over, code):
     assert _write(lib, **over) == code
