@@ -782,20 +782,18 @@ def _call_on(dev, stream, where, call, *args):
 
 
 def _int32_vector(t, name, dev, least=1):
-    if not isinstance(t, _torch().Tensor) or t.dtype != _torch().int32 or not t.is_cuda:
-        _need(t, _torch().int32, name)
-    if t.dim() > 1 or not t.is_contiguous() or t.numel() < least:
+    torch = _torch()
+    if not isinstance(t, torch.Tensor) or t.dtype != torch.int32 or not t.is_cuda:
+        _need(t, torch.int32, name)
+    if t.dim() > 1 or t.numel() < least or not t.is_contiguous():
         raise ValueError(f"{name} must be a contiguous int32 vector of at least {least}")
-    _on(dev, t, name)
+    if t.device != dev:
+        _on(dev, t, name)
     return t
 
 
 def _status_on(dev, status):
-    if status is None:
-        return new_status(dev)
-    _need(status, _torch().int32, "status")
-    _on(dev, status, "status")
-    return status
+    return new_status(dev) if status is None else _int32_vector(status, "status", dev)
 
 
 class Q4Cache:

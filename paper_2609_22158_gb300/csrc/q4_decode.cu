@@ -19,15 +19,15 @@
 // Every sum over keys starts from zero in the tensor core for 32 keys and is added in fp32, as its accumulation truncates.
 //
 // 543 instructions a block of 32 keys (G <= 4), of which unpacking V takes 176, K 96.  Mixed, they issue at 0.64 a cycle at
-// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 61.0 us, G =
-// 5: 68.5, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
+// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 61.1 us, G =
+// 5: 67.8, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
 // 66.0 (more moves), 8 of 255 72.4; three ring stages 66.0; a barrier that keeps the SM's warps in step 64-70 (they finish
 // between 45 and 60 us without, at the same rate in all); scales laid out in shared memory for their users 67.0.
 //
 // Each warp copies its blocks of 32 rows into a ring of its own with cp.async.  The list of all pairs' blocks is cut into
-// equal contiguous ranges, one per group of warps; the warps of a group interleave the blocks of a pair, join their states
-// in shared memory, and leave a partial state per pair that the range touches (slot group + pair), which a second kernel
-// joins in key order.  A range that holds the whole pair writes the output itself.
+// ranges (q4_split), one per group of warps; the warps of a group interleave the blocks of a pair, join their states in
+// shared memory, and leave a partial state per pair that the range touches, which a second kernel joins in key order.  A
+// range that holds the whole pair writes the output itself.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -45,6 +45,7 @@ constexpr int kQ4DecCtasPerSm = 3;
 constexpr int kQ4DecMinSmem = 228 * 1024 / (kQ4DecCtasPerSm + 1);
 constexpr int kQ4Block = 32;        // keys per warp step
 constexpr int kQ4Stages = 2;
+constexpr int kQ4Alone = 2;         // blocks of a pair that a warp takes by itself
 constexpr int kQ4MaxGroups = 4096;  // workspace sizing: groups (single warps) of a launch at most
 constexpr float kQ4WeightLog2 = 14.f;  // the largest weight is held as 2^14 (fp16 reaches 65504)
 
@@ -509,21 +510,21 @@ struct Q4Cursor {
   int left;             // blocks of the range from this pair's first one on
 };
 
-template <int D, int GP>
+// RAGGED: a count for each cache.
+template <int D, int GP, bool RAGGED>
 __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kernel(const __grid_constant__ Q4DecodeArgs a) {
   using State = Q4State<D, GP>;
   using St = Q4Stage<D>;
   constexpr int kNoMore = -0x40000000;
   extern __shared__ __align__(128) uint8_t q4_smem[];  // per-warp rings, then per-warp states, then per-warp queries
-  __shared__ Q4Lists s_list;
+  __shared__ Q4Lists s_list;  // RAGGED
   __shared__ float s_ml[kQ4DecWarps][2 * GP];
   __shared__ Q4Cursor s_cursor[kQ4DecWarps], s_here[kQ4DecWarps];  // where each warp's copies and its arithmetic are, out of its registers
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const bool uniform = q4_uniform(a);
   pdl_wait();
   pdl_launch_dependents();
   int n_all = 0, total;
-  if (uniform) {
+  if constexpr (!RAGGED) {
     n_all = q4_keys(a, 0, blockIdx.x == 0 && threadIdx.x == 0);
     total = q4_blocks(n_all) * a.n_layers * a.Hkv;
   } else {
@@ -531,10 +532,10 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     __syncthreads();
     total = s_list.first[a.n_layers];
   }
-  auto keys_of = [&](int layer) { return uniform ? n_all : s_list.n[layer]; };
+  auto keys_of = [&](int layer) { return RAGGED ? s_list.n[layer] : n_all; };
   auto blocks_of = [&](int layer) { return q4_blocks(keys_of(layer)); };
-  const Q4Split sp = q4_split(a, uniform, q4_blocks(n_all), total);
-  const int W = sp.W, rank = warp & (W - 1), wbase = warp - rank;
+  const Q4Split sp = q4_split(a, !RAGGED, q4_blocks(n_all), total);
+  const int W = sp.W, rank = warp & (W - 1);
   const int group = W == 1 ? blockIdx.x * kQ4DecWarps + warp : blockIdx.x;
   float* s_vals = reinterpret_cast<float*>(q4_smem + kQ4DecWarps * kQ4Stages * St::kBytes);
   uint8_t* s_q = reinterpret_cast<uint8_t*>(s_vals + kQ4DecWarps * GP * D) + warp * (State::NG + 1) * 512;
@@ -543,7 +544,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   // the range and its first pair
   Q4Cursor ci;
   ci.layer = a.n_layers;
-  if (sp.k > 0) {
+  if (!RAGGED && sp.k > 0) {
     const int nb = q4_blocks(n_all);
     ci.pair = fdiv(group, a.by_k[W == 1]);
     ci.blk = (group - ci.pair * sp.k) * sp.per;
@@ -556,7 +557,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     const int lo = min(total, group * sp.per), hi = min(total, lo + sp.per);
     if (lo < hi) {
       int at, nb;
-      if (uniform) {
+      if constexpr (!RAGGED) {
         nb = q4_blocks(n_all);
         ci.pair = (unsigned)lo / (unsigned)nb;
         ci.layer = fdivmod(ci.pair, a.by_heads, ci.h);
@@ -610,13 +611,23 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     Ks = reinterpret_cast<const uint8_t*>(a.K_scale[c.layer]) + scale;
     Vs = reinterpret_cast<const uint8_t*>(a.V_scale[c.layer]) + scale;
   };
-  const int code_step = W * kQ4Block * St::kRow, scale_step = W * kQ4Block * St::kScaleRow;
+  // RAGGED: a pair of which the range holds a block or two is one warp's, the warps taking turns, and the others go on: the
+  // short lists run side by side (24 caches of 1 to 8191 rows 15.7 -> 11.2 us).
+  auto alone = [&](const Q4Cursor& c) { return RAGGED && c.end - c.blk <= kQ4Alone; };
+  auto mine = [&](const Q4Cursor& c) { return !alone(c) || (c.pair & (W - 1)) == rank; };
   Q4Cursor& is = s_cursor[warp];
-  // from the next block on: blocks of this warp left in the pair, rows of the pair (0: no more)
-  int ahead, rows;
+  // from the next block on: blocks of this warp left in the pair (<= 0: none), rows of the pair; from one block to the next:
+  // rows, bytes of codes and of scales
+  int ahead, rows, row_step, code_step, scale_step;
   auto enter = [&](Q4Cursor& c) {  // c: a pair's, its first block
-    c.blk += rank;
-    ahead = (c.end - c.blk + W - 1) / W;  // (<= 0: none)
+    row_step = (alone(c) ? 1 : W) * kQ4Block;
+    code_step = row_step * St::kRow;
+    scale_step = row_step * St::kScaleRow;
+    ahead = mine(c) ? c.end - c.blk : 0;
+    if (!alone(c)) {
+      c.blk += rank;
+      ahead = (c.end - c.blk + W - 1) / W;
+    }
     rows = keys_of(c.layer) - c.blk * kQ4Block;
     bases(c);
   };
@@ -662,35 +673,33 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     }
     q4_cp_commit();
     --ahead;
-    rows -= W * kQ4Block;
+    rows -= row_step;
     Kc += code_step;
     Vc += code_step;
     Ks += scale_step;
     Vs += scale_step;
   };
-#pragma unroll
-  for (int s = 0; s < kQ4Stages; ++s) issue_next(ring + s * St::kBytes);
+  issue_next(ring);
 
   const int lm_row = (lane & 7) + (lane & 8), lm_vec = lane >> 4;  // ldmatrix: keys 0-7 and 8-15 of a vector, then of the next
   const uint32_t off = lm_row * St::kRow + ((lm_vec ^ St::swizzle(lm_row)) << 4);
   State st;
   st.magic = a.magic;
   int stage = 0;
-  auto sync_group = [&]() {
-    if (W == 1) __syncwarp();
-    else named_bar_sync(1 + wbase / W, W * 32);
-  };
+  bool fresh = true;
   for (;;) {
     __syncwarp();
-    {
-      const Q4Cursor c = s_here[warp];
-      const int n = keys_of(c.layer);
-      int kb = (c.blk + rank) * kQ4Block;
-      const int k_end = c.end * kQ4Block;
+    Q4Cursor ci = s_here[warp];
+    const bool solo = alone(ci) || W == 1, my = mine(ci);
+    if (my) {
+      const int n = keys_of(ci.layer), step = (solo ? 1 : W) * kQ4Block, k_end = ci.end * kQ4Block;
+      int kb = (ci.blk + (solo ? 0 : rank)) * kQ4Block;
       st.clear();
-      if (kb < k_end) st.load_q(a.q[c.layer] + (size_t)c.h * a.G * D, a.G, a.c, s_q, lane);
+      if (kb < k_end) st.load_q(a.q[ci.layer] + (size_t)ci.h * a.G * D, a.G, a.c, s_q, lane);
+      if (fresh) issue_next(ring + St::kBytes);  // (the first blocks of all warps go ahead of the second)
+      fresh = false;
 #pragma unroll 1
-      for (; kb < k_end; kb += W * kQ4Block) {
+      for (; kb < k_end; kb += step) {
         q4_cp_wait<kQ4Stages - 1>();
         __syncwarp();
         st.block(ring + stage * St::kBytes, off, q_at, kb, n, lane);
@@ -698,33 +707,39 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
         issue_next(ring + stage * St::kBytes);
         stage = stage + 1 == kQ4Stages ? 0 : stage + 1;
       }
-    }
-    Q4Cursor ci = s_here[warp];
-    const int first = ci.blk, G = a.G;
-    st.store(s_ml[warp], s_vals + warp * GP * D, G, lane);
-    sync_group();
-    const bool whole = first == 0 && ci.end == blocks_of(ci.layer);
-    for (int t = rank * 32 + lane; t < G * (D / 4); t += W * 32) {
-      const int g = t / (D / 4), e0 = (t - g * (D / 4)) * 4;
-      float mm = -INFINITY, ll = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
-      for (int w = wbase; w < wbase + W; ++w) {
-        const float4 x = *reinterpret_cast<const float4*>(s_vals + (w * GP + g) * D + e0);
-        const float v2[4] = {x.x, x.y, x.z, x.w};
-        q4_merge_state<4>(mm, ll, v, s_ml[w][2 * g], s_ml[w][2 * g + 1], v2);
-      }
-      if (whole) {
-        *reinterpret_cast<float4*>(a.out[ci.layer] + (size_t)(ci.h * G + g) * D + e0) =
-            make_float4(v[0] / ll, v[1] / ll, v[2] / ll, v[3] / ll);
-      } else {
-        float* dst = a.part + ((size_t)(sp.k > 0 ? group : group + ci.pair) * G + g) * (D + 4);
-        if (e0 == 0) {
-          dst[0] = mm;
-          dst[1] = ll;
+      ci = s_here[warp];
+      const int first = ci.blk, G = a.G;
+      st.store(s_ml[warp], s_vals + warp * GP * D, G, lane);
+      auto sync_group = [&]() {
+        if (solo) __syncwarp();
+        else named_bar_sync(1, kQ4DecThreads);
+      };
+      sync_group();
+      const int w0 = solo ? warp : 0, w1 = solo ? warp + 1 : kQ4DecWarps;
+      const int t0 = solo ? lane : (int)threadIdx.x, t_step = solo ? 32 : kQ4DecThreads;
+      const bool whole = first == 0 && ci.end == blocks_of(ci.layer);
+      for (int t = t0; t < G * (D / 4); t += t_step) {
+        const int g = t / (D / 4), e0 = (t - g * (D / 4)) * 4;
+        float mm = -INFINITY, ll = 0.f, v[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int w = w0; w < w1; ++w) {
+          const float4 x = *reinterpret_cast<const float4*>(s_vals + (w * GP + g) * D + e0);
+          const float v2[4] = {x.x, x.y, x.z, x.w};
+          q4_merge_state<4>(mm, ll, v, s_ml[w][2 * g], s_ml[w][2 * g + 1], v2);
         }
-        *reinterpret_cast<float4*>(dst + 4 + e0) = make_float4(v[0], v[1], v[2], v[3]);
+        if (whole) {
+          *reinterpret_cast<float4*>(a.out[ci.layer] + (size_t)(ci.h * G + g) * D + e0) =
+              make_float4(v[0] / ll, v[1] / ll, v[2] / ll, v[3] / ll);
+        } else {
+          float* dst = a.part + ((size_t)(!RAGGED && sp.k > 0 ? group : group + ci.pair) * G + g) * (D + 4);
+          if (e0 == 0) {
+            dst[0] = mm;
+            dst[1] = ll;
+          }
+          *reinterpret_cast<float4*>(dst + 4 + e0) = make_float4(v[0], v[1], v[2], v[3]);
+        }
       }
+      sync_group();
     }
-    sync_group();
     next_pair(ci);
     if (ci.layer == a.n_layers) break;
     if (lane == 0) s_here[warp] = ci;
@@ -825,7 +840,8 @@ size_t q4_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap) {
 
 template <int D, int GP>
 static cudaError_t q4_decode_launch(const Q4DecodeArgs& a, cudaStream_t stream) {
-  void (*kern)(Q4DecodeArgs) = q4_decode_kernel<D, GP>;
+  void (*kern)(Q4DecodeArgs) =
+      a.n_dev && a.n_stride && a.n_layers > 1 ? q4_decode_kernel<D, GP, true> : q4_decode_kernel<D, GP, false>;
   // (at least what lets no more than kQ4DecCtasPerSm on an SM: a fourth where registers allow one leaves other SMs without,
   // d = 64: 41 -> 51 us)
   const int smem = std::max(kQ4DecMinSmem, kQ4DecWarps * (kQ4Stages * Q4Stage<D>::kBytes + GP * D * (int)sizeof(float) + (D / 32 + 1) * 512));
