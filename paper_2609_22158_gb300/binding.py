@@ -8,6 +8,7 @@ is raised.
 from __future__ import annotations
 
 import array
+import contextlib
 import ctypes
 import os
 from dataclasses import dataclass, field
@@ -792,8 +793,16 @@ def _int32_vector(t, name, dev, least=1):
     return t
 
 
-def _status_on(dev, status):
-    return new_status(dev) if status is None else _int32_vector(status, "status", dev)
+def _made_on(stream):
+    """What a call allocates or zeroes belongs to the stream it runs on."""
+    return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
+
+
+def _status_on(dev, status, stream):
+    if status is not None:
+        return _int32_vector(status, "status", dev)
+    with _made_on(stream):
+        return new_status(dev)
 
 
 class Q4Cache:
@@ -896,7 +905,7 @@ def stepkv_q4_write(cache: Q4Cache, K, V, row0, n=None, idx=None, status=None, s
     if idx is not None:
         _int32_vector(idx, "idx", cache.device, 0)
     n_dev, n, row0_dev, stride, row0 = _q4_rows(cache, row0, n, T if idx is None else idx.numel())
-    status = _status_on(cache.device, status)
+    status = _status_on(cache.device, status, stream)
     _call_on(cache.device, stream, "stepkv_q4_write", lib.stepkv_q4_write, cache.c(), k.addr, None if v is None else v.addr,
              hs, rs, T, _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev), stride, row0, status.data_ptr())
     return status
@@ -906,22 +915,24 @@ def stepkv_q4_read(cache: Q4Cache, row0=0, n=None, idx=None, K=None, V=None, sta
     """Rows row0, row0 + 1, ... (or idx[0], idx[1], ...) of the cache as bf16, exactly: returns (K, V), per layer
     [Hkv, >= n, d].  n: an int or a device int32 tensor, default as many as K and V (or idx, or the cache from an int row0
     on) hold.  Give K or V alone to read only that; neither: both are allocated as [n_layers, Hkv, n, d] (a device n: with
-    room for all, zero past n)."""
+    room for all; rows that are not read are zero)."""
     torch = _torch()
     lib = load_library()
     if idx is not None:
         _int32_vector(idx, "idx", cache.device, 0)
     if K is None and V is None:
+        known = idx is None and isinstance(row0, int) and (n is None or isinstance(n, int))
         room = idx.numel() if idx is not None else cache.rows - (row0 if isinstance(row0, int) else 0)
-        new = torch.empty if n is None or isinstance(n, int) else torch.zeros
+        new = torch.empty if known else torch.zeros
         shape = (cache.n_layers, cache.Hkv, n if isinstance(n, int) else max(room, 0), cache.d)
-        K = new(shape, dtype=torch.bfloat16, device=cache.device)
-        V = None if cache.V is None else new(shape, dtype=torch.bfloat16, device=cache.device)
+        with _made_on(stream):
+            K = new(shape, dtype=torch.bfloat16, device=cache.device)
+            V = None if cache.V is None else new(shape, dtype=torch.bfloat16, device=cache.device)
     if V is not None and cache.V is None:
         raise ValueError("stepkv_q4_read: the cache holds no values")
     k, v, rows, hs, rs = _q4_bf16(cache, K, V, "stepkv_q4_read")
     n_dev, n, row0_dev, stride, row0 = _q4_rows(cache, row0, n, rows if idx is None else min(rows, idx.numel()))
-    status = _status_on(cache.device, status)
+    status = _status_on(cache.device, status, stream)
     _call_on(cache.device, stream, "stepkv_q4_read", lib.stepkv_q4_read, cache.c(), _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev),
              stride, row0, None if k is None else k.addr, None if v is None else v.addr, hs, rs, status.data_ptr())
     return K, V
@@ -939,7 +950,7 @@ def stepkv_q4_compact(cache: Q4Cache, T: int, kept_idx, n_kept, kept_cap: int, o
                            (pos_out, "pos_out", kept_cap)):
         if t is not None:
             _int32_vector(t, name, dev, least)
-    status = _status_on(dev, status)
+    status = _status_on(dev, status, stream)
     _on(dev, out, "out")
     _call_on(dev, stream, "stepkv_q4_compact", lib.stepkv_q4_compact, cache.c(), T, kept_idx.data_ptr(), n_kept.data_ptr(),
              kept_cap, out.c(), _ptr(step_id_in), _ptr(pos_in), _ptr(step_id_out), _ptr(pos_out), status.data_ptr())
@@ -965,7 +976,8 @@ def stepkv_q4_decode(q, cache: Q4Cache, n, out=None, ws=None, status=None, strea
     if qs.n != cache.n_layers or qs.shape[1] != cache.d or cache.V is None:
         raise ValueError("stepkv_q4_decode needs one [Hq, d] query per layer of a cache with keys and values")
     if out is None:
-        out = torch.empty((cache.n_layers, Hq, cache.d), dtype=torch.float32, device=cache.device)
+        with _made_on(stream):
+            out = torch.empty((cache.n_layers, Hq, cache.d), dtype=torch.float32, device=cache.device)
         out = out if isinstance(q, torch.Tensor) else list(out)
     outs = _PerLayer(out, torch.float32, 2, "out")
     for x, name in ((qs, "q"), (outs, "out")):
@@ -978,9 +990,10 @@ def stepkv_q4_decode(q, cache: Q4Cache, n, out=None, ws=None, status=None, strea
             raise ValueError("n must hold one count, or one for each layer")
         stride = int(n_dev.numel() > 1)
     if ws is None:
-        ws = q4_decode_workspace(cache, Hq)
+        with _made_on(stream):
+            ws = q4_decode_workspace(cache, Hq)
     wp, wn = _aligned_ws(ws)
-    status = _status_on(cache.device, status)
+    status = _status_on(cache.device, status, stream)
     _on(cache.device, ws, "ws")
     _call_on(cache.device, stream, "stepkv_q4_decode", lib.stepkv_q4_decode, cache.c(), qs.addr, Hq, _ptr(n_dev), stride, n,
              cache.rows, outs.addr, wp, wn, status.data_ptr())

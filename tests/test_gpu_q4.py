@@ -762,6 +762,52 @@ def test_captured_steps_replay_with_new_counts(B):
         _check(other[l], q[l], K[l], V[l], 33, f"other graph, layer {l}")
 
 
+def test_what_a_call_makes_belongs_to_its_stream(B):
+    """Calls on a stream while the current one is busy: the status, rows and workspace that they make are neither cleared nor
+    handed out again by what the current stream does late."""
+    import torch
+    rng = np.random.default_rng(34)
+    L, Hkv, G, d, n = 1, 2, 4, 64, 600
+    K, V = ([_bits(rng, (Hkv, n, d)) for _ in range(L)] for _ in range(2))
+    cache = _filled(B, K, V)
+    src, q = TL.bf16_dev(K[0])[None], _bits(rng, (Hkv * G, d))
+    qd = TL.bf16_dev(q)[None]
+    count, row0 = (torch.tensor([x], dtype=torch.int32, device="cuda") for x in (n - 7, 1))
+    side = torch.cuda.Stream()
+    B.stepkv_q4_decode(qd, cache, n), B.stepkv_q4_read(cache, n=count), B.stepkv_q4_write(cache, src, src, 0)
+    cache = _filled(B, K, V)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(50_000_000)  # some 25 ms on the current stream
+    st = B.stepkv_q4_write(cache, src, src, row0, stream=side)  # a row too many
+    Kb, Vb = B.stepkv_q4_read(cache, n=count, stream=side)
+    out = B.stepkv_q4_decode(qd, cache, count, stream=side)
+    made = torch.zeros(1 << 20, dtype=torch.uint8, device="cuda")
+    torch.cuda.synchronize()
+    assert st.item() == B.STEPKV_ENOSPACE and not made.any()
+    for got, X in ((Kb, K), (Vb, V)):
+        _same_bits(got[0, :, :n - 7], _back_bits(X[0])[:, :n - 7])
+        assert not got[0, :, n - 7:].any()
+    _check(out[0], q, K[0], V[0], n - 7, "on its own stream")
+
+
+def test_rows_that_are_not_read_are_zero(B):
+    """Allocated rows of an index or a first row outside the cache."""
+    import torch
+    rng = np.random.default_rng(35)
+    K = [_bits(rng, (2, 40, 64))]
+    cache, st = _filled(B, K), B.new_status()
+    junk = torch.full((1, 2, 3, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    del junk
+    Kb, Vb = B.stepkv_q4_read(cache, idx=_dev(np.array([5, 40, 7], np.int32)), status=st)
+    assert st.item() == B.STEPKV_EDATA and Vb is None
+    _same_bits(Kb[0], np.where(np.array([1, 0, 1])[None, :, None] == 1, _back_bits(K[0])[:, [5, 0, 7]], np.uint16(0)))
+    st = B.new_status()
+    junk = torch.full((1, 2, 3, 64), 7.0, dtype=torch.bfloat16, device="cuda")
+    del junk
+    Kb, _ = B.stepkv_q4_read(cache, _dev(np.array([38], np.int32)), n=3, status=st)
+    assert st.item() == B.STEPKV_EDATA and Kb.shape == (1, 2, 3, 64) and not Kb.any()
+
+
 def test_captured_boundary(B):
     """Write by an index list, compaction and reading back in one graph, replayed with other counts, indices and data."""
     import torch
