@@ -24,10 +24,10 @@
 // 66.0 (more moves), 8 of 255 72.4; three ring stages 66.0; a barrier that keeps the SM's warps in step 64-70 (they finish
 // between 45 and 60 us without, at the same rate in all); scales laid out in shared memory for their users 67.0.
 //
-// Each warp copies its blocks of 32 rows into a ring of its own with cp.async.  The list of all pairs' blocks is cut into
-// ranges (q4_split), one per group of warps; the warps of a group interleave the blocks of a pair, join their states in
-// shared memory, and leave a partial state per pair that the range touches, which a second kernel joins in key order.  A
-// range that holds the whole pair writes the output itself.
+// Each warp copies its blocks of 32 rows into a ring of its own with cp.async.  A group of warps takes a pair (q4_whole) or a
+// range of the list of all pairs' blocks (q4_split); its warps interleave the blocks of a pair, join their states in shared
+// memory, and write the output where they had the whole pair, or else leave a partial state, which a second kernel joins with
+// the others in key order.
 #include <cuda_fp16.h>
 #include <math.h>
 
@@ -45,6 +45,7 @@ constexpr int kQ4DecCtasPerSm = 3;
 constexpr int kQ4DecMinSmem = 228 * 1024 / (kQ4DecCtasPerSm + 1);
 constexpr int kQ4Block = 32;        // keys per warp step
 constexpr int kQ4Stages = 2;
+constexpr int kQ4Few = 16;          // blocks of a pair that one CTA takes at once, though the pair might be cut
 constexpr int kQ4Alone = 2;         // blocks of a pair that a warp takes by itself
 constexpr int kQ4MaxGroups = 4096;  // workspace sizing: groups (single warps) of a launch at most
 constexpr float kQ4WeightLog2 = 14.f;  // the largest weight is held as 2^14 (fp16 reaches 65504)
@@ -70,6 +71,7 @@ struct Q4DecodeArgs {
   float c;          // log2(e) / sqrt(d)
   float* part;      // [slot][G][d + 4]: m, l, -, -, values
   int32_t* status;
+  int whole;        // warps that take a pair, all of it: no states to join (0: the pairs are cut, q4_split)
   uint32_t magic;   // kQ4Magic: as a literal it is brought into a register 16 times a block (63.6 -> 61.8 us)
 };
 constexpr uint32_t kQ4Magic = 0x54005400u;  // two fp16 64
@@ -113,10 +115,10 @@ __device__ __forceinline__ void q4_lists(const Q4DecodeArgs& a, Q4Lists& s, bool
   if (lane == 0) s.first[0] = 0;
 }
 
-// How the list of blocks is cut.  Ranges of `per` blocks of the list, one after another; or (k > 0: one count for all, and k
-// ranges a pair are nearly as even) ranges that each lie in one pair, which spares a second start and end to those that would
-// reach over.  Groups are single warps where there are more pairs than CTAs and the pairs are short: a warp then takes a
-// pair by itself instead of waiting for three others at its end.
+// How the list of blocks is cut, where pairs are.  Ranges of `per` blocks of the list, one after another; or (k > 0: one count
+// for all, and ranges that each lie in one pair, k in each, are nearly as even) these, which spares a second start and end to
+// those that would reach over.  Groups are single warps where there are more pairs than CTAs and the pairs are short: a warp
+// then takes a range by itself instead of waiting for three others at its end.
 struct Q4Split {
   int W, per, k;
 };
@@ -128,12 +130,15 @@ __device__ __forceinline__ Q4Split q4_split(const Q4DecodeArgs& a, bool uniform,
   const FastDiv groups = a.by_groups[single], ks = a.by_k[single];
   p.per = fdiv(total + groups.d - 1, groups);
   p.k = 0;
-  if (uniform && pairs <= groups.d) {
+  if (uniform && nb > 0 && pairs <= groups.d) {
     // rounded up to whole rounds: a part of one takes as long, and fewer ranges are joined faster
     const int per = fdiv(nb + ks.d - 1, ks), whole = (per + p.W - 1) & -p.W;
-    if (per <= p.per + 2 * p.W) {
-      p.k = ks.d;
+    if (!single && nb <= kQ4Few) {  // (14 layers x 8 heads x 379 rows 8.0 -> 7.0 us; at 24 blocks 9.6 and 9.1, or slower)
+      p.k = 1;
+      p.per = nb;
+    } else if (per <= p.per + 2 * p.W) {
       p.per = whole;
+      p.k = (unsigned)(nb + whole - 1) / (unsigned)whole;
     }
   }
   return p;
@@ -535,7 +540,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   auto keys_of = [&](int layer) { return RAGGED ? s_list.n[layer] : n_all; };
   auto blocks_of = [&](int layer) { return q4_blocks(keys_of(layer)); };
   const Q4Split sp = q4_split(a, !RAGGED, q4_blocks(n_all), total);
-  const int W = sp.W, rank = warp & (W - 1);
+  const int W = a.whole ? a.whole : sp.W, rank = warp & (W - 1);
   const int group = W == 1 ? blockIdx.x * kQ4DecWarps + warp : blockIdx.x;
   float* s_vals = reinterpret_cast<float*>(q4_smem + kQ4DecWarps * kQ4Stages * St::kBytes);
   uint8_t* s_q = reinterpret_cast<uint8_t*>(s_vals + kQ4DecWarps * GP * D) + warp * (State::NG + 1) * 512;
@@ -544,9 +549,22 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   // the range and its first pair
   Q4Cursor ci;
   ci.layer = a.n_layers;
-  if (!RAGGED && sp.k > 0) {
+  if (a.whole) {
+    if (group < a.n_layers * a.Hkv) {
+      ci.pair = group;
+      const int layer = fdivmod(group, a.by_heads, ci.h), nb = blocks_of(layer);
+      ci.blk = 0;
+      ci.end = ci.left = nb;
+      if (nb > 0) {
+        ci.layer = layer;
+      } else {
+        float4* out = reinterpret_cast<float4*>(a.out[layer] + (size_t)ci.h * a.G * D);
+        for (int t = rank * 32 + lane; t < a.G * D / 4; t += W * 32) out[t] = make_float4(0.f, 0.f, 0.f, 0.f);
+      }
+    }
+  } else if (!RAGGED && sp.k > 0) {
     const int nb = q4_blocks(n_all);
-    ci.pair = fdiv(group, a.by_k[W == 1]);
+    ci.pair = (unsigned)group / (unsigned)sp.k;
     ci.blk = (group - ci.pair * sp.k) * sp.per;
     if (ci.pair < a.n_layers * a.Hkv && ci.blk < nb) {
       ci.layer = fdivmod(ci.pair, a.by_heads, ci.h);
@@ -746,30 +764,35 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   }
 }
 
-// The partial states of a pair joined in key order; one (pair, head) a block.  Pairs that one range held whole are
+// The partial states of a pair joined in key order, by NW warps a (pair, head).  Pairs that one range held whole are
 // written already; those without keys are set to zero.
 // Which slots a pair has follows from the counts, which are final once the kernel before has passed its own wait: they are
 // read before this one's, as is the code that comes after it, run once with nothing to join (its blocks lie idle then).
 // Many slots a pair: eight warps with eight slots each in flight (57 slots of 8 pairs: 10.6 -> 10.2 us a call, 228 of 2: 9.1 ->
-// 8.3); few: four of four (the wide form holds back 32 layers by 3 us).
+// 8.3); some: four of four (8 layers 11.7 us, by one warp 12.5); few: a warp by itself, four in a block (64 layers x 8 heads x
+// 1019 rows 25.4 -> 21.9 us, x 16000, G = 5, 224 -> 220: it is the number of blocks that costs).
 template <int D, int NW>
-__global__ void __launch_bounds__(NW * 32) q4_merge_kernel(const __grid_constant__ Q4DecodeArgs a) {
-  constexpr int PER = D / 32, kInFlight = NW;
+__global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q4_merge_kernel(const __grid_constant__ Q4DecodeArgs a) {
+  constexpr int PER = D / 32, kInFlight = NW == 1 ? 4 : NW, kItems = NW == 1 ? 4 : 1;
   __shared__ Q4Lists s_list;
   __shared__ float s_ml[NW][2];
   __shared__ float s_v[NW][D];
-  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  int g, h;
-  const int pair = fdivmod(blockIdx.x, a.by_G, g), layer = fdivmod(pair, a.by_heads, h);
+  const int warp = NW == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const int item = blockIdx.x * kItems + (NW == 1 ? threadIdx.x >> 5 : 0);
   const bool uniform = q4_uniform(a);
+  if (!uniform) {
+    if (threadIdx.x < 32) q4_lists(a, s_list, false);
+    __syncthreads();
+  }
+  int g, h;
+  const int pair = fdivmod(item, a.by_G, g), layer = fdivmod(pair, a.by_heads, h);
+  if (layer >= a.n_layers) return;  // NW == 1: past the last pair
   int n, first, total;  // keys of the pair's cache, its first block in the list, all blocks
   if (uniform) {
     n = q4_keys(a, 0);
     first = layer * a.Hkv * q4_blocks(n);
     total = a.n_layers * a.Hkv * q4_blocks(n);
   } else {
-    if (warp == 0) q4_lists(a, s_list, false);
-    __syncthreads();
     n = s_list.n[layer];
     first = s_list.first[layer];
     total = s_list.first[a.n_layers];
@@ -779,7 +802,7 @@ __global__ void __launch_bounds__(NW * 32) q4_merge_kernel(const __grid_constant
   int slot = 0, count = 0;
   if (nb > 0 && sp.k > 0) {
     slot = pair * sp.k;
-    count = (unsigned)(nb + sp.per - 1) / (unsigned)sp.per;
+    count = sp.k;
   } else if (nb > 0) {
     const int b0 = first + h * nb, g0 = (unsigned)b0 / (unsigned)sp.per;
     slot = g0 + pair;
@@ -787,11 +810,12 @@ __global__ void __launch_bounds__(NW * 32) q4_merge_kernel(const __grid_constant
   }
   float* out = a.out[layer] + (size_t)(h * a.G + g) * D;
 #pragma unroll 1
-  for (int live = 0; live < 2; ++live) {
+  for (int live = count <= 1; live < 2; ++live) {
     if (live) {
       pdl_wait();
       pdl_launch_dependents();
-      if (nb == 0 && (int)threadIdx.x < D) out[threadIdx.x] = 0.f;
+      const int t = NW == 1 ? lane : threadIdx.x;
+      if (nb == 0 && t < D / 4) reinterpret_cast<float4*>(out)[t] = make_float4(0.f, 0.f, 0.f, 0.f);
       if (count <= 1) return;
     }
     float mm = -INFINITY, ll = 0.f, aa[PER];
@@ -812,23 +836,29 @@ __global__ void __launch_bounds__(NW * 32) q4_merge_kernel(const __grid_constant
 #pragma unroll
       for (int u = 0; u < kInFlight; ++u) q4_merge_state<PER>(mm, ll, aa, ml[u].x, ml[u].y, a2[u]);
     }
-    if (lane == 0) {
-      s_ml[warp][0] = mm;
-      s_ml[warp][1] = ll;
-    }
+    if constexpr (NW == 1) {
+      if (live)
 #pragma unroll
-    for (int e = 0; e < PER; ++e) s_v[warp][e * 32 + lane] = aa[e];
-    __syncthreads();
-    if ((int)threadIdx.x < D) {
-      float m1 = -INFINITY, l1 = 0.f, v1[1] = {0.f};
-#pragma unroll 1
-      for (int w = 0; w < NW; ++w) {
-        const float v2[1] = {s_v[w][threadIdx.x]};
-        q4_merge_state<1>(m1, l1, v1, s_ml[w][0], s_ml[w][1], v2);
+        for (int e = 0; e < PER; ++e) out[e * 32 + lane] = aa[e] / ll;
+    } else {
+      if (lane == 0) {
+        s_ml[warp][0] = mm;
+        s_ml[warp][1] = ll;
       }
-      if (live) out[threadIdx.x] = v1[0] / l1;
+#pragma unroll
+      for (int e = 0; e < PER; ++e) s_v[warp][e * 32 + lane] = aa[e];
+      __syncthreads();
+      if ((int)threadIdx.x < D) {
+        float m1 = -INFINITY, l1 = 0.f, v1[1] = {0.f};
+#pragma unroll 1
+        for (int w = 0; w < NW; ++w) {
+          const float v2[1] = {s_v[w][threadIdx.x]};
+          q4_merge_state<1>(m1, l1, v1, s_ml[w][0], s_ml[w][1], v2);
+        }
+        if (live) out[threadIdx.x] = v1[0] / l1;
+      }
+      __syncthreads();
     }
-    __syncthreads();
   }
 }
 
@@ -836,6 +866,18 @@ __global__ void __launch_bounds__(NW * 32) q4_merge_kernel(const __grid_constant
 size_t q4_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap) {
   const int64_t pairs = (int64_t)n_layers * Hkv, blocks = pairs * ((n_cap + kQ4Block - 1) / kQ4Block);
   return (size_t)(std::min<int64_t>(kQ4MaxGroups, blocks) + pairs) * (Hq / Hkv) * (d + 4) * sizeof(float);
+}
+
+// Warps that take a pair whole, which needs no partial states and no second kernel (1.5 to 4 us of a call), or 0; by the most
+// blocks a pair can have (where the counts are on the device: by n_cap).  More pairs than CTAs, and short: a warp each (64 layers x 8 heads
+// x 91 rows 8.8 -> 6.6 us, by a CTA each 8.6; at 16 blocks that was faster).  Else a CTA, while what its last wave leaves idle
+// costs less than that kernel: a round (32 keys a warp) of an idle SM counts 0.4 of a busy one's time, and both sides met at
+// 4 to 8 rounds (1 layer x 8 heads x 507 rows 6.6 -> 6.2 us, 763 rows 6.8 -> 7.4; 57 layers 94.5 -> 92.1 at 8272 rows).
+// Counts that differ leave CTAs idle too, at worst all but one: 12 rounds (64 layers x 8 heads x up to 1531 rows 32 -> 22 us).
+static int q4_whole(int pairs, int slots, int nb, bool ragged) {
+  if (pairs > slots && nb <= 12) return 1;
+  const int64_t rounds = (nb + kQ4DecWarps - 1) / kQ4DecWarps, idle = pairs % slots ? slots - pairs % slots : 0;
+  return rounds * idle <= 6 * slots && !(ragged && rounds > 12) ? kQ4DecWarps : 0;
 }
 
 template <int D, int GP>
@@ -848,9 +890,11 @@ static cudaError_t q4_decode_launch(const Q4DecodeArgs& a, cudaStream_t stream) 
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), smem);
   const int pairs = a.n_layers * a.Hkv;
   if (e == cudaSuccess) e = launch_kernel(kern, dim3(a.n_groups), dim3(kQ4DecThreads), smem, stream, a, true);
-  const int wide = a.n_groups >= 16 * pairs;
-  if (e == cudaSuccess)
-    e = launch_kernel(wide ? q4_merge_kernel<D, 8> : q4_merge_kernel<D, 4>, dim3(pairs * a.G), dim3(wide ? 256 : 128), 0, stream, a, true);
+  if (e == cudaSuccess && !a.whole) {
+    if (a.n_groups >= 16 * pairs) e = launch_kernel(q4_merge_kernel<D, 8>, dim3(pairs * a.G), dim3(256), 0, stream, a, true);
+    else if (a.n_groups > 5 * pairs) e = launch_kernel(q4_merge_kernel<D, 4>, dim3(pairs * a.G), dim3(128), 0, stream, a, true);
+    else e = launch_kernel(q4_merge_kernel<D, 1>, dim3((pairs * a.G + 3) / 4), dim3(128), 0, stream, a, true);
+  }
   return e;
 }
 
@@ -878,7 +922,10 @@ stepkv_status_t q4_decode_run(const stepkv_q4_cache_t& c, const void* const* q, 
     a.G = Hq / c.Hkv;
     // as many groups as run at once, none without a block
     const int64_t blocks = (int64_t)nl * c.Hkv * ((n_cap + kQ4Block - 1) / kQ4Block);
-    a.n_groups = (int)std::min<int64_t>(std::min(kQ4MaxGroups / kQ4DecWarps, n_sm * kQ4DecCtasPerSm), blocks);
+    const int slots = std::min(kQ4MaxGroups / kQ4DecWarps, n_sm * kQ4DecCtasPerSm);
+    a.n_groups = (int)std::min<int64_t>(slots, blocks);
+    a.whole = q4_whole(nl * c.Hkv, slots, ((n_dev ? n_cap : n_host) + kQ4Block - 1) / kQ4Block, n_dev && n_stride && nl > 1);
+    if (a.whole) a.n_groups = (nl * c.Hkv * a.whole + kQ4DecWarps - 1) / kQ4DecWarps;
     for (int i = 0; i < 2; ++i) {
       const int groups = a.n_groups * (i ? kQ4DecWarps : 1);
       a.by_groups[i] = make_fastdiv(groups);

@@ -489,6 +489,41 @@ def test_decode_more_pairs_than_ctas(B, L, Hkv, G, d, n):
         _check(ragged[l], q, K, V, int(counts[l]), f"cache {l} of {counts[l]}")
 
 
+FORMS = [  # L, Hkv, G, d, rows: pairs taken whole, by a CTA or a warp, and cut, with few, some and many states to join
+    (1, 3, 3, 64, 500), (5, 7, 1, 128, 700), (33, 14, 2, 64, 300), (60, 9, 5, 128, 200), (31, 3, 1, 64, 2100),
+    (23, 5, 3, 128, 1700), (64, 9, 1, 64, 1800), (57, 8, 1, 64, 1000), (9, 7, 4, 64, 4000), (2, 2, 2, 128, 9000)]
+
+
+@pytest.mark.parametrize("L,Hkv,G,d,rows", FORMS)
+def test_decode_forms_and_counts(B, L, Hkv, G, d, rows):
+    """Caches of the same rows under one count, long, short and zero, and under counts of their own: whatever way the work is
+    divided, each output is within its bound of the oracle's."""
+    import torch
+    rng = np.random.default_rng(L + rows)
+    K, V, q = _keys(rng, (Hkv, rows, d)), _bits(rng, (Hkv, rows, d)), _bits(rng, (Hkv * G, d))
+    cache = B.Q4Cache.allocate(L, Hkv, rows, d)
+    src = [TL.bf16_dev(x)[None].expand(L, -1, -1, -1) for x in (K, V)]
+    st = B.stepkv_q4_write(cache, *src, 0)
+    qd = TL.bf16_dev(q).expand(L, -1, -1).contiguous()
+    own = rng.integers(0, rows + 1, L).astype(np.int32)
+    own[rng.integers(0, L, 3)] = 0, rows, 1
+    for counts in (rows, rows - 33, 75, 1, 0, own, np.minimum(own, 40)):
+        n = _dev(np.atleast_1d(np.asarray(counts, np.int32)))
+        out = torch.full((L, Hkv * G, d), 7.0, device="cuda")
+        B.stepkv_q4_decode(qd, cache, n, out=out, status=st)
+        torch.cuda.synchronize()
+        assert st.item() == 0
+        each = np.broadcast_to(counts, (L,))
+        for m in sorted(set(each)) if L < 10 else sorted({each[0], each[L // 2], each[-1], each.min(), each.max()}):
+            same = np.flatnonzero(each == m)
+            _check(out[same[0]], q, K, V, int(m), f"{m} of {counts}, cache {same[0]}")
+            if m:
+                bound = 2 * _dev(_decode_bound(q, _values(K[:, :m]), _values(V[:, :m])))
+                assert all(((out[l] - out[same[0]]).abs() <= bound).all() for l in same)
+            else:
+                assert not out[same].any()
+
+
 @pytest.mark.parametrize("magnitude", [2.0 ** -9, 1.0, 2.0 ** 9])
 def test_decode_keys_of_any_magnitude(B, magnitude):
     """Keys as small and as large as normal scales hold, with queries that make up for it."""
