@@ -19,8 +19,8 @@
 // Every sum over keys starts from zero in the tensor core for 32 keys and is added in fp32, as its accumulation truncates.
 //
 // 543 instructions a block of 32 keys (G <= 4), of which unpacking V takes 176, K 96.  Mixed, they issue at 0.64 a cycle at
-// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 61.1 us, G =
-// 5: 67.8, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
+// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 60.6 us, G =
+// 5: 66.8, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
 // 66.0 (more moves), 8 of 255 72.4; three ring stages 66.0; a barrier that keeps the SM's warps in step 64-70 (they finish
 // between 45 and 60 us without, at the same rate in all); scales laid out in shared memory for their users 67.0.
 //

@@ -610,6 +610,24 @@ def test_decode_bad_counts(B):
             _check(out[l], q, K, V, max(0, min(n, rows)), f"counts {counts}, cache {l}")
 
 
+@pytest.mark.parametrize("each", [False, True])
+def test_decode_bad_counts_of_long_caches(B, each):
+    """As above where the work is cut into ranges: a count above the capacity uses the capacity, a negative one none."""
+    import torch
+    rng = np.random.default_rng(13)
+    L, Hkv, G, d, rows = 2, 2, 2, 64, 5000
+    K, V, q = _bits(rng, (Hkv, rows, d)), _bits(rng, (Hkv, rows, d)), _bits(rng, (Hkv * G, d))
+    cache, qd = _filled(B, [K, K], [V, V]), TL.bf16_dev(q).expand(L, -1, -1).contiguous()
+    for n, code, used in (([rows + 1, 3000], B.STEPKV_ENOSPACE, (rows, 3000)), ([2 ** 31 - 1, 0], B.STEPKV_ENOSPACE, (rows, 0)),
+                          ([-1, 40], B.STEPKV_EDATA, (0, 40)), ([-2 ** 31, rows], B.STEPKV_EDATA, (0, rows))):
+        st, out = B.new_status(), torch.full((L, Hkv * G, d), 7.0, device="cuda")
+        B.stepkv_q4_decode(qd, cache, _dev(np.array(n if each else n[:1], np.int32)), out=out, status=st)
+        torch.cuda.synchronize()
+        assert st.item() == code
+        for l in range(L):
+            _check(out[l], q, K, V, used[l if each else 0], f"{n}, cache {l}")
+
+
 @pytest.mark.parametrize("G", [3, 8])
 @pytest.mark.parametrize("Hkv,d,n", [(2, 128, 60), (2, 64, 3001), (64, 128, 2000)])
 @pytest.mark.parametrize("kind", ["nan key", "inf key", "nan value", "inf query", "nan query"])
