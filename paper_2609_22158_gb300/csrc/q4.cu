@@ -144,7 +144,7 @@ __device__ __forceinline__ Q4Set q4_set(const Q4Args& a, int set) {
 
 // A lane takes 16 channels of a row, vectors (8 channels) v and v + 2 of a group with v = lane & 1, so that a pair of lanes has
 // a group and reads 32 consecutive bytes at a time.  32 layers x 8 heads x 8272 rows: 216 us = 6.4 TB/s (by an index list of
-// 8272 in 8911 rows 229), bound by the copies; a division per channel took 655, lanes of 8 channels 272.
+// 8272 in 8911 rows 236), bound by the copies; a division per channel took 655, lanes of 8 channels 272.
 constexpr int kQ4WriteUnroll = 3;
 
 template <bool IDX>
