@@ -491,7 +491,8 @@ def test_decode_more_pairs_than_ctas(B, L, Hkv, G, d, n):
 
 FORMS = [  # L, Hkv, G, d, rows: pairs taken whole, by a CTA or a warp, and cut, with few, some and many states to join
     (1, 3, 3, 64, 500), (5, 7, 1, 128, 700), (33, 14, 2, 64, 300), (60, 9, 5, 128, 200), (31, 3, 1, 64, 2100),
-    (23, 5, 3, 128, 1700), (64, 9, 1, 64, 1800), (57, 8, 1, 64, 1000), (9, 7, 4, 64, 4000), (2, 2, 2, 128, 9000)]
+    (23, 5, 3, 128, 1700), (64, 9, 1, 64, 1800), (57, 8, 1, 64, 1000), (9, 7, 4, 64, 4000), (2, 2, 2, 128, 9000),
+    (66, 3, 2, 64, 2100)]
 
 
 @pytest.mark.parametrize("L,Hkv,G,d,rows", FORMS)
