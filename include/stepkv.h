@@ -438,7 +438,9 @@ STEPKV_API stepkv_status_t stepkv_q4_read(const stepkv_q4_cache_t* cache, const 
 
 /* stepkv_compact over a cache held in 4 bits: retained rows move as they are (codes and scales bit for bit).  Arguments,
  * results and errors as stepkv_compact, with the source's T rows in `in` (T <= in->rows) and kept_cap <= out->rows; `out`
- * shares no buffer with `in` (STEPKV_EUNSUPPORTED where a base pointer is the same), and holds values where `in` does.
+ * holds values where `in` does.  No byte of what is written (the first kept_cap rows of `out`, in any layer, keys, values and
+ * scales alike; step_id_out and pos_out) may be one of what is read (the first T rows of `in`, the index list, the count,
+ * step_id_in and pos_in) or be written twice: STEPKV_EUNSUPPORTED.
  */
 STEPKV_API stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_t T, const int32_t* kept_idx,
                                   const int32_t* n_kept, int32_t kept_cap, const stepkv_q4_cache_t* out,

@@ -10,6 +10,7 @@
 #include <vector>
 
 #include "common.cuh"
+#include "footprint.h"
 #include "internal.h"
 
 namespace stepkv {
@@ -441,6 +442,17 @@ static stepkv_status_t check_q4_cache(const stepkv_q4_cache_t* c, int values) {
   return STEPKV_OK;
 }
 
+// What the first `rows` rows of a cache take.
+static void add_q4_rows(Footprints& f, const stepkv_q4_cache_t& c, int rows, bool written) {
+  const int groups = c.d / STEPKV_Q4_GROUP;
+  const Footprint codes = make_footprint(c.Hkv, c.code_head_stride, 1, 0, (int64_t)rows * (c.d / 2));
+  const Footprint scales = make_footprint(c.Hkv, 2 * c.scale_head_stride, 1, 0, (int64_t)rows * groups * 2);
+  f.add(c.K, c.n_layers, codes, written);
+  f.add(c.K_scale, c.n_layers, scales, written);
+  f.add(c.V, c.n_layers, codes, written);
+  f.add(c.V_scale, c.n_layers, scales, written);
+}
+
 // bf16 rows at any order of heads and rows: pointers present and aligned, strides that keep every row aligned.
 static stepkv_status_t check_q4_rows(int n_layers, const void* const* K, const void* const* V, int64_t head_stride,
                                      int64_t row_stride, const Q4Rows& r) {
@@ -497,10 +509,17 @@ stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_t T, const 
   if (in->n_layers != out->n_layers || in->Hkv != out->Hkv || in->d != out->d) return STEPKV_EINVAL;
   if ((in->V == nullptr) != (out->V == nullptr)) return STEPKV_EINVAL;
   if (T < 1 || T > in->rows || kept_cap < 0 || kept_cap > out->rows || !kept_idx || !n_kept) return STEPKV_EINVAL;
-  for (int l = 0; l < in->n_layers; ++l) {
-    if (in->K[l] == out->K[l] || in->K_scale[l] == out->K_scale[l]) return STEPKV_EUNSUPPORTED;
-    if (in->V && (in->V[l] == out->V[l] || in->V_scale[l] == out->V_scale[l])) return STEPKV_EUNSUPPORTED;
-  }
+  // a row written is no row read (or written twice); a step id or position neither
+  Footprints f;
+  add_q4_rows(f, *in, T, false);
+  add_q4_rows(f, *out, std::max(kept_cap, 1), true);
+  auto vector = [&](const void* const* p, int n, bool written) {
+    f.add(*p ? p : nullptr, 1, Footprint{1, 0, 1, 0, 4 * (int64_t)n}, written);
+  };
+  const void* const vectors[6] = {kept_idx, n_kept, step_id_in, pos_in, step_id_out, pos_out};
+  const int lengths[6] = {kept_cap, 1, T, T, kept_cap, kept_cap};
+  for (int i = 0; i < 6; ++i) vector(vectors + i, lengths[i], i >= 4);
+  if (f.clash()) return STEPKV_EUNSUPPORTED;
   return q4_compact_run(*in, T, kept_idx, n_kept, kept_cap, *out, step_id_in, pos_in, step_id_out, pos_out, dev_status,
                         static_cast<cudaStream_t>(stream));
 }

@@ -387,6 +387,49 @@ def test_compact_bad_data(B):
     assert pos.tolist() == [0, -1, -1, 19, -7, -7, -7, -7] and step.tolist() == [-1] * 4 + [-7] * 4
 
 
+@pytest.mark.parametrize("kind", ["rows of one buffer", "layers inside heads", "the next layers"])
+def test_compact_between_views_of_one_buffer(B, kind):
+    """Source and destination lie inside one another's strides without sharing a row."""
+    import torch
+    rng = np.random.default_rng(15)
+    L, Hkv, d, T, n = 3, 2, 128, 40, 17
+    idx = np.sort(rng.permutation(T)[:n]).astype(np.int32)
+
+    def views(w, t):
+        if kind == "rows of one buffer":      # [layer][head][row]: the first T rows, and those behind
+            x = torch.zeros((L, Hkv, T + n, w), dtype=t, device="cuda")
+            return x[:, :, :T], x[:, :, T:]
+        if kind == "layers inside heads":     # [head][source, destination][layer][row]
+            x = torch.zeros((Hkv, 2, L, T, w), dtype=t, device="cuda").transpose(0, 2)
+            return x[:, 0], x[:, 1]
+        x = torch.zeros((2 * L, Hkv, T, w), dtype=t, device="cuda")
+        return x[:L], x[L:]
+
+    parts = [views(64, torch.uint8), views(4, torch.float16), views(64, torch.uint8), views(4, torch.float16)]
+    src, dst = (B.Q4Cache(*[p[i] for p in parts]) for i in range(2))
+    for x in (src.K, src.V):
+        x.copy_(_dev(rng.integers(0, 256, tuple(x.shape), dtype=np.uint8)))
+    for x in (src.K_scale, src.V_scale):
+        x.copy_(_dev(rng.standard_normal(tuple(x.shape)).astype(np.float16)))
+    st = B.stepkv_q4_compact(src, T, _dev(idx), torch.tensor([n], dtype=torch.int32, device="cuda"), n, dst)
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    for a, b in parts:
+        assert torch.equal(b[:, :, :n], a[:, :, _dev(idx).long()])
+
+
+def test_compact_refuses_the_same_layers_moved_by_one(B):
+    import torch
+    cache = B.Q4Cache.allocate(3, 2, 20, 64)
+    kept, n = torch.zeros(20, dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    for src, dst in ((cache.layers(0, 2), cache.layers(1, 3)), (cache.layers(1, 3), cache.layers(0, 2)),
+                     (cache.layers(0, 1), B.Q4Cache(cache.V[:1], cache.V_scale[:1], cache.K[1:2], cache.K_scale[:1]))):
+        with pytest.raises(B.StepKVError):
+            B.stepkv_q4_compact(src, 20, kept, n, 20, dst)
+    B.stepkv_q4_compact(cache.layers(0, 1), 20, kept, n, 20, cache.layers(2, 3))  # another layer: no row in common
+    torch.cuda.synchronize()
+
+
 # ------------------------------------------------------------------------------------------------ decode attention
 def _decode_bound(q, K, V):
     """Per head and channel: what fp32 arithmetic may lose of out = sum_j p_j V_j / sum_j p_j.

@@ -186,6 +186,29 @@ def test_compact_refusals(lib):
         assert _compact(lib, **{part: p.value, "out_" + part: p.value}) == EUNSUPPORTED, part
 
 
+MB = 1 << 20
+
+
+@pytest.mark.parametrize("over", [
+    dict(out_K=(2 * MB, 30 * MB)),                         # layer 0 of the destination is layer 1 of the source, as
+    dict(out_K_scale=(4 * MB, 30 * MB)),                   # cache.layers(0, 2) -> cache.layers(1, 3) has it
+    dict(out_V=(1 * MB, 30 * MB)), dict(out_K=(30 * MB, 5 * MB)),      # keys over values, values over keys
+    dict(out_K=(2 * MB - 16, 30 * MB)), dict(out_V=(6 * MB + 6400 + 2480, 30 * MB)),  # a few rows of a head
+    dict(out_K_scale=(1 * MB + 64, 30 * MB)),              # scales over codes
+    dict(out_K=(30 * MB, 30 * MB)), dict(out_K=(30 * MB, 31 * MB), out_V=(32 * MB, 31 * MB + 6400)),  # the same row written twice
+    dict(step_in=40 * MB, step_out=40 * MB), dict(step_in=40 * MB, step_out=40 * MB + 396), dict(pos_in=40 * MB, step_out=40 * MB),
+    dict(step_out=40 * MB, pos_out=40 * MB + 196), dict(pos_out=1 << 27), dict(step_out=7 * MB)])
+def test_compact_refuses_destinations_that_meet_the_source(lib, over):
+    """Rows move in one launch in no order: a destination that is a source as well would be read half written."""
+    keep = [_ptrs(*v) for k, v in over.items() if isinstance(v, tuple)]
+    caches = dict(zip((k for k, v in over.items() if isinstance(v, tuple)), (p.value for p, _ in keep)))
+    a = _Args(**caches)
+    x = a.x
+    got = lib.stepkv_q4_compact(ctypes.byref(a.cache), x["T"], x["kept"], x["n_kept"], x["cap"], ctypes.byref(a.out),
+                                over.get("step_in"), over.get("pos_in"), over.get("step_out"), over.get("pos_out"), None, None)
+    assert got == EUNSUPPORTED
+
+
 @pytest.mark.parametrize("over,code", [
     (dict(src=None), EINVAL), (dict(outs=None), EINVAL), (dict(ws=None), EINVAL), (dict(Hq=0), EINVAL), (dict(Hq=7), EINVAL),
     (dict(Hq=18), EUNSUPPORTED), (dict(d=96, code=6400, scale=402), EUNSUPPORTED), (dict(n_cap=0), EINVAL), (dict(n_cap=101), EINVAL),
