@@ -417,7 +417,8 @@ typedef struct {
  *  row0        the first row written, the same for all layers; with row0_dev given, row0_dev[l * row0_dev_stride]
  *              (device; stride 0: one for all layers, 1: one each) takes its place.  A layer whose rows would
  *              not all lie in [0, rows) sets STEPKV_ENOSPACE and is not written.
- * Other rows of the cache are left as they are.
+ * Other rows of the cache are left as they are.  The cache's codes and scales share no memory with one another, in any layer
+ * (STEPKV_EINVAL; caches that are only read may share theirs), nor with K and V.
  */
 STEPKV_API stepkv_status_t stepkv_q4_write(const stepkv_q4_cache_t* cache, const void* const* K, const void* const* V,
                                 int64_t head_stride, int64_t row_stride, int32_t T, const int32_t* idx,
@@ -427,7 +428,9 @@ STEPKV_API stepkv_status_t stepkv_q4_write(const stepkv_q4_cache_t* cache, const
 /* Reads rows back to bf16 (exactly, see above): for every layer l, KV head h and r < n,
  *   K[l][h][r][:] = row (idx ? idx[r] : row0 + r) of the cache   (V alike).
  * E.g. the saliency layers' keys for stepkv_score, or a whole cache for a prefill.
- *  K, V        host arrays of device pointers to bf16, strides as in stepkv_q4_write; either may be NULL (not both).
+ *  K, V        host arrays of device pointers to bf16, strides as in stepkv_q4_write; either may be NULL (not both).  Rows
+ *              written do not share memory (STEPKV_EINVAL: one buffer for two layers or for keys and values, heads that
+ *              overlap; rows and heads nest in either order) nor lie in the cache.
  *  idx, n, n_dev, row0, row0_dev as in stepkv_q4_write; row0 is not used with idx.  A row outside [0, rows) sets
  *  STEPKV_EDATA and is not read: with idx that row, else the layer.
  */
@@ -454,7 +457,7 @@ STEPKV_API stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_
  *              else n_host (0 <= n_host <= n_cap).  0: nothing to attend to, the output is zero.  A count above n_cap
  *              sets STEPKV_ENOSPACE and n_cap rows are used; a negative one sets STEPKV_EDATA, the output is zero.
  *  n_cap       at most rows; the workspace and the split of the work go by it.
- *  out[l]      host array of device pointers, [Hq][d] fp32, 16-byte aligned.
+ *  out[l]      host array of device pointers, [Hq][d] fp32, 16-byte aligned; outputs that overlap are refused (STEPKV_EINVAL).
  *  ws          scratch of stepkv_q4_decode_workspace_size bytes (256-byte aligned): partial states.
  *  Rows at or past the count are not used, whatever they hold.  A key or a query with a NaN or an infinity makes the
  *  outputs of its heads NaN; a value row that reads back as NaN makes those channels NaN.

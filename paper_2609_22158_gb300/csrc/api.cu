@@ -480,6 +480,9 @@ stepkv_status_t stepkv_q4_write(const stepkv_q4_cache_t* cache, const void* cons
   if (!idx && n > T) return STEPKV_EINVAL;
   if (!row0_dev && !n_dev && (row0 < 0 || (int64_t)row0 + n > cache->rows)) return STEPKV_ENOSPACE;
   if (n == 0) return STEPKV_OK;
+  Footprints f;  // no two of the cache's tensors may share a row
+  add_q4_rows(f, *cache, cache->rows, true);
+  if (f.clash()) return STEPKV_EINVAL;
   return q4_write_run(*cache, K, V, head_stride, row_stride, T, r, dev_status, static_cast<cudaStream_t>(stream));
 }
 
@@ -496,6 +499,11 @@ stepkv_status_t stepkv_q4_read(const stepkv_q4_cache_t* cache, const int32_t* id
   if ((head_stride < cache->d && cache->Hkv > 1) || (row_stride < cache->d && n > 1)) return STEPKV_EINVAL;  // rows apart
   if (!idx && !row0_dev && !n_dev && (row0 < 0 || (int64_t)row0 + n > cache->rows)) return STEPKV_EINVAL;
   if (n == 0) return STEPKV_OK;
+  Footprints f;
+  const Footprint rows = make_footprint(cache->Hkv, 2 * head_stride, n, 2 * row_stride, 2 * (int64_t)cache->d);
+  f.add(K, cache->n_layers, rows, true);
+  f.add(V, cache->n_layers, rows, true);
+  if (f.clash()) return STEPKV_EINVAL;
   return q4_read_run(*cache, r, K, V, head_stride, row_stride, dev_status, static_cast<cudaStream_t>(stream));
 }
 
@@ -547,6 +555,9 @@ stepkv_status_t stepkv_q4_decode(const stepkv_q4_cache_t* cache, const void* con
     if (!q[l] || !out[l]) return STEPKV_EINVAL;
     if (!aligned16(q[l]) || !aligned16(out[l])) return STEPKV_EUNSUPPORTED;
   }
+  Footprints f;
+  f.add(reinterpret_cast<const void* const*>(out), cache->n_layers, Footprint{1, 0, 1, 0, 4 * (int64_t)Hq * cache->d}, true);
+  if (f.clash()) return STEPKV_EINVAL;
   return q4_decode_run(*cache, q, Hq, n_dev, n_dev_stride, n_host, n_cap, out, ws, dev_status,
                        static_cast<cudaStream_t>(stream));
 }

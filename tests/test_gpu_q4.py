@@ -334,6 +334,43 @@ def test_read_by_index_of_values_alone(B):
 
 
 # ------------------------------------------------------------------------------------------------ compaction
+@pytest.mark.parametrize("order", ["lhnd", "nlhd", "hlnd", "hnld", "lnhd", "nhld"])
+def test_read_into_any_order_of_axes(B, order):
+    """Rows of all layers, keys and values in one buffer whose axes come in any order: nothing shares memory, so each is read
+    into; a layer, a tensor or a head laid over another is refused."""
+    import torch
+    rng = np.random.default_rng(16)
+    size = dict(l=3, h=2, n=7, d=64)
+    K, V = [_bits(rng, (2, 7, 64)) for _ in range(3)], [_bits(rng, (2, 7, 64)) for _ in range(3)]
+    cache, st = _filled(B, K, V), B.new_status()
+    for front in (True, False):  # keys and values apart, or side by side inside each row's place
+        shape = [size[a] for a in order[:3]]
+        x = torch.full([2, *shape, 64] if front else [*shape, 2, 64], 7.0, dtype=torch.bfloat16, device="cuda")
+        kv = x.unbind(0 if front else 3)
+        Kb, Vb = (t.permute([order.index(a) for a in "lhnd"]) for t in kv)
+        B.stepkv_q4_read(cache, K=Kb, V=Vb, status=st)
+        torch.cuda.synchronize()
+        assert st.item() == 0
+        _same_bits(Kb, np.stack([_back_bits(k) for k in K]))
+        _same_bits(Vb, np.stack([_back_bits(v) for v in V]))
+    one = torch.zeros((1, 2, 7, 64), dtype=torch.bfloat16, device="cuda")
+    for bad in (lambda: B.stepkv_q4_read(cache, K=Kb, V=Kb), lambda: B.stepkv_q4_read(cache, K=one.expand(3, -1, -1, -1)),
+                lambda: B.stepkv_q4_read(cache, K=one.view(-1).as_strided((3, 2, 7, 64), (0, 64, 64, 1))),
+                lambda: B.stepkv_q4_decode(torch.zeros((3, 4, 64), dtype=torch.bfloat16, device="cuda"), cache, 5,
+                                           out=torch.zeros((1, 4, 64), device="cuda").expand(3, -1, -1)),
+                lambda: B.stepkv_q4_write(B.Q4Cache(*(t[:1].expand(3, -1, -1, -1) for t in (cache.K, cache.K_scale, cache.V, cache.V_scale))),
+                                          Kb, Vb, 0),
+                lambda: B.stepkv_q4_write(B.Q4Cache(cache.K, cache.K_scale, cache.K, cache.V_scale), Kb, Vb, 0)):
+        with pytest.raises(B.StepKVError):
+            bad()
+    shared = B.Q4Cache(*(t[:1].expand(3, -1, -1, -1) for t in (cache.K, cache.K_scale, cache.V, cache.V_scale)))
+    q = _bits(rng, (4, 64))
+    out = B.stepkv_q4_decode(TL.bf16_dev(q).expand(3, -1, -1), shared, 7, status=st)  # reading one cache for all is not refused
+    torch.cuda.synchronize()
+    for l in range(3):
+        _check(out[l], q, K[0], V[0], 7, f"cache {l}")
+
+
 @pytest.mark.parametrize("L,Hkv,d,T,n,values", [(1, 2, 64, 50, 13, True), (3, 2, 128, 100, 100, True), (2, 1, 32, 9, 1, True),
                                                  (2, 3, 96, 40, 39, False), (70, 2, 128, 20, 7, True), (1, 2, 256, 33, 5, True),
                                                  (2, 2, 160, 33, 20, True), (4, 8, 128, 3000, 2001, True)])

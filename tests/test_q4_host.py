@@ -209,6 +209,20 @@ def test_compact_refuses_destinations_that_meet_the_source(lib, over):
     assert got == EUNSUPPORTED
 
 
+@pytest.mark.parametrize("call,over", [
+    (_write, dict(V=(1 * MB, 2 * MB))), (_write, dict(K=(30 * MB, 30 * MB))), (_write, dict(K=(30 * MB, 30 * MB + 2 * 6400 - 16))),
+    (_write, dict(V=(30 * MB, 1 * MB + 6400))), (_write, dict(V_scale=(1 * MB, 8 * MB))), (_write, dict(V_scale=(3 * MB + 1592, 8 * MB))),
+    (_read, dict(val=(21 * MB, 22 * MB))),                            # keys and values to one buffer
+    (_read, dict(val=(30 * MB, 22 * MB))), (_read, dict(src=(30 * MB, 30 * MB))),   # a layer's twice
+    (_read, dict(src=(30 * MB, 30 * MB + 25600 + 2304))),             # the second head of layer 0
+    (_read, dict(hs=128, rs=128)), (_read, dict(hs=128 * 9)), (_read, dict(hs=128, rs=136)),  # heads that overlap
+    (_decode, dict(outs=(30 * MB, 30 * MB))), (_decode, dict(outs=(30 * MB, 30 * MB + 4080)))])
+def test_destinations_that_overlap_are_refused(lib, call, over):
+    """Two warps would write the same bytes in no order."""
+    keep = {k: _ptrs(*v) for k, v in over.items() if isinstance(v, tuple)}
+    assert call(lib, **{k: keep[k][0].value if k in keep else v for k, v in over.items()}) == EINVAL
+
+
 @pytest.mark.parametrize("over,code", [
     (dict(src=None), EINVAL), (dict(outs=None), EINVAL), (dict(ws=None), EINVAL), (dict(Hq=0), EINVAL), (dict(Hq=7), EINVAL),
     (dict(Hq=18), EUNSUPPORTED), (dict(d=96, code=6400, scale=402), EUNSUPPORTED), (dict(n_cap=0), EINVAL), (dict(n_cap=101), EINVAL),
