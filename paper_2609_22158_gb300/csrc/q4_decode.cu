@@ -758,6 +758,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
       }
       sync_group();
     }
+    __syncwarp();  // (another warp's pair: all lanes have read s_here)
     next_pair(ci);
     if (ci.layer == a.n_layers) break;
     if (lane == 0) s_here[warp] = ci;

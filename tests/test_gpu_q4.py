@@ -675,6 +675,31 @@ def test_decode_ragged_batch(B, Hkv, G, d, counts, rows):
         _check(out[l], q, K, V, counts[l], f"cache {l}")
 
 
+@pytest.mark.parametrize("G,d", [(4, 128), (6, 64)])
+def test_decode_pairs_that_other_warps_take(B, G, d):
+    """Ranges that run over many pairs of a block or two, of which each warp takes every fourth and passes over the others, with
+    long pairs in between that all take: a warp that lost its place would skip a pair or take one twice.  Every output against
+    the oracle."""
+    import torch
+    rng = np.random.default_rng(G)
+    Hkv, rows = 40, 1700  # 64 x 40 pairs in 456 ranges
+    counts = [int(x) for x in rng.choice([1, 31, 32, 33, 64], 64)]
+    counts[::9] = [rows - int(x) for x in rng.integers(0, 64, len(counts[::9]))]
+    K, V, q = _bits(rng, (1, rows, d)), _bits(rng, (1, rows, d)), _bits(rng, (G, d), 2.0)
+    one = _filled(B, [K], [V])
+    cache = B.Q4Cache(*(t.expand(64, Hkv, -1, -1).contiguous() for t in (one.K, one.K_scale, one.V, one.V_scale)))
+    st, out = B.new_status(), torch.full((64, Hkv * G, d), 7.0, device="cuda")
+    B.stepkv_q4_decode(TL.bf16_dev(q).repeat(64, Hkv, 1), cache, _dev(np.array(counts, np.int32)), out=out, status=st)
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    for n in sorted(set(counts)):
+        want = O.q4_decode_attention(q, _values(K[:, :n]), _values(V[:, :n]))
+        bound = _decode_bound(q, _values(K[:, :n]), _values(V[:, :n]))
+        for l in (l for l in range(64) if counts[l] == n):
+            err = np.abs(out[l].view(Hkv, G, d).cpu().numpy().astype(np.float64) - want)
+            assert (err <= bound).all(), f"cache {l} of {n} rows: off by {(err / bound).max():.3g} times the bound"
+
+
 def test_decode_bad_counts(B):
     import torch
     rng = np.random.default_rng(12)
