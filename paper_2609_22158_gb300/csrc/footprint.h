@@ -3,7 +3,7 @@
 // A tensor is outer_n runs, outer_step bytes apart, of inner_n pieces, inner_step bytes apart, of len bytes each: heads of a
 // cache (one piece a run), or heads and rows of bf16 rows in either order.  Layers may lie inside one another's strides ([head]
 // [layer][row] or [token][layer][head]), so extents alone do not tell; whether two tensors meet is answered exactly.
-// The usual case, extents that lie apart, is one walk over the addresses in order: no allocation, 0.1 us for 128 tensors.
+// On the host 0.2 us of a call over 32 layers where these lie in one tensor, 1 to 2 where each is allocated by itself.
 #pragma once
 
 #include <stdint.h>
@@ -38,7 +38,7 @@ class Footprints {
   bool clash() const {
     for (int i = 0; i < lists_; ++i)
       if (list_[i].written && list_[i].f.folds()) return true;
-    return !apart() && !apart_in_detail();
+    return !apart();
   }
 
  private:
@@ -49,89 +49,78 @@ class Footprints {
     Footprint f;
     bool written;
   };
-  struct Piece {
-    uint64_t at;
-    const List* of;
-    bool operator<(const Piece& o) const { return at < o.at; }
-  };
   List list_[kMaxLists];
   int lists_ = 0;
 
   static uint64_t addr(const void* p) { return reinterpret_cast<uintptr_t>(p); }
+  // a tensor as one number: its address and its list
+  static uint64_t at(uint64_t key) { return key / kMaxLists; }
+  const List& of(uint64_t key) const { return list_[key % kMaxLists]; }
 
-  // Every list rises or falls, and in the order of addresses no extent begins inside one it must not meet.
-  bool apart() const {
-    int next[kMaxLists], step[kMaxLists], left[kMaxLists];
+  // Lists whose tensors lie apart from one another and, all of them, from every list they must not meet are done with.
+  // Returns how many tensors the others have.
+  int mixed(bool (&done)[kMaxLists]) const {
+    uint64_t low[kMaxLists], high[kMaxLists];
     for (int i = 0; i < lists_; ++i) {
       const List& l = list_[i];
-      const bool falls = addr(l.at[l.n - 1]) < addr(l.at[0]);
-      step[i] = falls ? -1 : 1;
-      next[i] = falls ? l.n - 1 : 0;
-      left[i] = l.n;
-    }
-    uint64_t end = 0, end_written = 0;
-    for (;;) {
-      int first = -1;
-      uint64_t low = UINT64_MAX, second = UINT64_MAX;
-      for (int i = 0; i < lists_; ++i) {
-        if (!left[i]) continue;
-        const uint64_t a = addr(list_[i].at[next[i]]);
-        if (first < 0 || a < low) {
-          second = low;
-          low = a;
-          first = i;
-        } else {
-          second = std::min(second, a);
-        }
-      }
-      if (first < 0) return true;
-      const List& l = list_[first];
       const uint64_t span = (uint64_t)l.f.span();
-      for (uint64_t a = low; a <= second;) {  // (this list up to the next one's first)
-        if (a < (l.written ? end : end_written)) return false;
-        end = std::max(end, a + span);
-        if (l.written) end_written = std::max(end_written, a + span);
-        next[first] += step[first];
-        if (--left[first] == 0) break;
-        const uint64_t b = addr(l.at[next[first]]);
-        if (b < a) return false;  // not in order
+      uint64_t a = addr(l.at[0]);
+      bool up = true, down = true;
+      low[i] = high[i] = a;
+      for (int j = 1; j < l.n; ++j) {
+        const uint64_t b = addr(l.at[j]);
+        up &= b >= a + span;
+        down &= a >= b + span;
+        low[i] = std::min(low[i], b);
+        high[i] = std::max(high[i], b);
         a = b;
       }
+      high[i] += span;
+      done[i] = up || down || !l.written;
     }
+    for (int i = 0; i < lists_; ++i)
+      for (int j = i + 1; j < lists_; ++j)
+        if ((list_[i].written || list_[j].written) && low[i] < high[j] && low[j] < high[i]) done[i] = done[j] = false;
+    int n = 0;
+    for (int i = 0; i < lists_; ++i) n += done[i] ? 0 : list_[i].n;
+    return n;
   }
 
-  // The same with every tensor looked at: those whose extents meet, in groups, by how they interleave, else pair by pair.
-  bool apart_in_detail() const {
-    int n = 0;
-    for (int i = 0; i < lists_; ++i) n += list_[i].n;
-    std::unique_ptr<Piece[]> p(new (std::nothrow) Piece[n]);
+  bool apart() const {
+    bool done[kMaxLists];
+    const int n = mixed(done);
+    if (n == 0) return true;
+    constexpr int kHere = 512;
+    uint64_t here[kHere];
+    std::unique_ptr<uint64_t[]> heap(n > kHere ? new (std::nothrow) uint64_t[n] : nullptr);
+    uint64_t* const p = n > kHere ? heap.get() : here;
     if (!p) return false;
     int k = 0;
     for (int i = 0; i < lists_; ++i)
-      for (int j = 0; j < list_[i].n; ++j) p[k++] = Piece{addr(list_[i].at[j]), &list_[i]};
-    std::sort(p.get(), p.get() + n);
+      for (int j = 0; !done[i] && j < list_[i].n; ++j) p[k++] = addr(list_[i].at[j]) * kMaxLists + i;  // (addresses: 57 bits)
+    std::sort(p, p + n);
+    // tensors whose extents meet, in groups: apart by how they interleave, else pair by pair
     for (int i0 = 0, i1; i0 < n; i0 = i1) {
       uint64_t end = 0;
-      for (i1 = i0; i1 < n && (i1 == i0 || p[i1].at < end); ++i1)
-        end = std::max(end, p[i1].at + (uint64_t)p[i1].of->f.span());
-      if (i1 - i0 == 1 || interleaved(&p[i0], i1 - i0, true) || interleaved(&p[i0], i1 - i0, false)) continue;
+      for (i1 = i0; i1 < n && (i1 == i0 || at(p[i1]) < end); ++i1) end = std::max(end, at(p[i1]) + (uint64_t)of(p[i1]).f.span());
+      if (i1 - i0 == 1 || interleaved(p + i0, i1 - i0, true) || interleaved(p + i0, i1 - i0, false)) continue;
       for (int i = i0; i < i1; ++i)
         for (int j = i + 1; j < i1; ++j)
-          if ((p[i].of->written || p[j].of->written) && meet(p[i], p[j])) return false;
+          if ((of(p[i]).written || of(p[j]).written) && meet((int64_t)(at(p[j]) - at(p[i])), of(p[i]).f, of(p[j]).f)) return false;
     }
     return true;
   }
 
   // All of one period (the outer step, or the inner one as well), with their runs (pieces) one after another inside it.
-  static bool interleaved(const Piece* p, int n, bool runs) {
-    const Footprint& f = p[0].of->f;
+  bool interleaved(const uint64_t* p, int n, bool runs) const {
+    const Footprint& f = of(p[0]).f;
     const int64_t period = runs ? f.outer_step : f.inner_step;
     for (int i = 0; i < n; ++i) {
-      const Footprint& g = p[i].of->f;
+      const Footprint& g = of(p[i]).f;
       if (g.folds() || g.outer_n == 1 || g.outer_step != f.outer_step) return false;
       if (!runs && (g.inner_n == 1 || g.inner_step != f.inner_step || g.outer_step % g.inner_step)) return false;
-      const uint64_t end = p[i].at + (uint64_t)(runs ? g.run() : g.len);
-      if (end > (i + 1 < n ? p[i + 1].at : p[0].at + (uint64_t)period)) return false;
+      const uint64_t end = at(p[i]) + (uint64_t)(runs ? g.run() : g.len);
+      if (end > (i + 1 < n ? at(p[i + 1]) : at(p[0]) + (uint64_t)period)) return false;
     }
     return true;
   }
@@ -146,9 +135,8 @@ class Footprints {
     return (q < n && r < len) || (q + 1 < n && step - r < len);
   }
 
-  static bool meet(const Piece& a, const Piece& b) {
-    const Footprint &f = a.of->f, &g = b.of->f;
-    const int64_t d = (int64_t)(b.at - a.at);
+  // Whether a tensor of footprint g, d bytes behind one of footprint f, meets it.
+  static bool meet(int64_t d, const Footprint& f, const Footprint& g) {
     const bool alike = f.outer_n == g.outer_n && f.inner_n == g.inner_n && f.len == g.len &&
                        (f.outer_n == 1 || f.outer_step == g.outer_step) && (f.inner_n == 1 || f.inner_step == g.inner_step);
     if (alike && !f.folds()) {  // translates: a run of one can only meet the two of the other that lie next to it
