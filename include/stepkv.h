@@ -462,8 +462,10 @@ STEPKV_API stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_
  *  Rows at or past the count are not used, whatever they hold.  A key or a query with a NaN or an infinity makes the
  *  outputs of its heads NaN; a value row that reads back as NaN makes those channels NaN.
  *  Supported: d in {64, 128}; Hq a multiple of Hkv with at most 8 query heads per KV head.
- *  Accuracy is fp32's for groups whose scale is a normal fp16 number (2^-14: a largest channel of 2^-11); the logits
- *  and values of groups below that lose a bit for each halving.
+ *  Accuracy is fp32's relative to the largest channel of a group: a logit is off by at most 3 2^-22 / sqrt(d) times the sum,
+ *  over the key's groups, of (largest magnitude of the group) (sum of |q| over its channels).  Values are exact to fp32's
+ *  rounding where their group's scale is a normal fp16 number (2^-14: a largest channel of 2^-11); below, they lose a bit for
+ *  each halving.
  *  Deterministic; the last bits depend on the split, which goes by the counts, n_layers, Hkv and n_cap.
  */
 STEPKV_API size_t stepkv_q4_decode_workspace_size(int32_t n_layers, int32_t Hkv, int32_t Hq, int32_t d, int32_t n_cap);

@@ -10,17 +10,20 @@
 //     first binade run on linearly), with the code in bits 3-6 n 2^-21: two shifts and four masks turn a word of eight codes
 //     into operands.  (Lower still the tensor core loses bits: it does not normalise subnormals.  e4m3 operands, 0000nnnn =
 //     n 2^-9, take a shift and two masks, but their mma.sync runs as conversions and two fp16 MMAs: 81 us where this
-//     took 77.)  Q is scaled by a power of two and exact in fp16.  A group's 32 channels are two k-steps; its scale is applied
-//     to the fp32 sum, and the -8 of all groups is one more MMA, of the scales and -8 sum(q).
+//     took 77.)  Q is scaled by a power of two and exact in fp16.  A group's 32 channels are two k-steps from
+//     -8 sum(q) of the group, which the sum of n q nearly cancels where the codes are near 8; the scale is applied to what is
+//     left, so that groups do not round against each other.  (The -8 of all groups first, as one MMA of the scales and -8
+//     sum(q), took 12 instructions a block fewer, 60.5 us, but logits rounded by the sum of all |s| 8 sum(q): outputs off by
+//     1.5e-6 instead of 1.9e-7 for queries of one sign over keys with one channel a group.)
 //   O^T = V^T P^T.  ldmatrix with transposition puts the codes of two keys and one chunk of 4 channels into a word; each
 //     pair of codes becomes (64 + n) s - 72 s = (n - 8) s by a mask and one packed FMA, exactly (s has 5 bits, 72 has 4).
 //     The weights are two fp16 terms, 22 bits, and come from the layout of S^T by movmatrix.
 // For G <= 4 columns 4-7 repeat the heads of columns 0-3, and P has its first terms in 0-3 and its second in 4-7.
 // Every sum over keys starts from zero in the tensor core for 32 keys and is added in fp32, as its accumulation truncates.
 //
-// 543 instructions a block of 32 keys (G <= 4), of which unpacking V takes 176, K 96.  Mixed, they issue at 0.64 a cycle at
-// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 60.6 us, G =
-// 5: 66.8, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
+// 556 instructions a block of 32 keys (G <= 4), of which unpacking V takes 176, K 96.  Mixed, they issue at 0.64 a cycle at
+// most (a probe of LOP3, HFMA2, FFMA and MMA together), which bounds the kernel: 32 layers x 8 heads x 8272 rows 60.8 us, G =
+// 5: 67.7, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
 // 66.0 (more moves), 8 of 255 72.4; three ring stages 66.0; a barrier that keeps the SM's warps in step 64-70 (they finish
 // between 45 and 60 us without, at the same rate in all); scales laid out in shared memory for their users 67.0.
 //
@@ -184,11 +187,16 @@ __device__ __forceinline__ void q4_lds(uint32_t (&w)[BYTES / 4], uint32_t addr) 
     asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(addr));
 }
 
-// D = A B, and D += A B, for one m16n8k16 tile of fp16.
+// D = A B, D = A B + (c0, c1 in both rows), and D += A B, for one m16n8k16 tile of fp16.
 __device__ __forceinline__ void mma_f16_zero(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
                : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
                : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
+}
+__device__ __forceinline__ void mma_f16_from(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, uint32_t c0, uint32_t c1) {
+  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
+               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
+               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(__uint_as_float(c0)), "f"(__uint_as_float(c1)));
 }
 __device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
   asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
@@ -243,7 +251,8 @@ struct Q4State {
   static constexpr int NT = D / 16;     // 16-channel tiles of a value row
   static constexpr int NB = GP == 4 ? 2 : 4;
   // (Q itself lies in shared memory, a lane's B operand [group][b0, b1 of both k-steps] at q + 512 group + 16 lane.)
-  // (and at q + 512 NG + 16 lane its B operand of the offsets -8 sum(q), in three terms, and the logit per sum of its columns)
+  // (behind it, for each c4: at 64 p the offsets -8 sum(q) of its columns in groups 2p and 2p + 1, at 64 NG / 2 their logits per sum)
+  static constexpr int kOffsets = 512 * NG, kPerSum = 64 * (NG / 2), kQBytes = kOffsets + kPerSum + 64;
   float m[2];                           // largest logit so far (log2 units)
   uint64_t nm;                          // 14 - m, 0 before the first key
   uint64_t l;
@@ -277,7 +286,7 @@ struct Q4State {
     const float mul = __uint_as_float(up << 23);
     // 2^17: codes count as n 2^-17
     const float per_sum = e == 255u ? __uint_as_float(0x7FC00000u) : fminf(c * 131072.f * __uint_as_float((254u - up) << 23), 3.4e38f);
-    __half off[NG][3];
+    float off[2][2];
 #pragma unroll
     for (int g = 0; g < NG; ++g) {
       const uint32_t w[4] = {v[g].x, v[g].y, v[g].z, v[g].w};
@@ -298,45 +307,25 @@ struct Q4State {
       sum += __shfl_xor_sync(0xffffffffu, sum, 1);  // column r8's sum over the group
       sum += __shfl_xor_sync(0xffffffffu, sum, 2);
       sum *= -8.f / 131072.f;
-#pragma unroll
-      for (int t = 0; t < 3; ++t) {
-        off[g][t] = __float2half_rn(sum);
-        sum -= __half2float(off[g][t]);
-      }
+      off[g & 1][0] = __shfl_sync(0xffffffffu, sum, 8 * c4);
+      off[g & 1][1] = __shfl_sync(0xffffffffu, sum, 8 * c4 + 4);
+      if ((g & 1) && r8 == 0)
+        *reinterpret_cast<float4*>(q_smem + kOffsets + 64 * (g / 2) + 16 * c4) = make_float4(off[0][0], off[0][1], off[1][0], off[1][1]);
     }
-    // k of the offsets' product: groups 0 and 1 in the lower eight, term c4 in lane c4; groups 2 and 3 in the upper
-    uint32_t ob[2];
-#pragma unroll
-    for (int k = 0; k < 2; ++k) {
-      __half2 o = __half2half2(__ushort_as_half(0));
-#pragma unroll
-      for (int t = 0; t < 3; ++t)
-        if (c4 == t && 2 * k < NG) o = __halves2half2(off[(2 * k) % NG][t], off[(2 * k) % NG + 1][t]);
-      ob[k] = *reinterpret_cast<const uint32_t*>(&o);
-    }
-    *reinterpret_cast<uint4*>(q_smem + 512 * NG + 16 * lane) =
-        make_uint4(ob[0], ob[1], __float_as_uint(__shfl_sync(0xffffffffu, per_sum, 8 * c4)), __float_as_uint(__shfl_sync(0xffffffffu, per_sum, 8 * c4 + 4)));
+    const float2 ps = make_float2(__shfl_sync(0xffffffffu, per_sum, 8 * c4), __shfl_sync(0xffffffffu, per_sum, 8 * c4 + 4));
+    if (r8 == 0) *reinterpret_cast<float2*>(q_smem + kOffsets + kPerSum + 16 * c4) = ps;
   }
 
   // The logits (log2 units) of keys r8 + 8 i of the 32 whose codes this lane's ldmatrix address is `codes` in, their scales at
   // `scales` (key r8).
-  __device__ __forceinline__ void logits(uint64_t (&s)[4], uint32_t codes, uint32_t scales, uint32_t q) {
-    uint32_t sk[4][D / 64], of[4];
-    q4_lds<16>(of, q + 512 * NG);
+  __device__ __forceinline__ void logits(uint64_t (&s)[4], uint32_t codes, uint32_t scales, uint32_t q, uint32_t offsets) {
+    uint32_t sk[4][D / 64], per_sum[2];
 #pragma unroll
     for (int i = 0; i < 4; ++i) q4_lds<D / 16>(sk[i], scales + 8 * i * (D / 16));
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      // the offsets of all groups in one product: scales (k = group, again for each term) times -8 sum(q)
-      const uint32_t a[4] = {sk[2 * h][0], sk[2 * h + 1][0], sk[2 * h][D / 64 - 1], sk[2 * h + 1][D / 64 - 1]};
-      float d[4];
-      mma_f16_zero(d, a, of[0], of[1]);
-      s[2 * h] = f2_pack(d[0], d[1]);
-      s[2 * h + 1] = f2_pack(d[2], d[3]);
-    }
-#pragma unroll
     for (int p = 0; p < NG / 2; ++p) {
-      uint32_t qb[2][4];
+      uint32_t qb[2][4], of[4];
+      q4_lds<16>(of, offsets + 64 * p);
       q4_lds<16>(qb[0], q + 1024 * p);
       q4_lds<16>(qb[1], q + 1024 * p + 512);
 #pragma unroll
@@ -349,19 +338,21 @@ struct Q4State {
           const uint32_t a[4] = {l0 & 0x00780078u, l1 & 0x00780078u, l0 & 0x07800780u, l1 & 0x07800780u};
           const uint32_t b[4] = {r0 & 0x00780078u, r1 & 0x00780078u, r0 & 0x07800780u, r1 & 0x07800780u};
           float d[4];
-          mma_f16_zero(d, a, qb[v][0], qb[v][1]);
+          mma_f16_from(d, a, qb[v][0], qb[v][1], of[2 * v], of[2 * v + 1]);
           mma_f16(d, b, qb[v][2], qb[v][3]);
 #pragma unroll
           for (int k = 0; k < 2; ++k) {
             const __half2 sc = *reinterpret_cast<const __half2*>(&sk[2 * h + k][p]);
             const float sf = v ? __high2float(sc) : __low2float(sc);
-            s[2 * h + k] = f2_fma(f2_pack(d[2 * k], d[2 * k + 1]), f2_pack(sf, sf), s[2 * h + k]);
+            const uint64_t d2 = f2_pack(d[2 * k], d[2 * k + 1]), sf2 = f2_pack(sf, sf);
+            s[2 * h + k] = p == 0 && v == 0 ? f2_mul(d2, sf2) : f2_fma(d2, sf2, s[2 * h + k]);
           }
         }
       }
     }
+    q4_lds<8>(per_sum, offsets + kPerSum);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) s[i] = f2_mul(s[i], f2_pack(__uint_as_float(of[2]), __uint_as_float(of[3])));
+    for (int i = 0; i < 4; ++i) s[i] = f2_mul(s[i], f2_pack(__uint_as_float(per_sum[0]), __uint_as_float(per_sum[1])));
   }
 
   uint32_t magic;                       // kQ4Magic
@@ -371,7 +362,7 @@ struct Q4State {
     using St = Q4Stage<D>;
     const int r8 = lane >> 2, c4 = lane & 3;
     uint64_t s[4];  // key r8 + 8 i, both columns
-    logits(s, stage + off, stage + St::kKs + r8 * St::kScaleRow, q);
+    logits(s, stage + off, stage + St::kKs + r8 * St::kScaleRow, q, q + kOffsets - 64 * r8);
     if (kb + kQ4Block > n) {
 #pragma unroll
       for (int i = 0; i < 4; ++i)
@@ -543,7 +534,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   const int W = a.whole ? a.whole : sp.W, rank = warp & (W - 1);
   const int group = W == 1 ? blockIdx.x * kQ4DecWarps + warp : blockIdx.x;
   float* s_vals = reinterpret_cast<float*>(q4_smem + kQ4DecWarps * kQ4Stages * St::kBytes);
-  uint8_t* s_q = reinterpret_cast<uint8_t*>(s_vals + kQ4DecWarps * GP * D) + warp * (State::NG + 1) * 512;
+  uint8_t* s_q = reinterpret_cast<uint8_t*>(s_vals + kQ4DecWarps * GP * D) + warp * State::kQBytes;
   const uint32_t ring = smem_u32(q4_smem + warp * kQ4Stages * St::kBytes), q_at = smem_u32(s_q) + 16 * lane;
 
   // the range and its first pair
@@ -887,7 +878,7 @@ static cudaError_t q4_decode_launch(const Q4DecodeArgs& a, cudaStream_t stream) 
       a.n_dev && a.n_stride && a.n_layers > 1 ? q4_decode_kernel<D, GP, true> : q4_decode_kernel<D, GP, false>;
   // (at least what lets no more than kQ4DecCtasPerSm on an SM: a fourth where registers allow one leaves other SMs without,
   // d = 64: 41 -> 51 us)
-  const int smem = std::max(kQ4DecMinSmem, kQ4DecWarps * (kQ4Stages * Q4Stage<D>::kBytes + GP * D * (int)sizeof(float) + (D / 32 + 1) * 512));
+  const int smem = std::max(kQ4DecMinSmem, kQ4DecWarps * (kQ4Stages * Q4Stage<D>::kBytes + GP * D * (int)sizeof(float) + Q4State<D, GP>::kQBytes));
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), smem);
   const int pairs = a.n_layers * a.Hkv;
   if (e == cudaSuccess) e = launch_kernel(kern, dim3(a.n_groups), dim3(kQ4DecThreads), smem, stream, a, true);

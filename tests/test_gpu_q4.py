@@ -616,6 +616,78 @@ def test_decode_keys_of_any_magnitude(B, magnitude):
     _check(out, q, K, V, 300, "")
 
 
+def _weights_bound(q, K, V, e):
+    """_decode_bound's, of logits that are off by e[head] at most."""
+    G, out = q.shape[0] // K.shape[0], np.zeros((q.shape[0], K.shape[2]))
+    for g in range(q.shape[0]):
+        x = K[g // G] @ O.bf16_to_f64(q[g]) / math.sqrt(q.shape[1])
+        p, v = np.exp(x - x.max()), np.abs(V[g // G])
+        out[g] = (p / p.sum()) @ v * 2 * (e[g] + 2.0 ** -20 + (len(v) / 16 + 64) * 2.0 ** -24) + 2.0 ** -38 * v.sum(0)
+    return out
+
+
+@pytest.mark.parametrize("G,d", [(4, 128), (6, 128), (2, 64), (8, 64)])
+def test_decode_groups_do_not_round_against_each_other(B, G, d):
+    """A group whose one large channel meets a zero of the query adds nothing to a logit, however large 8 s sum(q) of it is.
+
+    The queries are whole numbers up to 15, so a group's sums are exact: the codes' products and -8 sum(q) are multiples of
+    2^-10 where the largest query element is brought to [2^10, 2^11) and codes count as n 2^-17, and no operand product or sum
+    reaches 2^3, so that 22 bits below the largest hold them all.  What is left is fp32's: a rounding for each group of a sum
+    no larger than the groups' sizes together, and two of the factor; less than 2^-20 in all."""
+    import torch
+    rng = np.random.default_rng(G)
+    Hkv, n = 2, 300
+    k = rng.standard_normal((Hkv, n, d))
+    k[..., :32] = 0
+    k[..., 0] = rng.choice([-1, 1], (Hkv, n)) * rng.uniform(5000, 7000, (Hkv, n))
+    qf = rng.integers(-3, 4, (Hkv * G, d)).astype(np.float32)
+    qf[:, 0], qf[:, 1:32] = 0, 15
+    K, V, q = wl.f32_to_bf16_bits(k.astype(np.float32)), _bits(rng, (Hkv, n, d)), wl.f32_to_bf16_bits(qf)
+    out = B.stepkv_q4_decode([TL.bf16_dev(q)], _filled(B, [K], [V]), n)[0].cpu().numpy().astype(np.float64)
+    Kv, Vv = _values(K), _values(V)
+    groups = np.abs((Kv[:, None] * qf.reshape(Hkv, G, 1, d)).reshape(Hkv, G, n, -1, 32).sum(-1)).sum(-1).max(-1).reshape(-1)
+    e = 6 * 2.0 ** -24 * groups / math.sqrt(d)
+    err, bound = np.abs(out - O.q4_decode_attention(q, Kv, Vv)), _weights_bound(q, Kv, Vv, e)
+    assert (err <= bound).all(), f"off by {(err / bound).max():.3g} times the bound"
+
+
+@pytest.mark.parametrize("G,d", [(4, 128), (5, 128), (8, 64)])
+def test_decode_one_signed_queries_and_sparse_keys(B, G, d):
+    """Queries of one sign over keys with one channel a group: a group's sum of n q and its -8 sum(q) nearly cancel.  Each of the
+    two and what is left is known to 22 bits of |s| 8 sum|q| (the codes that are not 8 are single), so that a logit is off by
+    3 2^-22 of the sum of these over the groups at most, which is what the header states."""
+    import torch
+    rng = np.random.default_rng(d + G)
+    Hkv, n = 2, 700
+    k = np.zeros((Hkv, n, d // 32, 32))
+    np.put_along_axis(k, rng.integers(0, 32, (Hkv, n, d // 32, 1)), rng.standard_normal((Hkv, n, d // 32, 1)) * 8, -1)
+    qf = np.abs(rng.standard_normal((Hkv * G, d))) + 0.1
+    K, V, q = wl.f32_to_bf16_bits(k.reshape(Hkv, n, d).astype(np.float32)), _bits(rng, (Hkv, n, d)), wl.f32_to_bf16_bits(qf.astype(np.float32))
+    out = B.stepkv_q4_decode([TL.bf16_dev(q)], _filled(B, [K], [V]), n)[0].cpu().numpy().astype(np.float64)
+    Kv, Vv = _values(K), _values(V)
+    top = np.abs(Kv).reshape(Hkv, 1, n, -1, 32).max(-1)  # 8 |s|
+    e = 3 * 2.0 ** -22 * (top * O.bf16_to_f64(q).reshape(Hkv, G, 1, -1, 32).sum(-1)).sum(-1).max(-1).reshape(-1) / math.sqrt(d)
+    err, bound = np.abs(out - O.q4_decode_attention(q, Kv, Vv)), _weights_bound(q, Kv, Vv, e)
+    assert (err <= bound).all(), f"off by {(err / bound).max():.3g} times the bound"
+
+
+@pytest.mark.parametrize("magnitude", [2.0 ** -14, 2.0 ** -19])
+def test_decode_keys_with_subnormal_scales(B, magnitude):
+    """The scale multiplies a group's fp32 sum, so that fp16's smallest scales (exact, if of fewer bits) cost a logit nothing:
+    the bound above."""
+    import torch
+    rng = np.random.default_rng(10)
+    Hkv, G, d, n = 2, 4, 128, 300
+    K, V, q = _bits(rng, (Hkv, n, d), magnitude), _bits(rng, (Hkv, n, d)), _bits(rng, (Hkv * G, d), 1 / magnitude)
+    out = B.stepkv_q4_decode([TL.bf16_dev(q)], _filled(B, [K], [V]), n)[0].cpu().numpy().astype(np.float64)
+    Kv, Vv = _values(K), _values(V)
+    assert (np.abs(Kv[Kv != 0]).min() < 2.0 ** -14) and (np.abs(Kv).max() > 0)
+    top = np.abs(Kv).reshape(Hkv, 1, n, -1, 32).max(-1)
+    e = 3 * 2.0 ** -22 * (top * np.abs(O.bf16_to_f64(q)).reshape(Hkv, G, 1, -1, 32).sum(-1)).sum(-1).max(-1).reshape(-1) / math.sqrt(d)
+    err, bound = np.abs(out - O.q4_decode_attention(q, Kv, Vv)), _weights_bound(q, Kv, Vv, e)
+    assert (err <= bound).all(), f"off by {(err / bound).max():.3g} times the bound"
+
+
 def test_offsets_past_32_bits(B):
     """68 million rows of one head: 4.4 GB of codes.  All but the last 40 are zero keys and values, so the output is known; the
     last rows are written, read back, moved and attended where offsets need more than 32 bits."""
