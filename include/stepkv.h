@@ -458,7 +458,8 @@ STEPKV_API stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_
  *              sets STEPKV_ENOSPACE and n_cap rows are used; a negative one sets STEPKV_EDATA, the output is zero.
  *  n_cap       at most rows; the workspace and the split of the work go by it.
  *  out[l]      host array of device pointers, [Hq][d] fp32, 16-byte aligned; outputs that overlap are refused (STEPKV_EINVAL).
- *  ws          scratch of stepkv_q4_decode_workspace_size bytes (256-byte aligned): partial states.
+ *  ws          scratch of stepkv_q4_decode_workspace_size bytes (256-byte aligned): partial states.  The size is 0 for
+ *              shapes that the decode does not support.
  *  Rows at or past the count are not used, whatever they hold.  A key or a query with a NaN or an infinity makes the
  *  outputs of its heads NaN; a value row that reads back as NaN makes those channels NaN.
  *  Supported: d in {64, 128}; Hq a multiple of Hkv with at most 8 query heads per KV head.

@@ -532,8 +532,16 @@ stepkv_status_t stepkv_q4_compact(const stepkv_q4_cache_t* in, int32_t T, const 
                         static_cast<cudaStream_t>(stream));
 }
 
+// The blocks of a launch are counted in 32 bits.
+static bool q4_decode_fits(int n_layers, int Hkv, int n_cap) {
+  return (int64_t)std::min(n_layers, kQ4Layers) * Hkv * ((int64_t)n_cap / 32 + 1) < ((int64_t)1 << 30);
+}
+
 size_t stepkv_q4_decode_workspace_size(int32_t n_layers, int32_t Hkv, int32_t Hq, int32_t d, int32_t n_cap) {
-  if (n_layers < 1 || Hkv < 1 || Hq < Hkv || n_cap < 1 || (d != 64 && d != 128)) return 0;
+  // (0 for what stepkv_q4_decode refuses)
+  if (n_layers < 1 || Hkv < 1 || Hkv > 65535 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 8 || n_cap < 1 || n_cap > kQ4MaxRows || (d != 64 && d != 128))
+    return 0;
+  if (!q4_decode_fits(n_layers, Hkv, n_cap)) return 0;
   return q4_decode_ws_bytes(std::min(n_layers, kQ4Layers), Hkv, Hq, d, n_cap);
 }
 
@@ -545,9 +553,7 @@ stepkv_status_t stepkv_q4_decode(const stepkv_q4_cache_t* cache, const void* con
   if (!q || !out || !ws || Hq < 1 || Hq % cache->Hkv != 0 || n_cap < 1 || n_cap > cache->rows) return STEPKV_EINVAL;
   if (cache->d != 64 && cache->d != 128) return STEPKV_EUNSUPPORTED;
   if (Hq / cache->Hkv > 8) return STEPKV_EUNSUPPORTED;
-  // the blocks of a launch are counted in 32 bits
-  if ((int64_t)std::min(cache->n_layers, kQ4Layers) * cache->Hkv * ((int64_t)n_cap / 32 + 1) >= ((int64_t)1 << 30))
-    return STEPKV_EUNSUPPORTED;
+  if (!q4_decode_fits(cache->n_layers, cache->Hkv, n_cap)) return STEPKV_EUNSUPPORTED;
   if (n_dev ? (n_dev_stride != 0 && n_dev_stride != 1) : (n_host < 0 || n_host > n_cap)) return STEPKV_EINVAL;
   if (ws_bytes < stepkv_q4_decode_workspace_size(cache->n_layers, cache->Hkv, Hq, cache->d, n_cap)) return STEPKV_ENOSPACE;
   if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return STEPKV_EINVAL;

@@ -856,7 +856,7 @@ __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q4_merge_kernel(const
 
 // A pair of n rows leaves at most one slot per block, and all pairs together at most one per group and pair.
 size_t q4_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap) {
-  const int64_t pairs = (int64_t)n_layers * Hkv, blocks = pairs * ((n_cap + kQ4Block - 1) / kQ4Block);
+  const int64_t pairs = (int64_t)n_layers * Hkv, blocks = pairs * (((int64_t)n_cap + kQ4Block - 1) / kQ4Block);
   return (size_t)(std::min<int64_t>(kQ4MaxGroups, blocks) + pairs) * (Hq / Hkv) * (d + 4) * sizeof(float);
 }
 

@@ -238,6 +238,21 @@ def test_workspace_size(lib):
     assert size(1, 8, 32, 128, 0) == 0 and size(200, 8, 32, 128, 8272) == size(64, 8, 32, 128, 8272)  # 64 layers a launch
 
 
+@pytest.mark.parametrize("shape", [
+    (1, 8, 32, 128, 2 ** 31 - 1), (1, 8, 32, 128, 2 ** 31 - 32), (1, 8, 32, 128, 2 ** 30 + 1), (1, 1, 1, 64, -1),  # capacities
+    (1, 8, 33, 128, 100), (1, 8, 72, 128, 100), (1, 3, 8, 64, 100), (1, 65536, 65536, 64, 10),                 # heads
+    (64, 65535, 65535, 64, 2 ** 20)])                                                                       # blocks of a launch
+def test_workspace_size_of_what_is_refused(lib, shape):
+    """0 for what the decode does not take, and no count wraps."""
+    assert lib.stepkv_q4_decode_workspace_size(*shape) == 0
+
+
+def test_workspace_size_of_the_largest_caches(lib):
+    """A partial state is d + 4 floats for each head, group of warps (4096 at most) and pair."""
+    assert lib.stepkv_q4_decode_workspace_size(1, 1, 8, 128, 2 ** 30) == (4096 + 1) * 8 * 132 * 4
+    assert lib.stepkv_q4_decode_workspace_size(1, 2, 2, 64, 32) == 4 * 68 * 4
+
+
 def test_header_declares_and_library_exports(lib):
     from paper_2609_22158_gb300 import binding as B
     from test_cpu_abi import HEADER
