@@ -479,7 +479,7 @@ stepkv_status_t stepkv_q4_write(const stepkv_q4_cache_t* cache, const void* cons
   if (st != STEPKV_OK) return st;
   if (!idx && n > T) return STEPKV_EINVAL;
   if (!row0_dev && !n_dev && (row0 < 0 || (int64_t)row0 + n > cache->rows)) return STEPKV_ENOSPACE;
-  if (n == 0) return STEPKV_OK;
+  if (n == 0 && !n_dev) return STEPKV_OK;  // (a device count above a limit of 0 is told like any other)
   Footprints f;  // no two of the cache's tensors may share a row
   add_q4_rows(f, *cache, cache->rows, true);
   if (f.clash()) return STEPKV_EINVAL;
@@ -498,11 +498,13 @@ stepkv_status_t stepkv_q4_read(const stepkv_q4_cache_t* cache, const int32_t* id
   if (st != STEPKV_OK) return st;
   if ((head_stride < cache->d && cache->Hkv > 1) || (row_stride < cache->d && n > 1)) return STEPKV_EINVAL;  // rows apart
   if (!idx && !row0_dev && !n_dev && (row0 < 0 || (int64_t)row0 + n > cache->rows)) return STEPKV_EINVAL;
-  if (n == 0) return STEPKV_OK;
+  if (n == 0 && !n_dev) return STEPKV_OK;  // (a device count above a limit of 0 is told like any other)
   Footprints f;
-  const Footprint rows = make_footprint(cache->Hkv, 2 * head_stride, n, 2 * row_stride, 2 * (int64_t)cache->d);
-  f.add(K, cache->n_layers, rows, true);
-  f.add(V, cache->n_layers, rows, true);
+  if (n > 0) {
+    const Footprint rows = make_footprint(cache->Hkv, 2 * head_stride, n, 2 * row_stride, 2 * (int64_t)cache->d);
+    f.add(K, cache->n_layers, rows, true);
+    f.add(V, cache->n_layers, rows, true);
+  }
   if (f.clash()) return STEPKV_EINVAL;
   return q4_read_run(*cache, r, K, V, head_stride, row_stride, dev_status, static_cast<cudaStream_t>(stream));
 }

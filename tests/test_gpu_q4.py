@@ -321,6 +321,26 @@ def test_empty_writes_and_reads(B):
     assert torch.equal(cache.K, was[0]) and torch.equal(cache.V, was[2])
 
 
+def test_device_counts_over_no_rows(B):
+    """A limit of no rows, as an empty index list or an empty block of tokens has it: a count of 0 on the device does nothing, any
+    other is told."""
+    import torch
+    cache = B.Q4Cache.allocate(2, 2, 10, 64)
+    X, idx = torch.zeros((2, 2, 5, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros(0, dtype=torch.int32, device="cuda")
+    out = torch.zeros((2, 2, 0, 64), dtype=torch.bfloat16, device="cuda")
+    for n, want in ((0, 0), (3, B.STEPKV_ENOSPACE), (-1, B.STEPKV_EDATA)):
+        count = torch.tensor([n], dtype=torch.int32, device="cuda")
+        for call in (lambda st: B.stepkv_q4_write(cache, X, X, 0, n=count, idx=idx, status=st),
+                     lambda st: B.stepkv_q4_write(cache, X[:, :, :0], X[:, :, :0], 4, n=count, status=st),
+                     lambda st: B.stepkv_q4_read(cache, 0, count, K=out, status=st),
+                     lambda st: B.stepkv_q4_read(cache, idx=idx, n=count, status=st)):
+            st = B.new_status()
+            call(st)
+            torch.cuda.synchronize()
+            assert st.item() == want
+    assert not cache.K.any() and not cache.V.any()
+
+
 def test_read_by_index_of_values_alone(B):
     import torch
     rng = np.random.default_rng(8)
