@@ -820,6 +820,13 @@ def _int32_vector(t, name, dev, least=1):
     return t
 
 
+def _int32(v, name):
+    """v, if the C call can take it (ctypes would cut off the bits above 32)."""
+    if not -2 ** 31 <= v < 2 ** 31:
+        raise ValueError(f"{name} = {v} does not fit 32 bits")
+    return v
+
+
 def _made_on(stream):
     """What a call allocates or zeroes belongs to the stream it runs on."""
     return contextlib.nullcontext() if stream is None else _torch().cuda.stream(stream)
@@ -860,6 +867,8 @@ class Q4Cache:
                 raise ValueError(f"{name} rows must be dense")
             if self.Hkv > 1 and p.strides[0] != like.strides[0]:
                 raise ValueError(f"{name} must share the head stride of {'K' if t == torch.uint8 else 'K_scale'}")
+        for x, name in ((self.n_layers, "layers"), (self.Hkv, "Hkv"), (self.rows, "rows"), (self.d, "d")):
+            _int32(x, name)
         stride = [p.strides[0] if self.Hkv > 1 else self.rows * p.shape[2] for p in (codes, scales)]
         self._ptrs = [array.array("Q", p.ptrs) for p in self._parts]
         args = [p.buffer_info()[0] for p in self._ptrs] + [None, None]
@@ -887,6 +896,7 @@ def _q4_rows(cache, row0, n, limit):
     """(n_dev, n, row0_dev, stride, row0) as the C calls take them, device vectors as tensors (the caller holds them until
     the launch: freed earlier, their memory would go to its next allocation); n None: the limit."""
     n_dev = row0_dev = None
+    _int32(limit, "rows")
     if n is None:
         n = limit
     elif not isinstance(n, int):
@@ -894,7 +904,9 @@ def _q4_rows(cache, row0, n, limit):
     elif not 0 <= n <= limit:
         raise ValueError(f"n = {n} rows, at most {limit} here")
     stride = 0
-    if not isinstance(row0, int):
+    if isinstance(row0, int):
+        _int32(row0, "row0")
+    else:
         row0_dev, row0 = _int32_vector(row0, "row0", cache.device), 0
         if row0_dev.numel() not in (1, cache.n_layers):
             raise ValueError("row0 must hold one row, or one for each layer")
@@ -971,6 +983,7 @@ def stepkv_q4_compact(cache: Q4Cache, T: int, kept_idx, n_kept, kept_cap: int, o
     status word."""
     lib = load_library()
     dev = cache.device
+    _int32(T, "T"), _int32(kept_cap, "kept_cap")
     _int32_vector(kept_idx, "kept_idx", dev, kept_cap)
     _int32_vector(n_kept, "n_kept", dev)
     for t, name, least in ((step_id_in, "step_id_in", T), (pos_in, "pos_in", T), (step_id_out, "step_id_out", kept_cap),
@@ -987,7 +1000,7 @@ def stepkv_q4_compact(cache: Q4Cache, T: int, kept_idx, n_kept, kept_cap: int, o
 def q4_decode_workspace(cache: Q4Cache, Hq: int):
     """A workspace for stepkv_q4_decode calls over this cache (one call at a time may use it)."""
     torch = _torch()
-    need = load_library().stepkv_q4_decode_workspace_size(cache.n_layers, cache.Hkv, Hq, cache.d, cache.rows)
+    need = load_library().stepkv_q4_decode_workspace_size(cache.n_layers, cache.Hkv, _int32(Hq, "Hq"), cache.d, cache.rows)
     return torch.empty(need + 512, dtype=torch.uint8, device=cache.device)
 
 
@@ -1011,7 +1024,9 @@ def stepkv_q4_decode(q, cache: Q4Cache, n, out=None, ws=None, status=None, strea
         if x.n != cache.n_layers or x.shape != qs.shape or x.strides != (cache.d, 1) or x.device != cache.device:
             raise ValueError(f"{name} must be contiguous [Hq, d] per layer, on the cache's device")
     n_dev, stride = None, 0
-    if not isinstance(n, int):
+    if isinstance(n, int):
+        _int32(n, "n")
+    else:
         n_dev, n = _int32_vector(n, "n", cache.device), 0
         if n_dev.numel() not in (1, cache.n_layers):
             raise ValueError("n must hold one count, or one for each layer")

@@ -1186,3 +1186,23 @@ def test_binding_refusals(B):
         with pytest.raises(B.StepKVError):
             f()
     torch.cuda.synchronize()
+
+
+def test_numbers_past_32_bits_are_refused(B):
+    """Not cut to their lower 32 bits, which would name another row or count."""
+    import torch
+    cache, other = B.Q4Cache.allocate(1, 1, 20, 64), B.Q4Cache.allocate(1, 1, 20, 64)
+    X, i32 = torch.ones((1, 1, 2, 64), dtype=torch.bfloat16, device="cuda"), torch.zeros(20, dtype=torch.int32, device="cuda")
+    q = torch.zeros((1, 4, 64), dtype=torch.bfloat16, device="cuda")
+    many = torch.empty((1, 1, 1, 64), dtype=torch.bfloat16, device="cuda").expand(-1, -1, 2 ** 32 + 2, -1)
+    for call in (lambda: B.stepkv_q4_write(cache, X, X, 2 ** 32), lambda: B.stepkv_q4_write(cache, X, X, -2 ** 32 + 3),
+                 lambda: B.stepkv_q4_write(cache, many, many, 0), lambda: B.stepkv_q4_write(cache, many, many, 0, n=2),
+                 lambda: B.stepkv_q4_read(cache, 2 ** 32, 2, K=X), lambda: B.stepkv_q4_decode(q, cache, 2 ** 32 + 5),
+                 lambda: B.stepkv_q4_decode(q, cache, 2 ** 32), lambda: B.q4_decode_workspace(cache, 2 ** 32 + 4),
+                 lambda: B.stepkv_q4_compact(cache, 2 ** 32 + 20, i32, i32[:1], 20, other),
+                 lambda: B.stepkv_q4_compact(cache, 20, i32, i32[:1], 20 - 2 ** 32, other),
+                 lambda: B.Q4Cache(cache.K.expand(-1, 2 ** 32 + 1, -1, -1), cache.K_scale.expand(-1, 2 ** 32 + 1, -1, -1))):
+        with pytest.raises(ValueError):
+            call()
+    torch.cuda.synchronize()
+    assert not cache.K.any() and not other.K.any()
