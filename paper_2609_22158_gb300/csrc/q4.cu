@@ -88,8 +88,9 @@ __device__ __forceinline__ __half q4_scale(float x) {
 
 // The codes of 8 channels (four bf16 pairs) as one word, channel i in bits 4i .. 4i + 3; inv: 1 / s (0 where s is 0).
 // rint(x / s) with the exact quotient's ties: x has 8 bits and s 5, so a quotient near a tie k + 1/2 (k < 8) is the tie or
-// at least 2^-8.95 from it, and x inv is off by 2^-19 at most.  Added to 6144 it is rounded to multiples of 2^-11, a tie to
-// itself and nothing else to a tie; the next sum rounds that to an integer, ties to even, which lies in the low bits.
+// at least 2^-9 from it (1/2 - 255 2^-5 / 16), and x inv is off by 2^-19 at most.  Added to 6144 it is rounded to multiples
+// of 2^-11, a tie to itself and nothing else to a tie; the next sum rounds that to an integer, ties to even, which lies in
+// the low bits.
 // LOW: quotients below -8 can occur (a saturated scale, or one on fp16's last steps).
 template <bool LOW>
 __device__ __forceinline__ uint32_t q4_codes(const uint32_t (&v)[4], float inv) {

@@ -4,8 +4,9 @@
 //
 // A row pair is 144 bytes at d = 128 where bf16 takes 512, so at the copy rate a scheduler has 24 cycles per row pair and
 // turning codes into operands has to cost next to nothing.  Both contractions run on the tensor cores (mma.sync: a KV
-// head's G <= 8 query heads are the 8 columns of a tile, the rows of the cache its 16 rows; tcgen05 would want its
-// operands back in shared memory, 16 bits a code), a warp on 32 keys at a time:
+// head's G <= 8 query heads are the 8 columns of a tile, the rows of the cache its 16 rows; tcgen05 takes none
+// from registers: the unpacked codes would go through shared or tensor memory first, 16 bits a code, for tiles of which the few
+// heads fill an eighth or less), a warp on 32 keys at a time:
 //   S^T = K Q^T.  A half whose bits 7-10 hold a code n, and nothing else, is the fp16 number n 2^-17 (its subnormals and
 //     first binade run on linearly), with the code in bits 3-6 n 2^-21: two shifts and four masks turn a word of eight codes
 //     into operands.  (Lower still the tensor core loses bits: it does not normalise subnormals.  e4m3 operands, 0000nnnn =
@@ -26,6 +27,9 @@
 // 5: 67.7, where the reads take 45 and the scalar kernel took 995.  12 warps of 168 registers on an SM; 16 warps of 128 took
 // 66.0 (more moves), 8 of 255 72.4; three ring stages 66.0; a barrier that keeps the SM's warps in step 64-70 (they finish
 // between 45 and 60 us without, at the same rate in all); scales laid out in shared memory for their users 67.0.
+// (Times here and below: a call of a captured graph of ten equal ones.  Caches under some 100 MB, as those of one layer, short
+// lists or ragged batches are, then come out of L2; a chain of 32 layers, one call each from DRAM, takes 10.5 us a layer where
+// the captured loop of one layer takes 10.1.)
 //
 // Each warp copies its blocks of 32 rows into a ring of its own with cp.async.  A group of warps takes a pair (q4_whole) or a
 // range of the list of all pairs' blocks (q4_split); its warps interleave the blocks of a pair, join their states in shared
