@@ -478,6 +478,123 @@ STEPKV_API stepkv_status_t stepkv_q4_decode(const stepkv_q4_cache_t* cache, cons
                                  float* const* out, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
 
 /* ---------------------------------------------------------------------------------------------
+ * A cache held in 8 bits: e4m3 codes, with one scale for each block of STEPKV_Q8_BLOCK rows (tokens) of a KV head.  Half the
+ * bytes of bf16.  A value is off by at most 2^-4 of itself, and channels much larger than the others take nothing from them
+ * (e4m3 keeps its 4 significant bits down to 2^-14 of the block's largest value).
+ *
+ * Format.  A block's scale is s = 2^k with k the smallest integer for which every finite value of the rows written to it has
+ * |x| <= 448 s, at least -100 and at most 119; a value's code is e4m3(x / s), ties to even; NaN and infinities get the code of
+ * NaN; magnitudes above 448 2^119 saturate; a block of zeros has s = 2^-100.  A code stands for code * s, which bf16 holds
+ * exactly: reading back does not round, and attention over the cache is attention over the rows read back.
+ * Rows are appended.  Where the first row written does not begin a block, the block's rows before it stay: its scale becomes
+ * the larger of what it was and what the new rows need, and the codes that stay become e4m3(code s_old / s_new), which is exact
+ * unless they fall below 2^-6 of the new scale.
+ *
+ * Layout, per layer and for keys and values alike:
+ *   codes   [Hkv][rows][d] e4m3 (1 sign, 4 exponent, 3 mantissa bits, no infinities; 0x7F and 0xFF are NaN)
+ *   scales  [Hkv][ceil(rows / 32)] float32: row r of a head has scale r / 32
+ * Codes: bases 16-byte aligned, code_head_stride (bytes) a multiple of 16.  Scales: bases 4-byte aligned.
+ * d is 64 or 128.  At most 2^30 rows.
+ */
+#define STEPKV_Q8_BLOCK 32
+typedef struct {
+  int32_t n_layers, Hkv, d;
+  int32_t rows;                /* capacity of a head, rows */
+  void* const* K;              /* host [n_layers]: codes of the keys */
+  float* const* K_scale;       /* host [n_layers] */
+  void* const* V;              /* host [n_layers] */
+  float* const* V_scale;       /* host [n_layers] */
+  int64_t code_head_stride;    /* bytes between KV heads of codes (>= rows * d) */
+  int64_t scale_head_stride;   /* floats between KV heads of scales (>= ceil(rows / 32)) */
+} stepkv_q8_cache_t;
+
+/* Quantises rows as they are appended: for every layer l, KV head h and r < n,
+ *   row row0 + r of the cache = the codes of K[l][h][idx ? idx[r] : r][:]   (V alike).
+ * The heads of the layers written end with these rows: what stood at or behind row row0 no longer counts (a block's rows behind
+ * the last one written keep their bytes, but not what they stood for), so appending a token is n = 1 with row0 the rows
+ * so far, and row0 = 0 starts anew.  Rows before row0 stay (see the format for what a block's scale does to them).
+ *  K, V, head_stride, row_stride, T, idx, n, n_dev, row0, row0_dev, row0_dev_stride: as in stepkv_q4_write; both K and V
+ *  are given.  An index outside [0, T) sets STEPKV_EDATA and its row reads back as 0.  A bad count or row0 as there.
+ * The cache's codes and scales share no memory with one another, in any layer, nor with K and V (STEPKV_EINVAL).
+ */
+STEPKV_API stepkv_status_t stepkv_q8_write(const stepkv_q8_cache_t* cache, const void* const* K, const void* const* V,
+                                int64_t head_stride, int64_t row_stride, int32_t T, const int32_t* idx,
+                                const int32_t* n_dev, int32_t n, const int32_t* row0_dev, int32_t row0_dev_stride,
+                                int32_t row0, int32_t* dev_status, void* stream);
+
+/* Reads rows back to bf16, exactly: arguments, results and errors as stepkv_q4_read.  Rows written do not share memory with one
+ * another nor with the cache (STEPKV_EINVAL).
+ */
+STEPKV_API stepkv_status_t stepkv_q8_read(const stepkv_q8_cache_t* cache, const int32_t* idx, const int32_t* n_dev, int32_t n,
+                               const int32_t* row0_dev, int32_t row0_dev_stride, int32_t row0, void* const* K,
+                               void* const* V, int64_t head_stride, int64_t row_stride, int32_t* dev_status,
+                               void* stream);
+
+/* Decode attention over a cache held in 8 bits: stepkv_decode's formula over the values the codes stand for, for n_layers
+ * caches (the layers of a trajectory, or the trajectories of a batch), each with its own count.
+ *  q, Hq, n_dev, n_dev_stride, n_host, n_cap, out, ws: as in stepkv_q4_decode (0 keys: the output is zero).
+ *  mass[l]     host array of device pointers, or NULL: [Hkv][mass_head_stride >= n_cap] float32, 4-byte aligned, read and
+ *              written: to every key's entry its softmax weight, averaged over the KV head's query heads, is added
+ *              (stepkv_decode_h2o's accumulated attention).  Entries at or past the count are left as they are.
+ *              Outputs and masses that overlap are refused (STEPKV_EINVAL).
+ *  ws          scratch of stepkv_q8_decode_workspace_size bytes (256-byte aligned); with_mass: 1 for calls with masses.
+ *              The size is 0 for shapes that the decode does not support.
+ *  Rows at or past the count are not used, whatever they hold.  A key or a query with a NaN or an infinity makes the
+ *  outputs of its heads NaN (and their keys' masses); a value that reads back as NaN makes its channel NaN.
+ *  Supported: d in {64, 128}; Hq a multiple of Hkv with at most 8 query heads per KV head.
+ *  Deterministic; out is the same with and without masses.  The last bits depend on the split of the work, which goes by
+ *  the counts, n_layers, Hkv, n_cap and the device's number of SMs.
+ */
+STEPKV_API size_t stepkv_q8_decode_workspace_size(int32_t n_layers, int32_t Hkv, int32_t Hq, int32_t d, int32_t n_cap,
+                                       int32_t with_mass);
+STEPKV_API stepkv_status_t stepkv_q8_decode(const stepkv_q8_cache_t* cache, const void* const* q, int32_t Hq,
+                                 const int32_t* n_dev, int32_t n_dev_stride, int32_t n_host, int32_t n_cap,
+                                 float* const* out, float* const* mass, int64_t mass_head_stride, void* ws,
+                                 size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
+ * Eviction by accumulated attention (H2O): every KV head of every layer keeps, by itself, `keep` of its n rows, in place.
+ * (stepkv_select and stepkv_compact choose one set of tokens for all heads at the end of a step; this is for a cache that is
+ * held at a budget while tokens are decoded, each head by the attention it has paid.)
+ *
+ * For a head with rows j < n, accumulated attention mass[j] and positions pos[j] of their tokens, n > keep:
+ *   protected(j)  = pos[j] < n_sink, or pos[j] > (largest pos) - n_recent
+ *   retained      = the first `keep` in the order: protected rows first, then mass descending (a NaN behind every number,
+ *                   -0 is 0); ties in either part: the lower slot first
+ *   moves         = the i-th slot below keep that is not retained receives the row of the i-th slot at or above keep that is
+ *                   (both ascending): K, V, mass and pos
+ * Then rows [0, keep) are the retained ones (those that were below keep stay where they are), mass[j] = 0 for keep <= j < n, so
+ * that new rows start with nothing, and the count is min(n, keep).  A head with n <= keep is left as it is.  Attention over
+ * the rows does not depend on their order; pos tells which token a row belongs to.
+ *
+ *  K[l], V[l]  host arrays of device pointers, [Hkv][rows >= n_cap][d] bf16, head stride kv_head_stride elements; d * 2 a multiple
+ *              of 16, d <= 256; bases 16-byte aligned, kv_head_stride % 8 == 0.
+ *  n           rows of layer l: n_dev[l * n_dev_stride] (device; stride 0: one for all, 1: one each) where n_dev is given, else
+ *              n_host (0 <= n_host <= n_cap).  A count above n_cap sets STEPKV_ENOSPACE, a negative one STEPKV_EDATA, and the
+ *              layer and its entry of n_out are left as they are.
+ *  keep        1 <= keep <= n_cap; n_sink, n_recent >= 0 with n_sink + n_recent <= keep.
+ *  mass[l]     host array of device pointers, [Hkv][mass_head_stride >= n_cap] float32, 4-byte aligned.
+ *  pos[l]      host array of device pointers, [Hkv][pos_head_stride >= n_cap] int32, 4-byte aligned.
+ *  n_out       device, laid out as n_dev (without it, or with stride 0: one value), or NULL: min(n, keep).  May be n_dev itself.
+ *  ws          scratch of stepkv_evict_workspace_size bytes (256-byte aligned); 0 for what is not supported.
+ *  Nothing that is written may share memory with another tensor of the call (STEPKV_EINVAL; n_out may be n_dev).
+ *  Supported: n_cap <= 262144, Hkv <= 65535.
+ *  stepkv_q8_evict: the same over a cache held in 8 bits (n_cap <= cache->rows).  The scale of a block that receives rows becomes
+ *  the larger of what it was and what those rows need; the codes of rows that stay in it become e4m3(code s_old / s_new), those
+ *  of rows received e4m3(code s_source / s_new).
+ */
+STEPKV_API size_t stepkv_evict_workspace_size(int32_t n_layers, int32_t Hkv, int32_t n_cap);
+STEPKV_API stepkv_status_t stepkv_evict(int32_t n_layers, void* const* K, void* const* V, int64_t kv_head_stride, int32_t Hkv,
+                             int32_t d, const int32_t* n_dev, int32_t n_dev_stride, int32_t n_host, int32_t n_cap,
+                             int32_t keep, int32_t n_sink, int32_t n_recent, float* const* mass, int64_t mass_head_stride,
+                             int32_t* const* pos, int64_t pos_head_stride, int32_t* n_out, void* ws, size_t ws_bytes,
+                             int32_t* dev_status, void* stream);
+STEPKV_API stepkv_status_t stepkv_q8_evict(const stepkv_q8_cache_t* cache, const int32_t* n_dev, int32_t n_dev_stride,
+                                int32_t n_host, int32_t n_cap, int32_t keep, int32_t n_sink, int32_t n_recent,
+                                float* const* mass, int64_t mass_head_stride, int32_t* const* pos, int64_t pos_head_stride,
+                                int32_t* n_out, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream);
+
+/* ---------------------------------------------------------------------------------------------
  * Step signals from evidence cues (Sec. 4.1: observation validity, evidence gain, action redundancy of
  * Eq. 2 and the similarity that drives Eq. 3).  Every field of a step (0 Thought, 1 Action,
  * 2 Observation) is given as up to STEPKV_MAX_CUES evidence cues: distinct 32-bit ids in strictly

@@ -416,3 +416,114 @@ def q4_decode_attention(q: np.ndarray, K: np.ndarray, V: np.ndarray) -> np.ndarr
         e = np.exp(s - s.max())
         out[g] = (e / e.sum()) @ V[g // G]
     return out
+
+
+# --------------------------------------------------------------------------------------
+# A cache held in 8 bits (no counterpart in the paper): e4m3 codes, a scale 2^k for each head and block of 32 rows
+# --------------------------------------------------------------------------------------
+Q8_BLOCK = 32
+
+
+def e4m3_values(codes: np.ndarray) -> np.ndarray:
+    """float64 values of e4m3 codes (uint8: sign, 4 exponent, 3 mantissa bits; exponent bias 7; 0x7F and 0xFF are NaN)."""
+    c = np.asarray(codes, np.int64)
+    e, m = (c >> 3) & 15, c & 7
+    v = np.where(e == 0, m * 2.0 ** -9, (8 + m) * np.exp2(e - 10.0))
+    v = np.where((c & 127) == 127, np.nan, v)
+    return np.where(c >> 7 != 0, -v, v)
+
+
+def e4m3_round(y: np.ndarray) -> np.ndarray:
+    """The e4m3 value nearest to float64 y, ties to the even code, saturating at 448; NaN for what is not finite."""
+    y = np.asarray(y, np.float64)
+    a = np.where(np.isfinite(y), np.abs(y), 0.0)
+    step = np.exp2(np.maximum(np.floor(np.log2(np.maximum(a, 2.0 ** -30))), -6) - 3)
+    return np.where(np.isfinite(y), np.copysign(np.minimum(np.rint(a / step) * step, 448.0), y), np.nan)
+
+
+def q8_scale(most: float) -> float:
+    """2^k with k the smallest integer in [-100, 119] for which most <= 448 2^k (119 where there is none)."""
+    k = -100
+    while k < 119 and most > 448.0 * 2.0 ** k:
+        k += 1
+    return 2.0 ** k
+
+
+def q8_append(values: np.ndarray, scales: np.ndarray, X: np.ndarray, row0: int):
+    """Rows X [n, d] (bf16 bits, or float64 values) appended as rows row0 .. of one head, whose values [rows, d] and scales
+    [ceil(rows / 32)] (float64) are changed in place."""
+    x = bf16_to_f64(X) if np.asarray(X).dtype == np.uint16 else np.asarray(X, np.float64)
+    n = len(x)
+    at = row0
+    while at < row0 + n:
+        b = at // Q8_BLOCK
+        end = min((b + 1) * Q8_BLOCK, row0 + n)
+        rows = x[at - row0:end - row0]
+        finite = np.abs(rows[np.isfinite(rows)])
+        s = q8_scale(finite.max() if finite.size else 0.0)
+        if at > b * Q8_BLOCK:                       # rows of the block that stay
+            s = max(s, scales[b])
+            old = slice(b * Q8_BLOCK, at)
+            values[old] = e4m3_round(values[old] / s) * s
+        values[at:end] = e4m3_round(rows / s) * s
+        scales[b] = s
+        at = end
+
+
+def q8_quantise(X: np.ndarray):
+    """X [..., rows, d] bf16 bits written to an empty cache: (values, scales [..., blocks]) float64."""
+    flat = X.reshape(-1, *X.shape[-2:])
+    v = np.zeros(flat.shape)
+    s = np.zeros((len(flat), -(-X.shape[-2] // Q8_BLOCK)))
+    for i, x in enumerate(flat):
+        q8_append(v[i], s[i], x, 0)
+    return v.reshape(X.shape), s.reshape(*X.shape[:-2], -1)
+
+
+def attention_weights(q: np.ndarray, K: np.ndarray) -> np.ndarray:
+    """q [Hq, d] bf16 bits, K [Hkv, n, d] float64 -> softmax weights averaged over each KV head's query heads [Hkv, n]."""
+    qf = bf16_to_f64(q)
+    Hkv, n, d = K.shape
+    G = len(qf) // Hkv
+    w = np.zeros((Hkv, n))
+    for g in range(len(qf) if n else 0):
+        s = K[g // G] @ qf[g] / math.sqrt(d)
+        e = np.exp(s - s.max())
+        w[g // G] += e / e.sum() / G
+    return w
+
+
+# --------------------------------------------------------------------------------------
+# Eviction by accumulated attention (H2O): one head
+# --------------------------------------------------------------------------------------
+def evict_moves(mass: np.ndarray, pos: np.ndarray, keep: int, n_sink: int, n_recent: int):
+    """One head's n masses and positions -> (slots below keep that are filled, slots they are filled from), both ascending.
+    Retained are the first `keep` by: protected (pos < n_sink or pos > max(pos) - n_recent), mass descending (NaN last), slot."""
+    n = len(mass)
+    if n <= keep:
+        return [], []
+    newest = int(max(pos))
+
+    def rank(j):
+        if pos[j] < n_sink or int(pos[j]) > newest - n_recent:
+            return (0, 0.0, j)
+        return (2, 0.0, j) if math.isnan(mass[j]) else (1, -float(mass[j]), j)
+
+    kept = set(sorted(range(n), key=rank)[:keep])
+    return [j for j in range(keep) if j not in kept], [j for j in range(keep, n) if j in kept]
+
+
+def q8_evict(values: np.ndarray, scales: np.ndarray, to, start):
+    """The moves of evict_moves on one head held in 8 bits (values [rows, d], scales [blocks]): returns (values, scales)
+    after them.  Only rows below keep count afterwards."""
+    v, s = values.copy(), scales.copy()
+    for b in sorted({t // Q8_BLOCK for t in to}):
+        got = [(t, f) for t, f in zip(to, start) if t // Q8_BLOCK == b]
+        rows = np.array([values[f] for _, f in got])
+        finite = np.abs(rows[np.isfinite(rows)])
+        s[b] = max(scales[b], q8_scale(finite.max() if finite.size else 0.0))
+        block = slice(b * Q8_BLOCK, (b + 1) * Q8_BLOCK)
+        v[block] = e4m3_round(values[block] / s[b]) * s[b]
+        for t, f in got:
+            v[t] = e4m3_round(values[f] / s[b]) * s[b]
+    return v, s

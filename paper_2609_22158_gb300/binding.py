@@ -75,6 +75,12 @@ class CQ4Cache(ctypes.Structure):
                 ("code_head_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64)]
 
 
+class CQ8Cache(ctypes.Structure):
+    _fields_ = [("n_layers", ctypes.c_int32), ("Hkv", ctypes.c_int32), ("d", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("K", ctypes.c_void_p), ("K_scale", ctypes.c_void_p), ("V", ctypes.c_void_p), ("V_scale", ctypes.c_void_p),
+                ("code_head_stride", ctypes.c_int64), ("scale_head_stride", ctypes.c_int64)]
+
+
 STEPKV_MEM_DEVICE = 0
 STEPKV_MEM_HOST = 1
 
@@ -117,6 +123,17 @@ SIGNATURES = {
                                  _VP, _VP, _VP]),
     "stepkv_q4_decode_workspace_size": (_SZ, [_I32, _I32, _I32, _I32, _I32]),
     "stepkv_q4_decode": (_I32, [ctypes.POINTER(CQ4Cache), _VP, _I32, _VP, _I32, _I32, _I32, _VP, _VP, _SZ, _VP, _VP]),
+    "stepkv_q8_write": (_I32, [ctypes.POINTER(CQ8Cache), _VP, _VP, _I64, _I64, _I32, _VP, _VP, _I32, _VP, _I32, _I32, _VP,
+                               _VP]),
+    "stepkv_q8_read": (_I32, [ctypes.POINTER(CQ8Cache), _VP, _VP, _I32, _VP, _I32, _I32, _VP, _VP, _I64, _I64, _VP, _VP]),
+    "stepkv_q8_decode_workspace_size": (_SZ, [_I32, _I32, _I32, _I32, _I32, _I32]),
+    "stepkv_q8_decode": (_I32, [ctypes.POINTER(CQ8Cache), _VP, _I32, _VP, _I32, _I32, _I32, _VP, _VP, _I64, _VP, _SZ, _VP,
+                                _VP]),
+    "stepkv_evict_workspace_size": (_SZ, [_I32, _I32, _I32]),
+    "stepkv_evict": (_I32, [_I32, _VP, _VP, _I64, _I32, _I32, _VP, _I32, _I32, _I32, _I32, _I32, _I32, _VP, _I64, _VP, _I64,
+                            _VP, _VP, _SZ, _VP, _VP]),
+    "stepkv_q8_evict": (_I32, [ctypes.POINTER(CQ8Cache), _VP, _I32, _I32, _I32, _I32, _I32, _I32, _VP, _I64, _VP, _I64, _VP,
+                               _VP, _SZ, _VP, _VP]),
     "stepkv_compress_workspace_size": (_SZ, [ctypes.POINTER(CProblem), _I32]),
     "stepkv_compress": (_I32, [ctypes.POINTER(CProblem), _I32, ctypes.POINTER(CParams), _VP, _SZ, _VP, _VP]),
 }
@@ -1040,3 +1057,222 @@ def stepkv_q4_decode(q, cache: Q4Cache, n, out=None, ws=None, status=None, strea
     _call_on(cache.device, stream, "stepkv_q4_decode", lib.stepkv_q4_decode, cache.c(), qs.ptrs, Hq, _ptr(n_dev), stride, n,
              cache.rows, outs.ptrs, wp, wn, status.data_ptr())
     return out
+
+
+# ----------------------------------------------------------------------------- a cache held in 8 bits
+Q8_BLOCK = 32  # rows of a head that share a scale (STEPKV_Q8_BLOCK in the header)
+
+
+class Q8Cache:
+    """A KV cache held in 8 bits (format in include/stepkv.h).  K, V: codes, per layer [Hkv, rows, d] float8_e4m3fn;
+    K_scale, V_scale: [Hkv, ceil(rows / 32)] float32; each a list of per-layer tensors or one tensor with the layers in
+    front.  The checked C struct is built once: the tensors must not be replaced."""
+
+    def __init__(self, K, K_scale, V, V_scale):
+        torch = _torch()
+        self.K, self.K_scale, self.V, self.V_scale = K, K_scale, V, V_scale
+        f8, f32 = torch.float8_e4m3fn, torch.float32
+        parts = [(K, f8, 3, "K"), (K_scale, f32, 2, "K_scale"), (V, f8, 3, "V"), (V_scale, f32, 2, "V_scale")]
+        self._parts = [_PerLayer(*p) for p in parts]
+        codes, scales = self._parts[:2]
+        self.n_layers, (self.Hkv, self.rows, self.d), self.device = codes.n, codes.shape, codes.device
+        for x, name in ((self.n_layers, "layers"), (self.Hkv, "Hkv"), (self.rows, "rows"), (self.d, "d")):
+            _int32(x, name)
+        if self.rows < 1 or self.d < 1:
+            raise ValueError("codes must be [Hkv, rows >= 1, d]")
+        blocks = (self.rows + Q8_BLOCK - 1) // Q8_BLOCK
+        for p, (_, t, ndim, name), like in zip(self._parts, parts, (codes, scales) * 2):
+            want = (self.Hkv, self.rows, self.d) if ndim == 3 else (self.Hkv, blocks)
+            if p.n != self.n_layers or p.shape != want or p.device != self.device:
+                raise ValueError(f"{name} must be {self.n_layers} x {list(want)} on {self.device}")
+            if ndim == 3 and (p.strides[2] != 1 or (self.rows > 1 and p.strides[1] != self.d)):
+                raise ValueError(f"{name} rows must be dense")
+            if ndim == 2 and blocks > 1 and p.strides[1] != 1:
+                raise ValueError(f"{name}: a head's scales must be contiguous")
+            if self.Hkv > 1 and p.strides[0] != like.strides[0]:
+                raise ValueError(f"{name} must share the head stride of {'K' if ndim == 3 else 'K_scale'}")
+        stride = [codes.strides[0], scales.strides[0]] if self.Hkv > 1 else [self.rows * self.d, blocks]
+        self._ptrs = [array.array("Q", p.ptrs) for p in self._parts]
+        self._c = CQ8Cache(self.n_layers, self.Hkv, self.d, self.rows, *[p.buffer_info()[0] for p in self._ptrs], *stride)
+        self._ref = ctypes.byref(self._c)
+
+    @staticmethod
+    def allocate(n_layers: int, Hkv: int, rows: int, d: int, device="cuda") -> "Q8Cache":
+        """An empty cache (zeroed: every row reads back as 0)."""
+        torch = _torch()
+        z = lambda *shape, dtype: torch.zeros((n_layers, Hkv, *shape), dtype=dtype, device=device)
+        kv = [x for _ in "kv" for x in (z(rows, d, dtype=torch.float8_e4m3fn),
+                                        z((rows + Q8_BLOCK - 1) // Q8_BLOCK, dtype=torch.float32))]
+        return Q8Cache(*kv)
+
+    def layers(self, lo: int, hi: Optional[int] = None) -> "Q8Cache":
+        """Layers lo .. hi of this cache (as a slice of a list takes them), sharing its memory."""
+        return Q8Cache(self.K[lo:hi], self.K_scale[lo:hi], self.V[lo:hi], self.V_scale[lo:hi])
+
+    def c(self):
+        return self._ref
+
+
+def stepkv_q8_write(cache: Q8Cache, K, V, row0, n=None, idx=None, status=None, stream=None):
+    """Appends rows of K and V (per layer [Hkv, T, d] bf16, any head and row strides) to the cache as its rows row0,
+    row0 + 1, ...: rows idx[0], idx[1], ... of K and V, or all of them in order.  The heads end with the rows written; rows
+    before row0 stay.  row0: an int, or a device int32 tensor of one row or one per layer; n: how many rows (default all), an
+    int or a device int32 tensor.  Returns the status word."""
+    lib = load_library()
+    k, v, T, hs, rs = _q4_bf16(cache, K, V, "stepkv_q8_write")
+    if k is None or v is None:
+        raise ValueError("stepkv_q8_write needs K and V")
+    _int32(T, "T")
+    if idx is not None:
+        _int32_vector(idx, "idx", cache.device, 0)
+    n_dev, n, row0_dev, stride, row0 = _q4_rows(cache, row0, n, T if idx is None else idx.numel())
+    status = _status_on(cache.device, status, stream)
+    _call_on(cache.device, stream, "stepkv_q8_write", lib.stepkv_q8_write, cache.c(), k.ptrs, v.ptrs, hs, rs, T, _ptr(idx),
+             _ptr(n_dev), n, _ptr(row0_dev), stride, row0, status.data_ptr())
+    return status
+
+
+def stepkv_q8_read(cache: Q8Cache, row0=0, n=None, idx=None, K=None, V=None, status=None, stream=None):
+    """Rows row0, row0 + 1, ... (or idx[0], idx[1], ...) of the cache as bf16, exactly: returns (K, V), per layer
+    [Hkv, >= n, d].  n: an int or a device int32 tensor, default as many as K and V (or idx, or the cache from an int row0
+    on) hold.  Give K or V alone to read only that; neither: both are allocated as [n_layers, Hkv, n, d] (a device n: with
+    room for all; rows that are not read are zero)."""
+    torch = _torch()
+    lib = load_library()
+    if idx is not None:
+        _int32_vector(idx, "idx", cache.device, 0)
+    if K is None and V is None:
+        known = idx is None and isinstance(row0, int) and (n is None or isinstance(n, int))
+        room = idx.numel() if idx is not None else cache.rows - (row0 if isinstance(row0, int) else 0)
+        new = torch.empty if known else torch.zeros
+        shape = (cache.n_layers, cache.Hkv, n if isinstance(n, int) else max(room, 0), cache.d)
+        with _made_on(stream):
+            K, V = (new(shape, dtype=torch.bfloat16, device=cache.device) for _ in "kv")
+    k, v, rows, hs, rs = _q4_bf16(cache, K, V, "stepkv_q8_read")
+    n_dev, n, row0_dev, stride, row0 = _q4_rows(cache, row0, n, rows if idx is None else min(rows, idx.numel()))
+    status = _status_on(cache.device, status, stream)
+    _call_on(cache.device, stream, "stepkv_q8_read", lib.stepkv_q8_read, cache.c(), _ptr(idx), _ptr(n_dev), n, _ptr(row0_dev),
+             stride, row0, None if k is None else k.ptrs, None if v is None else v.ptrs, hs, rs, status.data_ptr())
+    return K, V
+
+
+def _counts_arg(n, cache_layers, dev):
+    """(n_dev, stride, n_host) of a count given as an int, or a device int32 tensor of one count or one per layer."""
+    if isinstance(n, int):
+        return None, 0, _int32(n, "n")
+    n = _int32_vector(n, "n", dev)
+    if n.numel() not in (1, cache_layers):
+        raise ValueError("n must hold one count, or one for each layer")
+    return n, int(n.numel() > 1), 0
+
+
+def _per_row(x, dtype, L, Hkv, rows, dev, name):
+    """Per layer [Hkv, >= rows] with contiguous rows of numbers: (_PerLayer, head stride)."""
+    p = _PerLayer(x, dtype, 2, name)
+    if p.n != L or p.shape[0] != Hkv or p.shape[1] < rows or p.device != dev or (p.shape[1] > 1 and p.strides[1] != 1):
+        raise ValueError(f"{name} must be {L} x [{Hkv}, >= {rows}] with contiguous rows, on {dev}")
+    return p, p.strides[0] if Hkv > 1 else p.shape[1]
+
+
+def q8_decode_workspace(cache: Q8Cache, Hq: int, mass: bool = False):
+    """A workspace for stepkv_q8_decode calls over this cache (one call at a time may use it); mass: for calls with masses."""
+    torch = _torch()
+    need = load_library().stepkv_q8_decode_workspace_size(cache.n_layers, cache.Hkv, _int32(Hq, "Hq"), cache.d, cache.rows,
+                                                          int(bool(mass)))
+    return torch.empty(need + 512, dtype=torch.uint8, device=cache.device)
+
+
+def stepkv_q8_decode(q, cache: Q8Cache, n, out=None, mass=None, ws=None, status=None, stream=None):
+    """One query token per layer (or per trajectory of a batch) over a cache held in 8 bits: stepkv_decode's formula.
+
+    q: per layer [Hq, d] bf16; n: an int, or a device int32 tensor of one count or one per layer (0: the output is
+    zero); mass: per layer [Hkv, >= rows] float32, to which every key's softmax weight, averaged over its query heads,
+    is added.  Returns out, per layer [Hq, d] fp32, as a list or (where q is one tensor) one tensor."""
+    torch = _torch()
+    lib = load_library()
+    qs = _PerLayer(q, torch.bfloat16, 2, "q")
+    Hq = qs.shape[0]
+    if qs.n != cache.n_layers or qs.shape[1] != cache.d:
+        raise ValueError("stepkv_q8_decode needs one [Hq, d] query per layer of the cache")
+    if out is None:
+        with _made_on(stream):
+            out = torch.empty((cache.n_layers, Hq, cache.d), dtype=torch.float32, device=cache.device)
+        out = out if isinstance(q, torch.Tensor) else list(out)
+    outs = _PerLayer(out, torch.float32, 2, "out")
+    for x, name in ((qs, "q"), (outs, "out")):
+        if x.n != cache.n_layers or x.shape != qs.shape or x.strides != (cache.d, 1) or x.device != cache.device:
+            raise ValueError(f"{name} must be contiguous [Hq, d] per layer, on the cache's device")
+    masses, mass_stride = None, 0
+    if mass is not None:
+        masses, mass_stride = _per_row(mass, torch.float32, cache.n_layers, cache.Hkv, cache.rows, cache.device, "mass")
+    n_dev, stride, n = _counts_arg(n, cache.n_layers, cache.device)
+    if ws is None:
+        with _made_on(stream):
+            ws = q8_decode_workspace(cache, Hq, mass is not None)
+    wp, wn = _aligned_ws(ws)
+    status = _status_on(cache.device, status, stream)
+    _on(cache.device, ws, "ws")
+    _call_on(cache.device, stream, "stepkv_q8_decode", lib.stepkv_q8_decode, cache.c(), qs.ptrs, Hq, _ptr(n_dev), stride, n,
+             cache.rows, outs.ptrs, None if masses is None else masses.ptrs, mass_stride, wp, wn, status.data_ptr())
+    return out
+
+
+# ----------------------------------------------------------------------------- eviction by accumulated attention
+def evict_workspace(mass, rows: Optional[int] = None):
+    """A workspace for evictions from a cache of `rows` rows (default: as many as mass has) whose accumulated attention is
+    `mass` (one call at a time may use it)."""
+    torch = _torch()
+    p = _PerLayer(mass, torch.float32, 2, "mass")
+    need = load_library().stepkv_evict_workspace_size(p.n, p.shape[0], _int32(p.shape[1] if rows is None else rows, "rows"))
+    return torch.empty(need + 512, dtype=torch.uint8, device=p.device)
+
+
+def _evict(where, call, front, L, Hkv, rows, dev, mass, pos, n, keep, n_sink, n_recent, n_out, ws, status, stream):
+    torch = _torch()
+    m, ms = _per_row(mass, torch.float32, L, Hkv, rows, dev, "mass")
+    p, ps = _per_row(pos, torch.int32, L, Hkv, rows, dev, "pos")
+    n_dev, stride, n_host = _counts_arg(n, L, dev)
+    for x, name in ((rows, "rows"), (keep, "keep"), (n_sink, "n_sink"), (n_recent, "n_recent")):
+        _int32(x, name)
+    counts = n_dev.numel() if stride else 1
+    if n_out is None:
+        with _made_on(stream):
+            n_out = torch.zeros(counts, dtype=torch.int32, device=dev)
+    elif _int32_vector(n_out, "n_out", dev, counts).numel() != counts:
+        raise ValueError(f"n_out must hold {counts}, as n does")
+    if ws is None:
+        with _made_on(stream):
+            ws = evict_workspace(mass, rows)
+    wp, wn = _aligned_ws(ws)
+    status = _status_on(dev, status, stream)
+    _on(dev, ws, "ws")
+    _call_on(dev, stream, where, call, *front, _ptr(n_dev), stride, n_host, rows, keep, n_sink, n_recent, m.ptrs, ms, p.ptrs,
+             ps, n_out.data_ptr(), wp, wn, status.data_ptr())
+    return n_out
+
+
+def stepkv_evict(K, V, mass, pos, n, keep: int, n_sink: int = 0, n_recent: int = 0, n_out=None, ws=None, status=None,
+                 stream=None):
+    """Every KV head of every layer keeps, by itself and in place, `keep` of its n rows: those with a position below n_sink
+    or among the n_recent newest, then those of the largest accumulated attention.
+
+    K, V: per layer [Hkv, rows, d] bf16; mass: per layer [Hkv, >= rows] float32 (stepkv_decode_h2o's); pos: per layer
+    [Hkv, >= rows] int32, the position of each row's token; n: an int, or a device int32 tensor of one count or one per
+    layer.  Rows [0, keep) are the retained ones afterwards, with their masses and positions; masses behind them
+    are zero.  Returns n_out, min(n, keep) on the device, as many as n has (n itself may be given)."""
+    torch = _torch()
+    k, v = (_PerLayer(x, torch.bfloat16, 3, name) for x, name in ((K, "K"), (V, "V")))
+    Hkv, rows, d = k.shape
+    if not k.like(v) or k.strides[2] != 1 or (rows > 1 and k.strides[1] != d):
+        raise ValueError("stepkv_evict: K and V must be laid out alike, with dense rows")
+    front = (_int32(k.n, "layers"), k.ptrs, v.ptrs, k.strides[0] if Hkv > 1 else rows * d, _int32(Hkv, "Hkv"), _int32(d, "d"))
+    return _evict("stepkv_evict", load_library().stepkv_evict, front, k.n, Hkv, rows, k.device, mass, pos, n, keep, n_sink,
+                  n_recent, n_out, ws, status, stream)
+
+
+def stepkv_q8_evict(cache: Q8Cache, mass, pos, n, keep: int, n_sink: int = 0, n_recent: int = 0, n_out=None, ws=None,
+                    status=None, stream=None):
+    """stepkv_evict from a cache held in 8 bits: blocks that receive rows keep their scale or take the larger one that these
+    need (format in include/stepkv.h)."""
+    return _evict("stepkv_q8_evict", load_library().stepkv_q8_evict, (cache.c(),), cache.n_layers, cache.Hkv, cache.rows,
+                  cache.device, mass, pos, n, keep, n_sink, n_recent, n_out, ws, status, stream)

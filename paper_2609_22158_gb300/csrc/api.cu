@@ -570,6 +570,189 @@ stepkv_status_t stepkv_q4_decode(const stepkv_q4_cache_t* cache, const void* con
                        static_cast<cudaStream_t>(stream));
 }
 
+// ---- a cache held in 8 bits
+static stepkv_status_t check_q8_cache(const stepkv_q8_cache_t* c) {
+  if (!c || c->n_layers < 1 || c->Hkv < 1 || c->d < 1 || c->rows < 1) return STEPKV_EINVAL;
+  if (c->d != 64 && c->d != 128) return STEPKV_EUNSUPPORTED;
+  if (c->rows > kQ8MaxRows || c->Hkv > 65535) return STEPKV_EUNSUPPORTED;
+  if (!c->K || !c->K_scale || !c->V || !c->V_scale) return STEPKV_EINVAL;
+  if (c->code_head_stride < (int64_t)c->rows * c->d || c->scale_head_stride < (c->rows + STEPKV_Q8_BLOCK - 1) / STEPKV_Q8_BLOCK)
+    return STEPKV_EINVAL;
+  if (c->code_head_stride % 16) return STEPKV_EUNSUPPORTED;
+  for (int l = 0; l < c->n_layers; ++l) {
+    if (!c->K[l] || !c->K_scale[l] || !c->V[l] || !c->V_scale[l]) return STEPKV_EINVAL;
+    if (!aligned16(c->K[l]) || !aligned16(c->V[l])) return STEPKV_EUNSUPPORTED;
+    if ((reinterpret_cast<uintptr_t>(c->K_scale[l]) & 3u) || (reinterpret_cast<uintptr_t>(c->V_scale[l]) & 3u))
+      return STEPKV_EUNSUPPORTED;
+  }
+  return STEPKV_OK;
+}
+
+static void add_q8_rows(Footprints& f, const stepkv_q8_cache_t& c, bool written) {
+  const Footprint codes = make_footprint(c.Hkv, c.code_head_stride, 1, 0, (int64_t)c.rows * c.d);
+  const Footprint scales =
+      make_footprint(c.Hkv, 4 * c.scale_head_stride, 1, 0, 4 * (((int64_t)c.rows + STEPKV_Q8_BLOCK - 1) / STEPKV_Q8_BLOCK));
+  f.add(c.K, c.n_layers, codes, written);
+  f.add(reinterpret_cast<const void* const*>(c.K_scale), c.n_layers, scales, written);
+  f.add(c.V, c.n_layers, codes, written);
+  f.add(reinterpret_cast<const void* const*>(c.V_scale), c.n_layers, scales, written);
+}
+
+stepkv_status_t stepkv_q8_write(const stepkv_q8_cache_t* cache, const void* const* K, const void* const* V,
+                                int64_t head_stride, int64_t row_stride, int32_t T, const int32_t* idx,
+                                const int32_t* n_dev, int32_t n, const int32_t* row0_dev, int32_t row0_dev_stride,
+                                int32_t row0, int32_t* dev_status, void* stream) {
+  stepkv_status_t st = check_q8_cache(cache);
+  if (st != STEPKV_OK) return st;
+  if (!K || !V || T < 0) return STEPKV_EINVAL;
+  const Q4Rows r{idx, n_dev, n, row0_dev, row0_dev_stride, row0};
+  st = check_q4_rows(cache->n_layers, K, V, head_stride, row_stride, r);
+  if (st != STEPKV_OK) return st;
+  if (!idx && n > T) return STEPKV_EINVAL;
+  if (!row0_dev && !n_dev && (row0 < 0 || (int64_t)row0 + n > cache->rows)) return STEPKV_ENOSPACE;
+  if (n == 0 && !n_dev) return STEPKV_OK;
+  Footprints f;
+  add_q8_rows(f, *cache, true);
+  if (n > 0 && T > 0) {  // (a stride of 0: the same row for all)
+    const Footprint rows = make_footprint(head_stride ? cache->Hkv : 1, 2 * head_stride, row_stride ? T : 1, 2 * row_stride,
+                                          2 * (int64_t)cache->d);
+    f.add(K, cache->n_layers, rows, false);
+    f.add(V, cache->n_layers, rows, false);
+  }
+  if (f.clash()) return STEPKV_EINVAL;
+  return q8_write_run(*cache, K, V, head_stride, row_stride, T, r, dev_status, static_cast<cudaStream_t>(stream));
+}
+
+stepkv_status_t stepkv_q8_read(const stepkv_q8_cache_t* cache, const int32_t* idx, const int32_t* n_dev, int32_t n,
+                               const int32_t* row0_dev, int32_t row0_dev_stride, int32_t row0, void* const* K,
+                               void* const* V, int64_t head_stride, int64_t row_stride, int32_t* dev_status,
+                               void* stream) {
+  stepkv_status_t st = check_q8_cache(cache);
+  if (st != STEPKV_OK) return st;
+  if (!K && !V) return STEPKV_EINVAL;
+  const Q4Rows r{idx, n_dev, n, row0_dev, row0_dev_stride, row0};
+  st = check_q4_rows(cache->n_layers, K, V, head_stride, row_stride, r);
+  if (st != STEPKV_OK) return st;
+  if ((head_stride < cache->d && cache->Hkv > 1) || (row_stride < cache->d && n > 1)) return STEPKV_EINVAL;  // rows apart
+  if (!idx && !row0_dev && !n_dev && (row0 < 0 || (int64_t)row0 + n > cache->rows)) return STEPKV_EINVAL;
+  if (n == 0 && !n_dev) return STEPKV_OK;
+  Footprints f;
+  add_q8_rows(f, *cache, false);
+  if (n > 0) {
+    const Footprint rows = make_footprint(cache->Hkv, 2 * head_stride, n, 2 * row_stride, 2 * (int64_t)cache->d);
+    f.add(K, cache->n_layers, rows, true);
+    f.add(V, cache->n_layers, rows, true);
+  }
+  if (f.clash()) return STEPKV_EINVAL;
+  return q8_read_run(*cache, r, K, V, head_stride, row_stride, dev_status, static_cast<cudaStream_t>(stream));
+}
+
+size_t stepkv_q8_decode_workspace_size(int32_t n_layers, int32_t Hkv, int32_t Hq, int32_t d, int32_t n_cap,
+                                       int32_t with_mass) {
+  if (n_layers < 1 || Hkv < 1 || Hkv > 65535 || Hq < Hkv || Hq % Hkv != 0 || Hq / Hkv > 8 || n_cap < 1 || n_cap > kQ8MaxRows ||
+      (d != 64 && d != 128))
+    return 0;
+  if (!q4_decode_fits(n_layers, Hkv, n_cap)) return 0;
+  return q8_decode_ws_bytes(std::min(n_layers, kQ8Layers), Hkv, Hq, d, n_cap, with_mass != 0);
+}
+
+stepkv_status_t stepkv_q8_decode(const stepkv_q8_cache_t* cache, const void* const* q, int32_t Hq, const int32_t* n_dev,
+                                 int32_t n_dev_stride, int32_t n_host, int32_t n_cap, float* const* out, float* const* mass,
+                                 int64_t mass_head_stride, void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  stepkv_status_t st = check_q8_cache(cache);
+  if (st != STEPKV_OK) return st;
+  if (!q || !out || !ws || Hq < 1 || Hq % cache->Hkv != 0 || n_cap < 1 || n_cap > cache->rows) return STEPKV_EINVAL;
+  if (Hq / cache->Hkv > 8) return STEPKV_EUNSUPPORTED;
+  if (!q4_decode_fits(cache->n_layers, cache->Hkv, n_cap)) return STEPKV_EUNSUPPORTED;
+  if (n_dev ? (n_dev_stride != 0 && n_dev_stride != 1) : (n_host < 0 || n_host > n_cap)) return STEPKV_EINVAL;
+  if (mass && mass_head_stride < n_cap) return STEPKV_EINVAL;
+  if (ws_bytes < stepkv_q8_decode_workspace_size(cache->n_layers, cache->Hkv, Hq, cache->d, n_cap, mass != nullptr))
+    return STEPKV_ENOSPACE;
+  if ((reinterpret_cast<uintptr_t>(ws) & 255u) != 0) return STEPKV_EINVAL;
+  for (int l = 0; l < cache->n_layers; ++l) {
+    if (!q[l] || !out[l] || (mass && !mass[l])) return STEPKV_EINVAL;
+    if (!aligned16(q[l]) || !aligned16(out[l])) return STEPKV_EUNSUPPORTED;
+    if (mass && (reinterpret_cast<uintptr_t>(mass[l]) & 3u)) return STEPKV_EUNSUPPORTED;
+  }
+  Footprints f;
+  f.add(reinterpret_cast<const void* const*>(out), cache->n_layers, Footprint{1, 0, 1, 0, 4 * (int64_t)Hq * cache->d}, true);
+  if (mass)
+    f.add(reinterpret_cast<const void* const*>(mass), cache->n_layers,
+          make_footprint(cache->Hkv, 4 * mass_head_stride, 1, 0, 4 * (int64_t)n_cap), true);
+  if (f.clash()) return STEPKV_EINVAL;
+  return q8_decode_run(*cache, q, Hq, n_dev, n_dev_stride, n_host, n_cap, out, mass, mass_head_stride, ws, dev_status,
+                       static_cast<cudaStream_t>(stream));
+}
+
+// ---- eviction by accumulated attention
+size_t stepkv_evict_workspace_size(int32_t n_layers, int32_t Hkv, int32_t n_cap) {
+  if (n_layers < 1 || Hkv < 1 || Hkv > 65535 || n_cap < 1 || n_cap > kEvictMaxRows) return 0;
+  return evict_ws_bytes(std::min(n_layers, kQ8Layers), Hkv, n_cap);
+}
+
+// What both evictions check alike; `f` holds the cache's tensors.
+static stepkv_status_t check_evict(int n_layers, int Hkv, const EvictSpec& e, size_t ws_bytes, Footprints& f) {
+  if (!e.mass || !e.pos || !e.ws || e.n_cap < 1 || e.keep < 1 || e.keep > e.n_cap) return STEPKV_EINVAL;
+  if (e.n_sink < 0 || e.n_recent < 0 || (int64_t)e.n_sink + e.n_recent > e.keep) return STEPKV_EINVAL;
+  if (e.mass_stride < e.n_cap || e.pos_stride < e.n_cap) return STEPKV_EINVAL;
+  if (e.n_cap > kEvictMaxRows || Hkv > 65535) return STEPKV_EUNSUPPORTED;
+  if (e.n_dev ? (e.n_stride != 0 && e.n_stride != 1) : (e.n_host < 0 || e.n_host > e.n_cap)) return STEPKV_EINVAL;
+  if (ws_bytes < stepkv_evict_workspace_size(n_layers, Hkv, e.n_cap)) return STEPKV_ENOSPACE;
+  if ((reinterpret_cast<uintptr_t>(e.ws) & 255u) != 0) return STEPKV_EINVAL;
+  for (int l = 0; l < n_layers; ++l) {
+    if (!e.mass[l] || !e.pos[l]) return STEPKV_EINVAL;
+    if ((reinterpret_cast<uintptr_t>(e.mass[l]) & 3u) || (reinterpret_cast<uintptr_t>(e.pos[l]) & 3u)) return STEPKV_EUNSUPPORTED;
+  }
+  f.add(reinterpret_cast<const void* const*>(e.mass), n_layers, make_footprint(Hkv, 4 * e.mass_stride, 1, 0, 4 * (int64_t)e.n_cap), true);
+  f.add(reinterpret_cast<const void* const*>(e.pos), n_layers, make_footprint(Hkv, 4 * e.pos_stride, 1, 0, 4 * (int64_t)e.n_cap), true);
+  const int64_t counts = e.n_dev && e.n_stride ? n_layers : 1;
+  const void* const n_in = e.n_dev;
+  const void* const n_out = e.n_out;
+  if (n_out) f.add(&n_out, 1, Footprint{1, 0, 1, 0, 4 * counts}, true);
+  if (n_in && n_in != n_out) f.add(&n_in, 1, Footprint{1, 0, 1, 0, 4 * counts}, false);
+  return f.clash() ? STEPKV_EINVAL : STEPKV_OK;
+}
+
+stepkv_status_t stepkv_evict(int32_t n_layers, void* const* K, void* const* V, int64_t kv_head_stride, int32_t Hkv, int32_t d,
+                             const int32_t* n_dev, int32_t n_dev_stride, int32_t n_host, int32_t n_cap, int32_t keep,
+                             int32_t n_sink, int32_t n_recent, float* const* mass, int64_t mass_head_stride,
+                             int32_t* const* pos, int64_t pos_head_stride, int32_t* n_out, void* ws, size_t ws_bytes,
+                             int32_t* dev_status, void* stream) {
+  if (n_layers < 1 || Hkv < 1 || d < 8 || !K || !V || n_cap < 1) return STEPKV_EINVAL;
+  if (d % 8 || d > 256) return STEPKV_EUNSUPPORTED;
+  if (kv_head_stride < (int64_t)n_cap * d) return STEPKV_EINVAL;
+  if (kv_head_stride % 8) return STEPKV_EUNSUPPORTED;
+  for (int l = 0; l < n_layers; ++l) {
+    if (!K[l] || !V[l]) return STEPKV_EINVAL;
+    if (!aligned16(K[l]) || !aligned16(V[l])) return STEPKV_EUNSUPPORTED;
+  }
+  Footprints f;
+  const Footprint rows = make_footprint(Hkv, 2 * kv_head_stride, 1, 0, 2 * (int64_t)n_cap * d);
+  f.add(K, n_layers, rows, true);
+  f.add(V, n_layers, rows, true);
+  const EvictSpec e{n_dev, n_dev_stride, n_host, n_cap, keep, n_sink, n_recent, mass, mass_head_stride, pos, pos_head_stride,
+                    n_out, ws, dev_status};
+  const stepkv_status_t st = check_evict(n_layers, Hkv, e, ws_bytes, f);
+  if (st != STEPKV_OK) return st;
+  return evict_run(n_layers, K, V, kv_head_stride, Hkv, d, e, static_cast<cudaStream_t>(stream));
+}
+
+stepkv_status_t stepkv_q8_evict(const stepkv_q8_cache_t* cache, const int32_t* n_dev, int32_t n_dev_stride, int32_t n_host,
+                                int32_t n_cap, int32_t keep, int32_t n_sink, int32_t n_recent, float* const* mass,
+                                int64_t mass_head_stride, int32_t* const* pos, int64_t pos_head_stride, int32_t* n_out,
+                                void* ws, size_t ws_bytes, int32_t* dev_status, void* stream) {
+  stepkv_status_t st = check_q8_cache(cache);
+  if (st != STEPKV_OK) return st;
+  if (n_cap > cache->rows) return STEPKV_EINVAL;
+  Footprints f;
+  add_q8_rows(f, *cache, true);
+  const EvictSpec e{n_dev, n_dev_stride, n_host, n_cap, keep, n_sink, n_recent, mass, mass_head_stride, pos, pos_head_stride,
+                    n_out, ws, dev_status};
+  st = check_evict(cache->n_layers, cache->Hkv, e, ws_bytes, f);
+  if (st != STEPKV_OK) return st;
+  return q8_evict_run(*cache, e, static_cast<cudaStream_t>(stream));
+}
+
 stepkv_status_t stepkv_step_signals(const uint32_t* cues, const int32_t* n_cues, int32_t n_steps, int32_t k0,
                                     float* gain, float* red, float* obs_sim, int32_t* dev_status, void* stream) {
   if (!cues || !n_cues || n_steps < 1 || n_steps > 65535 || k0 < 0 || k0 > n_steps) return STEPKV_EINVAL;

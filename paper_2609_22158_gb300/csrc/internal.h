@@ -113,6 +113,35 @@ size_t q4_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap);
 stepkv_status_t q4_decode_run(const stepkv_q4_cache_t& c, const void* const* q, int Hq, const int32_t* n_dev, int n_stride,
                               int n_host, int n_cap, float* const* out, void* ws, int32_t* status, cudaStream_t stream);
 
+// ---- a cache held in 8 bits (q8.cu, q8_decode.cu), eviction (evict.cu)
+constexpr int kQ8Layers = 64;        // layers per launch (pointer arrays travel in the kernel parameters)
+constexpr int kQ8MaxRows = 1 << 30;  // of a head, and of one call
+stepkv_status_t q8_write_run(const stepkv_q8_cache_t& c, const void* const* K, const void* const* V, int64_t head_stride,
+                             int64_t row_stride, int T, const Q4Rows& rows, int32_t* status, cudaStream_t stream);
+stepkv_status_t q8_read_run(const stepkv_q8_cache_t& c, const Q4Rows& rows, void* const* K, void* const* V,
+                            int64_t head_stride, int64_t row_stride, int32_t* status, cudaStream_t stream);
+size_t q8_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap, bool mass);
+stepkv_status_t q8_decode_run(const stepkv_q8_cache_t& c, const void* const* q, int Hq, const int32_t* n_dev, int n_stride,
+                              int n_host, int n_cap, float* const* out, float* const* mass, int64_t mass_stride, void* ws,
+                              int32_t* status, cudaStream_t stream);
+constexpr int kEvictMaxRows = 1 << 18;
+// What both evictions are told.
+struct EvictSpec {
+  const int32_t* n_dev;
+  int n_stride, n_host, n_cap, keep, n_sink, n_recent;
+  float* const* mass;
+  int64_t mass_stride;
+  int32_t* const* pos;
+  int64_t pos_stride;
+  int32_t* n_out;
+  void* ws;
+  int32_t* status;
+};
+size_t evict_ws_bytes(int n_layers, int Hkv, int n_cap);
+stepkv_status_t evict_run(int n_layers, void* const* K, void* const* V, int64_t kv_head_stride, int Hkv, int d,
+                          const EvictSpec& e, cudaStream_t stream);
+stepkv_status_t q8_evict_run(const stepkv_q8_cache_t& c, const EvictSpec& e, cudaStream_t stream);
+
 // ---- step signals from evidence cues (signals.cu)
 stepkv_status_t signals_run(const uint32_t* cues, const int32_t* n_cues, int n_steps, int k0, float* gain, float* red,
                             float* obs_sim, int32_t* status, cudaStream_t stream);
