@@ -32,7 +32,7 @@
 // the captured loop of one layer takes 10.1.)
 //
 // Each warp copies its blocks of 32 rows into a ring of its own with cp.async.  A group of warps takes a pair (q4_whole) or a
-// range of the list of all pairs' blocks (q4_split); its warps interleave the blocks of a pair, join their states in shared
+// range of the list of all pairs' blocks (list_split); its warps interleave the blocks of a pair, join their states in shared
 // memory, and write the output where they had the whole pair, or else leave a partial state, which a second kernel joins with
 // the others in key order.
 #include <cuda_fp16.h>
@@ -41,23 +41,21 @@
 #include <algorithm>
 
 #include "common.cuh"
+#include "decode_list.cuh"
 #include "fastdiv.h"
 #include "internal.h"
 
 namespace stepkv {
 
-constexpr int kQ4DecWarps = 4;      // of a CTA: a group, unless the pairs are many and short
+constexpr int kQ4DecWarps = kListWarps;
 constexpr int kQ4DecThreads = kQ4DecWarps * 32;
 constexpr int kQ4DecCtasPerSm = 3;
 constexpr int kQ4DecMinSmem = 228 * 1024 / (kQ4DecCtasPerSm + 1);
-constexpr int kQ4Block = 32;        // keys per warp step
+constexpr int kQ4Block = kListBlock;
 constexpr int kQ4Stages = 2;
-constexpr int kQ4Few = 16;          // blocks of a pair that one CTA takes at once, though the pair might be cut
-constexpr int kQ4Alone = 2;         // blocks of a pair that a warp takes by itself
-constexpr int kQ4MaxGroups = 4096;  // workspace sizing: groups (single warps) of a launch at most
 constexpr float kQ4WeightLog2 = 14.f;  // the largest weight is held as 2^14 (fp16 reaches 65504)
 
-struct Q4DecodeArgs {
+struct Q4DecodeArgs : DecodeList {
   const uint16_t* q[kQ4Layers];
   const uint8_t* K[kQ4Layers];
   const uint8_t* V[kQ4Layers];
@@ -65,148 +63,15 @@ struct Q4DecodeArgs {
   const __half* V_scale[kQ4Layers];
   float* out[kQ4Layers];
   int64_t code_head_stride, scale_head_stride;
-  int n_layers, layer0;
-  int Hkv, G;
-  int n_groups;     // CTAs
-  // with groups of kQ4DecWarps warps, and of one: divisors groups and k = groups / pairs (1 where there are more pairs)
-  FastDiv by_groups[2], by_k[2];
-  FastDiv by_heads, by_G;
-  const int32_t* n_dev;
-  int n_stride;
-  int n_host;
-  int n_cap;
+  int G;
+  FastDiv by_G;
   float c;          // log2(e) / sqrt(d)
   float* part;      // [slot][G][d + 4]: m, l, -, -, values
-  int32_t* status;
-  int whole;        // warps that take a pair, all of it: no states to join (0: the pairs are cut, q4_split)
+  int whole;        // warps that take a pair, all of it: no states to join (0: the pairs are cut, list_split)
   uint32_t magic;   // kQ4Magic: as a literal it is brought into a register 16 times a block (63.6 -> 61.8 us)
 };
 constexpr uint32_t kQ4Magic = 0x54005400u;  // two fp16 64
 static_assert(sizeof(Q4DecodeArgs) <= 32000, "kernel parameter space");
-
-// The keys of a cache of this launch.
-__device__ __forceinline__ int q4_keys(const Q4DecodeArgs& a, int layer, bool tell = false) {
-  if (!a.n_dev) return a.n_host;
-  const int n = __ldcg(a.n_dev + (a.layer0 + layer) * a.n_stride);  // (the merge reads it early: not from L1)
-  if (tell && n > a.n_cap) record_status(a.status, STEPKV_ENOSPACE);
-  if (tell && n < 0) record_status(a.status, STEPKV_EDATA);
-  return max(0, min(n, a.n_cap));
-}
-
-// Keys of every cache and the first block of each in the list of all pairs' blocks; first[n_layers]: all blocks.  By the
-// first warp of a CTA; the caller synchronises.  Not used where all caches have one count.
-struct Q4Lists {
-  int n[kQ4Layers];
-  int first[kQ4Layers + 1];
-};
-__device__ __forceinline__ int q4_blocks(int n) { return (n + kQ4Block - 1) / kQ4Block; }
-__device__ __forceinline__ bool q4_uniform(const Q4DecodeArgs& a) { return !a.n_dev || a.n_stride == 0 || a.n_layers == 1; }
-__device__ __forceinline__ void q4_lists(const Q4DecodeArgs& a, Q4Lists& s, bool tell) {
-  const int lane = threadIdx.x & 31;
-  int sum[2];
-#pragma unroll
-  for (int i = 0; i < 2; ++i) {
-    const int l = 2 * lane + i;
-    const int n = l < a.n_layers ? q4_keys(a, l, tell) : 0;
-    s.n[l] = n;
-    sum[i] = q4_blocks(n) * a.Hkv;
-  }
-  int total = sum[0] + sum[1];
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int x = __shfl_up_sync(0xffffffffu, total, o);
-    if (lane >= o) total += x;
-  }
-  s.first[2 * lane + 2] = total;
-  s.first[2 * lane + 1] = total - sum[1];
-  if (lane == 0) s.first[0] = 0;
-}
-
-// How the list of blocks is cut, where pairs are.  Ranges of `per` blocks of the list, one after another; or (k > 0: one count
-// for all, and ranges that each lie in one pair, k in each, are nearly as even) these, which spares a second start and end to
-// those that would reach over.  Groups are single warps where there are more pairs than CTAs and the pairs are short: a warp
-// then takes a range by itself instead of waiting for three others at its end.
-struct Q4Split {
-  int W, per, k;
-};
-__device__ __forceinline__ Q4Split q4_split(const Q4DecodeArgs& a, bool uniform, int nb, int total) {
-  Q4Split p;
-  const int pairs = a.n_layers * a.Hkv;
-  const int single = pairs > a.n_groups && total <= 16 * pairs;
-  p.W = single ? 1 : kQ4DecWarps;
-  const FastDiv groups = a.by_groups[single], ks = a.by_k[single];
-  p.per = fdiv(total + groups.d - 1, groups);
-  p.k = 0;
-  if (uniform && nb > 0 && pairs <= groups.d) {
-    // rounded up to whole rounds: a part of one takes as long, and fewer ranges are joined faster
-    const int per = fdiv(nb + ks.d - 1, ks), whole = (per + p.W - 1) & -p.W;
-    if (!single && nb <= kQ4Few) {  // (14 layers x 8 heads x 379 rows 8.0 -> 7.0 us; at 24 blocks 9.6 and 9.1, or slower)
-      p.k = 1;
-      p.per = nb;
-    } else if (per <= p.per + 2 * p.W) {
-      p.per = whole;
-      p.k = (unsigned)(nb + whole - 1) / (unsigned)whole;
-    }
-  }
-  return p;
-}
-
-// Copies of N bytes, and with fewer to read (then zeros).
-template <int N>
-__device__ __forceinline__ void q4_cp(uint32_t dst, const void* src) {
-  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(src) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(src), "n"(N) : "memory");
-}
-template <int N>
-__device__ __forceinline__ void q4_cp_part(uint32_t dst, const void* src, int bytes) {
-  if constexpr (N == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "r"(bytes) : "memory");
-  else asm volatile("cp.async.ca.shared.global [%0], [%1], %2, %3;" ::"r"(dst), "l"(src), "n"(N), "r"(bytes) : "memory");
-}
-__device__ __forceinline__ void q4_cp_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
-template <int N>
-__device__ __forceinline__ void q4_cp_wait() {
-  asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory");
-}
-
-__device__ __forceinline__ void ldmatrix_x4(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) );
-}
-__device__ __forceinline__ void ldmatrix_x4_trans(uint32_t (&r)[4], uint32_t addr) {
-  asm volatile("ldmatrix.sync.aligned.m8n8.x4.trans.shared.b16 {%0,%1,%2,%3}, [%4];"
-               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]) : "r"(addr) );
-}
-__device__ __forceinline__ uint32_t movmatrix_trans(uint32_t x) {
-  uint32_t y;
-  asm("movmatrix.sync.aligned.m8n8.trans.b16 %0, %1;" : "=r"(y) : "r"(x));
-  return y;
-}
-template <int BYTES>
-__device__ __forceinline__ void q4_lds(uint32_t (&w)[BYTES / 4], uint32_t addr) {
-  if constexpr (BYTES == 16)
-    asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];" : "=r"(w[0]), "=r"(w[1]), "=r"(w[2]), "=r"(w[3]) : "r"(addr));
-  else if constexpr (BYTES == 8)
-    asm volatile("ld.shared.v2.u32 {%0,%1}, [%2];" : "=r"(w[0]), "=r"(w[1]) : "r"(addr));
-  else
-    asm volatile("ld.shared.u32 %0, [%1];" : "=r"(w[0]) : "r"(addr));
-}
-
-// D = A B, D = A B + (c0, c1 in both rows), and D += A B, for one m16n8k16 tile of fp16.
-__device__ __forceinline__ void mma_f16_zero(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%10,%10,%10};"
-               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(0.f));
-}
-__device__ __forceinline__ void mma_f16_from(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1, uint32_t c0, uint32_t c1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%10,%11,%10,%11};"
-               : "=f"(d[0]), "=f"(d[1]), "=f"(d[2]), "=f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1), "f"(__uint_as_float(c0)), "f"(__uint_as_float(c1)));
-}
-__device__ __forceinline__ void mma_f16(float (&d)[4], const uint32_t (&a)[4], uint32_t b0, uint32_t b1) {
-  asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
-               : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
-               : "r"(a[0]), "r"(a[1]), "r"(a[2]), "r"(a[3]), "r"(b0), "r"(b1));
-}
 
 // Codes I of the two 4-code chunks in w (one per half) times their scales: (64 + n) s - 72 s.
 template <int I>
@@ -221,18 +86,6 @@ __device__ __forceinline__ uint32_t q4_times_m72(uint32_t s) {
   uint32_t y;
   asm("mul.rn.f16x2 %0, %1, %2;" : "=r"(y) : "r"(s), "r"(0xD480D480u));
   return y;
-}
-
-// Merge the state (m2, l2, acc2) into (m, l, acc), m in log2 units; -inf marks an empty state.
-template <int E>
-__device__ __forceinline__ void q4_merge_state(float& m, float& l, float (&acc)[E], float m2, float l2, const float (&acc2)[E]) {
-  const float mn = fmaxf(m, m2);
-  if (mn == -INFINITY) return;
-  const float a = ex2_approx(m - mn), b = ex2_approx(m2 - mn);
-  l = l * a + l2 * b;
-#pragma unroll
-  for (int e = 0; e < E; ++e) acc[e] = acc[e] * a + acc2[e] * b;
-  m = mn;
 }
 
 // A ring stage: codes of 32 keys, codes of 32 values, their scales, as they lie in memory but for the 16-byte vectors of a
@@ -325,13 +178,13 @@ struct Q4State {
   __device__ __forceinline__ void logits(uint64_t (&s)[4], uint32_t codes, uint32_t scales, uint32_t q, uint32_t offsets) {
     uint32_t sk[4][D / 64], per_sum[2];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) q4_lds<D / 16>(sk[i], scales + 8 * i * (D / 16));
+    for (int i = 0; i < 4; ++i) lds<D / 16>(sk[i], scales + 8 * i * (D / 16));
 #pragma unroll
     for (int p = 0; p < NG / 2; ++p) {
       uint32_t qb[2][4], of[4];
-      q4_lds<16>(of, offsets + 64 * p);
-      q4_lds<16>(qb[0], q + 1024 * p);
-      q4_lds<16>(qb[1], q + 1024 * p + 512);
+      lds<16>(of, offsets + 64 * p);
+      lds<16>(qb[0], q + 1024 * p);
+      lds<16>(qb[1], q + 1024 * p + 512);
 #pragma unroll
       for (int h = 0; h < 2; ++h) {
         uint32_t w[4];
@@ -354,7 +207,7 @@ struct Q4State {
         }
       }
     }
-    q4_lds<8>(per_sum, offsets + kPerSum);
+    lds<8>(per_sum, offsets + kPerSum);
 #pragma unroll
     for (int i = 0; i < 4; ++i) s[i] = f2_mul(s[i], f2_pack(__uint_as_float(per_sum[0]), __uint_as_float(per_sum[1])));
   }
@@ -431,7 +284,7 @@ struct Q4State {
 #pragma unroll
       for (int k = 0; k < 2; ++k) {
         uint32_t w[D / 32];
-        q4_lds<D / 8>(w, stage + St::kVs + (h * 16 + 8 * k + 2 * c4) * St::kScaleRow);
+        lds<D / 8>(w, stage + St::kVs + (h * 16 + 8 * k + 2 * c4) * St::kScaleRow);
 #pragma unroll
         for (int g = 0; g < NG; ++g) ss[h][k][g] = __byte_perm(w[g >> 1], w[NG / 2 + (g >> 1)], g & 1 ? 0x7632 : 0x5410);
       }
@@ -503,13 +356,6 @@ struct Q4State {
   }
 };
 
-// A warp's blocks in the order it takes them: of each pair that the group's range touches, every W-th block.
-struct Q4Cursor {
-  int pair, layer, h;   // the pair at hand; layer == n_layers: none
-  int blk, end;         // its next block for this warp, and where the range ends in it
-  int left;             // blocks of the range from this pair's first one on
-};
-
 // RAGGED: a count for each cache.
 template <int D, int GP, bool RAGGED>
 __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kernel(const __grid_constant__ Q4DecodeArgs a) {
@@ -517,24 +363,24 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   using St = Q4Stage<D>;
   constexpr int kNoMore = -0x40000000;
   extern __shared__ __align__(128) uint8_t q4_smem[];  // per-warp rings, then per-warp states, then per-warp queries
-  __shared__ Q4Lists s_list;  // RAGGED
+  __shared__ ListCounts s_list;  // RAGGED
   __shared__ float s_ml[kQ4DecWarps][2 * GP];
-  __shared__ Q4Cursor s_cursor[kQ4DecWarps], s_here[kQ4DecWarps];  // where each warp's copies and its arithmetic are, out of its registers
+  __shared__ ListCursor s_cursor[kQ4DecWarps], s_here[kQ4DecWarps];  // where each warp's copies and its arithmetic are, out of its registers
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
   pdl_launch_dependents();
   int n_all = 0, total;
   if constexpr (!RAGGED) {
-    n_all = q4_keys(a, 0, blockIdx.x == 0 && threadIdx.x == 0);
-    total = q4_blocks(n_all) * a.n_layers * a.Hkv;
+    n_all = list_keys(a, 0, blockIdx.x == 0 && threadIdx.x == 0);
+    total = list_blocks(n_all) * a.n_layers * a.Hkv;
   } else {
-    if (warp == 0) q4_lists(a, s_list, blockIdx.x == 0);
+    if (warp == 0) list_counts(a, s_list, blockIdx.x == 0);
     __syncthreads();
     total = s_list.first[a.n_layers];
   }
   auto keys_of = [&](int layer) { return RAGGED ? s_list.n[layer] : n_all; };
-  auto blocks_of = [&](int layer) { return q4_blocks(keys_of(layer)); };
-  const Q4Split sp = q4_split(a, !RAGGED, q4_blocks(n_all), total);
+  auto blocks_of = [&](int layer) { return list_blocks(keys_of(layer)); };
+  const ListSplit sp = list_split(a, !RAGGED, list_blocks(n_all), total);
   const int W = a.whole ? a.whole : sp.W, rank = warp & (W - 1);
   const int group = W == 1 ? blockIdx.x * kQ4DecWarps + warp : blockIdx.x;
   float* s_vals = reinterpret_cast<float*>(q4_smem + kQ4DecWarps * kQ4Stages * St::kBytes);
@@ -542,7 +388,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   const uint32_t ring = smem_u32(q4_smem + warp * kQ4Stages * St::kBytes), q_at = smem_u32(s_q) + 16 * lane;
 
   // the range and its first pair
-  Q4Cursor ci;
+  ListCursor ci;
   ci.layer = a.n_layers;
   if (a.whole) {
     if (group < a.n_layers * a.Hkv) {
@@ -558,7 +404,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
       }
     }
   } else if (!RAGGED && sp.k > 0) {
-    const int nb = q4_blocks(n_all);
+    const int nb = list_blocks(n_all);
     ci.pair = (unsigned)group / (unsigned)sp.k;
     ci.blk = (group - ci.pair * sp.k) * sp.per;
     if (ci.pair < a.n_layers * a.Hkv && ci.blk < nb) {
@@ -571,7 +417,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     if (lo < hi) {
       int at, nb;
       if constexpr (!RAGGED) {
-        nb = q4_blocks(n_all);
+        nb = list_blocks(n_all);
         ci.pair = (unsigned)lo / (unsigned)nb;
         ci.layer = fdivmod(ci.pair, a.by_heads, ci.h);
         at = lo - ci.pair * nb;
@@ -591,7 +437,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   }
   if (ci.layer == a.n_layers) return;  // whole groups
   if (lane == 0) s_here[warp] = ci;
-  auto next_pair = [&](Q4Cursor& c) {
+  auto next_pair = [&](ListCursor& c) {
     c.left -= c.end;
     if (c.left <= 0) {
       c.layer = a.n_layers;
@@ -615,7 +461,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   const int cp_row = lane / kVecRow, cp_vec = lane & (kVecRow - 1);
   const uint32_t cp_dst = cp_row * St::kRow + ((cp_vec ^ St::swizzle(cp_row)) << 4);
   const uint8_t *Kc = nullptr, *Vc = nullptr, *Ks = nullptr, *Vs = nullptr;  // this lane's part of the next block
-  auto bases = [&](const Q4Cursor& c) {
+  auto bases = [&](const ListCursor& c) {
     const int64_t row = (int64_t)c.blk * kQ4Block;
     const int64_t code = c.h * a.code_head_stride + row * St::kRow + lane * 16;
     const int64_t scale = 2 * c.h * a.scale_head_stride + (row + lane) * St::kScaleRow;
@@ -626,13 +472,13 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   };
   // RAGGED: a pair of which the range holds a block or two is one warp's, the warps taking turns, and the others go on: the
   // short lists run side by side (24 caches of 1 to 8191 rows 15.7 -> 11.2 us).
-  auto alone = [&](const Q4Cursor& c) { return RAGGED && c.end - c.blk <= kQ4Alone; };
-  auto mine = [&](const Q4Cursor& c) { return !alone(c) || (c.pair & (W - 1)) == rank; };
-  Q4Cursor& is = s_cursor[warp];
+  auto alone = [&](const ListCursor& c) { return RAGGED && c.end - c.blk <= kListAlone; };
+  auto mine = [&](const ListCursor& c) { return !alone(c) || (c.pair & (W - 1)) == rank; };
+  ListCursor& is = s_cursor[warp];
   // from the next block on: blocks of this warp left in the pair (<= 0: none), rows of the pair; from one block to the next:
   // rows, bytes of codes and of scales
   int ahead, rows, row_step, code_step, scale_step;
-  auto enter = [&](Q4Cursor& c) {  // c: a pair's, its first block
+  auto enter = [&](ListCursor& c) {  // c: a pair's, its first block
     row_step = (alone(c) ? 1 : W) * kQ4Block;
     code_step = row_step * St::kRow;
     scale_step = row_step * St::kScaleRow;
@@ -645,14 +491,14 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
     bases(c);
   };
   {
-    Q4Cursor c = ci;
+    ListCursor c = ci;
     enter(c);
     if (lane == 0) is = c;
     __syncwarp();
   }
   auto issue_next = [&](uint32_t dst) {
     if (ahead <= 0 && ahead > kNoMore / 2) {
-      Q4Cursor c = is;
+      ListCursor c = is;
       do {
         next_pair(c);
         if (c.layer < a.n_layers) enter(c);
@@ -667,24 +513,24 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
       if (rows >= kQ4Block) {
 #pragma unroll
         for (int i = 0; i < kVecRow; ++i) {
-          q4_cp<16>(d16 + i * 512, Kc + i * 512);
-          q4_cp<16>(d16 + St::kV + i * 512, Vc + i * 512);
+          cp_async<16>(d16 + i * 512, Kc + i * 512);
+          cp_async<16>(d16 + St::kV + i * 512, Vc + i * 512);
         }
-        q4_cp<St::kScaleRow>(ds + St::kKs, Ks);
-        q4_cp<St::kScaleRow>(ds + St::kVs, Vs);
+        cp_async<St::kScaleRow>(ds + St::kKs, Ks);
+        cp_async<St::kScaleRow>(ds + St::kVs, Vs);
       } else {  // rows past the count: zeros, nothing is read
 #pragma unroll 1
         for (int i = 0; i < kVecRow; ++i) {
           const int bytes = i * (32 / kVecRow) + cp_row < rows ? 16 : 0;
-          q4_cp_part<16>(d16 + i * 512, Kc + i * 512, bytes);
-          q4_cp_part<16>(d16 + St::kV + i * 512, Vc + i * 512, bytes);
+          cp_async_part<16>(d16 + i * 512, Kc + i * 512, bytes);
+          cp_async_part<16>(d16 + St::kV + i * 512, Vc + i * 512, bytes);
         }
         const int bytes = lane < rows ? St::kScaleRow : 0;
-        q4_cp_part<St::kScaleRow>(ds + St::kKs, Ks, bytes);
-        q4_cp_part<St::kScaleRow>(ds + St::kVs, Vs, bytes);
+        cp_async_part<St::kScaleRow>(ds + St::kKs, Ks, bytes);
+        cp_async_part<St::kScaleRow>(ds + St::kVs, Vs, bytes);
       }
     }
-    q4_cp_commit();
+    cp_async_commit();
     --ahead;
     rows -= row_step;
     Kc += code_step;
@@ -702,7 +548,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
   bool fresh = true;
   for (;;) {
     __syncwarp();
-    Q4Cursor ci = s_here[warp];
+    ListCursor ci = s_here[warp];
     const bool solo = alone(ci) || W == 1, my = mine(ci);
     if (my) {
       const int n = keys_of(ci.layer), step = (solo ? 1 : W) * kQ4Block, k_end = ci.end * kQ4Block;
@@ -713,7 +559,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
       fresh = false;
 #pragma unroll 1
       for (; kb < k_end; kb += step) {
-        q4_cp_wait<kQ4Stages - 1>();
+        cp_async_wait<kQ4Stages - 1>();
         __syncwarp();
         st.block(ring + stage * St::kBytes, off, q_at, kb, n, lane);
         __syncwarp();
@@ -737,7 +583,7 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
         for (int w = w0; w < w1; ++w) {
           const float4 x = *reinterpret_cast<const float4*>(s_vals + (w * GP + g) * D + e0);
           const float v2[4] = {x.x, x.y, x.z, x.w};
-          q4_merge_state<4>(mm, ll, v, s_ml[w][2 * g], s_ml[w][2 * g + 1], v2);
+          merge_state<4>(mm, ll, v, s_ml[w][2 * g], s_ml[w][2 * g + 1], v2);
         }
         if (whole) {
           *reinterpret_cast<float4*>(a.out[ci.layer] + (size_t)(ci.h * G + g) * D + e0) =
@@ -770,14 +616,14 @@ __global__ void __launch_bounds__(kQ4DecThreads, kQ4DecCtasPerSm) q4_decode_kern
 template <int D, int NW>
 __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q4_merge_kernel(const __grid_constant__ Q4DecodeArgs a) {
   constexpr int PER = D / 32, kInFlight = NW == 1 ? 4 : NW, kItems = NW == 1 ? 4 : 1;
-  __shared__ Q4Lists s_list;
+  __shared__ ListCounts s_list;
   __shared__ float s_ml[NW][2];
   __shared__ float s_v[NW][D];
   const int warp = NW == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int item = blockIdx.x * kItems + (NW == 1 ? threadIdx.x >> 5 : 0);
-  const bool uniform = q4_uniform(a);
+  const bool uniform = list_uniform(a);
   if (!uniform) {
-    if (threadIdx.x < 32) q4_lists(a, s_list, false);
+    if (threadIdx.x < 32) list_counts(a, s_list, false);
     __syncthreads();
   }
   int g, h;
@@ -785,16 +631,16 @@ __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q4_merge_kernel(const
   if (layer >= a.n_layers) return;  // NW == 1: past the last pair
   int n, first, total;  // keys of the pair's cache, its first block in the list, all blocks
   if (uniform) {
-    n = q4_keys(a, 0);
-    first = layer * a.Hkv * q4_blocks(n);
-    total = a.n_layers * a.Hkv * q4_blocks(n);
+    n = list_keys(a, 0);
+    first = layer * a.Hkv * list_blocks(n);
+    total = a.n_layers * a.Hkv * list_blocks(n);
   } else {
     n = s_list.n[layer];
     first = s_list.first[layer];
     total = s_list.first[a.n_layers];
   }
-  const int nb = q4_blocks(n);
-  const Q4Split sp = q4_split(a, uniform, nb, total);
+  const int nb = list_blocks(n);
+  const ListSplit sp = list_split(a, uniform, nb, total);
   int slot = 0, count = 0;
   if (nb > 0 && sp.k > 0) {
     slot = pair * sp.k;
@@ -830,7 +676,7 @@ __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q4_merge_kernel(const
         for (int e = 0; e < PER; ++e) a2[u][e] = ok ? __ldcg(src + 4 + e * 32 + lane) : 0.f;
       }
 #pragma unroll
-      for (int u = 0; u < kInFlight; ++u) q4_merge_state<PER>(mm, ll, aa, ml[u].x, ml[u].y, a2[u]);
+      for (int u = 0; u < kInFlight; ++u) merge_state<PER>(mm, ll, aa, ml[u].x, ml[u].y, a2[u]);
     }
     if constexpr (NW == 1) {
       if (live)
@@ -849,7 +695,7 @@ __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q4_merge_kernel(const
 #pragma unroll 1
         for (int w = 0; w < NW; ++w) {
           const float v2[1] = {s_v[w][threadIdx.x]};
-          q4_merge_state<1>(m1, l1, v1, s_ml[w][0], s_ml[w][1], v2);
+          merge_state<1>(m1, l1, v1, s_ml[w][0], s_ml[w][1], v2);
         }
         if (live) out[threadIdx.x] = v1[0] / l1;
       }
@@ -861,7 +707,7 @@ __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q4_merge_kernel(const
 // A pair of n rows leaves at most one slot per block, and all pairs together at most one per group and pair.
 size_t q4_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap) {
   const int64_t pairs = (int64_t)n_layers * Hkv, blocks = pairs * (((int64_t)n_cap + kQ4Block - 1) / kQ4Block);
-  return (size_t)(std::min<int64_t>(kQ4MaxGroups, blocks) + pairs) * (Hq / Hkv) * (d + 4) * sizeof(float);
+  return (size_t)(std::min<int64_t>(kListMaxGroups, blocks) + pairs) * (Hq / Hkv) * (d + 4) * sizeof(float);
 }
 
 // Warps that take a pair whole, which needs no partial states and no second kernel (1.5 to 4 us of a call), or 0; by the most
@@ -918,7 +764,7 @@ stepkv_status_t q4_decode_run(const stepkv_q4_cache_t& c, const void* const* q, 
     a.G = Hq / c.Hkv;
     // as many groups as run at once, none without a block
     const int64_t blocks = (int64_t)nl * c.Hkv * ((n_cap + kQ4Block - 1) / kQ4Block);
-    const int slots = std::min(kQ4MaxGroups / kQ4DecWarps, n_sm * kQ4DecCtasPerSm);
+    const int slots = std::min(kListMaxGroups / kQ4DecWarps, n_sm * kQ4DecCtasPerSm);
     a.n_groups = (int)std::min<int64_t>(slots, blocks);
     a.whole = q4_whole(nl * c.Hkv, slots, ((n_dev ? n_cap : n_host) + kQ4Block - 1) / kQ4Block, n_dev && n_stride && nl > 1);
     if (a.whole) a.n_groups = (nl * c.Hkv * a.whole + kQ4DecWarps - 1) / kQ4DecWarps;

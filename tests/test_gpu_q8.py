@@ -443,7 +443,7 @@ def test_decode_forms_and_counts(B, L, Hkv, G, d, rows):
                 assert not out[same].any()
 
 
-@pytest.mark.parametrize("magnitude", [2.0 ** -90, 1e-20, 1e-3, 1.0, 1e3, 1e20, 2.0 ** 90])
+@pytest.mark.parametrize("magnitude", [2.0 ** -110, 2.0 ** -90, 1e-20, 1e-3, 1.0, 1e3, 1e20, 2.0 ** 90, 2.0 ** 118])
 def test_decode_keys_queries_and_values_of_any_magnitude(B, magnitude):
     """Keys of any magnitude with queries that make up for it; and values of it."""
     import torch
