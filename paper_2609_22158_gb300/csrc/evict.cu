@@ -3,13 +3,14 @@
 //   retained     = the first `keep` by (protected, mass descending, slot ascending)
 //   the i-th slot below keep that goes receives the i-th slot at or above keep that stays
 //
-// Two kernels.  The first, a CTA per (layer, head), finds the retained rows from n masses and positions, writes the list of
-// moves, and moves masses and positions; the second moves rows of keys and values over the whole machine.  In 8 bits it moves
-// them block by block, as the block's scale may have to grow.
+// A CTA takes a (layer, head): it finds the retained rows from n masses and positions, makes the list of moves, and moves masses
+// and positions.  Where there are enough heads to fill the machine it moves the rows of keys and values too, in one launch;
+// else a second kernel moves them over the whole machine.  In 8 bits a block that receives rows may have to take a larger scale.
 //
 // A row's rank is a 32-bit key: all ones where it is protected, else the mass as an integer that orders like the number (0 for
-// a NaN).  The key T of the last retained row comes from three histograms of 11, 11 and 10 bits; with R(j) = min(rows below j
-// that equal T, those of them that stay) + rows below j above T, the retained rows below slot j,
+// a NaN).  Keys stay in registers, a warp's being consecutive slots.  The key T of the last retained row comes from histograms
+// of 11, 11 and 10 bits, as many as it takes; with R(j) = min(rows below j that equal T, those of them that stay) + rows below
+// j above T, the retained rows below slot j,
 //   a slot j < keep that goes is number j - R(j) of those, a slot j >= keep that stays number R(j) - R(keep).
 #include <limits.h>
 
@@ -22,21 +23,27 @@
 
 namespace stepkv {
 
-constexpr int kEvictThreads = 1024;
-constexpr int kEvictWarps = kEvictThreads / 32;
-constexpr int kEvictSmemKeys = 49152;  // keys held in shared memory (192 KB); the rest are made anew in every pass
+constexpr int kEvictLongThreads = 1024;    // of a head of more than kEvictShort rows
+constexpr int kEvictShortThreads = 512;
+constexpr int kEvictShort = 32 * kEvictShortThreads;
+constexpr int kEvictSmemKeys = 49152;      // heads too long for registers: keys held in shared memory (192 KB), the rest made anew
 constexpr uint32_t kEvictProtected = 0xFFFFFFFFu;
 
 struct EvictArgs {
   float* mass[kQ8Layers];
   int32_t* pos[kQ8Layers];
-  const float* K_scale[kQ8Layers];  // 8 bits: read before the moves where a block is cut by `keep`
-  const float* V_scale[kQ8Layers];
-  int64_t mass_stride, pos_stride, scale_stride;
-  int layer0, Hkv;
+  uint8_t* K[kQ8Layers];            // bf16 rows, or codes
+  uint8_t* V[kQ8Layers];
+  float* K_scale[kQ8Layers];        // 8 bits
+  float* V_scale[kQ8Layers];
+  int64_t mass_stride, pos_stride, head_bytes, scale_stride;
+  int layer0, n_layers, Hkv;
+  int row_bytes;
   const int32_t* n_dev;
   int n_stride, n_host, n_cap, keep, n_sink, n_recent;
   int smem_keys;
+  int moves_rows;   // this launch moves keys and values
+  int32_t* n_out;   // NULL: not this launch
   // workspace, per (layer, head):
   int2* plan;       // [plan_cap]: (slot filled, slot it is filled from), both ascending
   int2* blocks;     // [block_cap], 8 bits: (block, number of its first move * 64 + moves) of blocks that receive rows, in any order
@@ -52,34 +59,216 @@ __device__ __forceinline__ uint32_t evict_key(float mass, int pos, int n_sink, i
   return mass == mass ? float_to_ordered(mass + 0.f) : 0u;  // (-0 + 0 is 0)
 }
 
-// Inclusive sums over the CTA's threads; s_warp: 32 words.  Two barriers.
-__device__ __forceinline__ uint32_t evict_scan(uint32_t x, uint32_t* s_warp) {
+// The bin of the histogram (2048 bins, counted from the top) in which the `ties`-th key lies, and its number there; `count`: the
+// keys of that bin.  All threads get them; one barrier, after the counting's.
+template <int NT>
+__device__ __forceinline__ uint32_t evict_bin(const uint32_t* hist, uint32_t* s_total, uint32_t& ties, uint32_t& count) {
+  constexpr int NW = NT / 32, BPL = 2048 / NT, SEG = 32 * BPL;  // bins a lane, a warp
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  uint32_t sum = 0;
+#pragma unroll
+  for (int i = 0; i < BPL; ++i) sum += hist[warp * SEG + i * 32 + lane];
+  sum = __reduce_add_sync(0xffffffffu, sum);
+  if (lane == 0) s_total[warp] = sum;
+  __syncthreads();
+  // (every warp by itself from here on) the warp's part, from the top
+  uint32_t t = lane < NW ? s_total[NW - 1 - lane] : 0u, upto = t;
 #pragma unroll
   for (int o = 1; o < 32; o <<= 1) {
-    const uint32_t y = __shfl_up_sync(0xffffffffu, x, o);
-    if (lane >= o) x += y;
+    const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+    if (lane >= o) upto += y;
   }
-  if (lane == 31) s_warp[warp] = x;
-  __syncthreads();
-  uint32_t w = s_warp[lane];
-  const uint32_t before = __reduce_add_sync(0xffffffffu, lane < warp ? w : 0u);
-  __syncthreads();
-  return x + before;
+  const int at = __ffs(__ballot_sync(0xffffffffu, upto >= ties)) - 1;
+  ties -= __shfl_sync(0xffffffffu, upto - t, at);
+  const int seg = NW - 1 - at;
+  // its bins, 32 at a time from the top
+  uint32_t bin = 0;
+  count = 0;
+#pragma unroll
+  for (int i = BPL - 1; i >= 0; --i) {
+    if (count) continue;
+    t = hist[seg * SEG + i * 32 + 31 - lane];
+    upto = t;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const uint32_t y = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += y;
+    }
+    const uint32_t hit = __ballot_sync(0xffffffffu, upto >= ties);
+    if (hit) {
+      const int l = __ffs(hit) - 1;
+      ties -= __shfl_sync(0xffffffffu, upto - t, l);
+      count = __shfl_sync(0xffffffffu, t, l);
+      bin = seg * SEG + i * 32 + 31 - l;
+    } else {
+      ties -= __shfl_sync(0xffffffffu, upto, 31);
+    }
+  }
+  return bin;
 }
 
-template <bool Q8>
-__global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __grid_constant__ EvictArgs a) {
-  extern __shared__ uint32_t s_key[];
-  __shared__ uint32_t s_hist[2048];
-  __shared__ uint32_t s_warp[kEvictWarps];
-  __shared__ uint4 s_count[kEvictWarps];
-  __shared__ int s_top[kEvictWarps];
-  __shared__ uint32_t s_bin, s_rem, s_safe, s_blocks;
+// Rows of bf16 by one CTA, 16 bytes a lane.
+template <int NT>
+__device__ __forceinline__ void evict_move_rows(const EvictArgs& a, const int2* plan, int moves, int layer, int h) {
+  constexpr int U = 6;
+  const int lpr = a.row_bytes >> 4, rpi = 32 / lpr;  // lanes a row, rows an instruction
+  const int lane = threadIdx.x & 31, sub = lane / lpr, col = lane - sub * lpr;
+  const int per_chunk = rpi * U, chunks = (moves + per_chunk - 1) / per_chunk;
+  for (int c = threadIdx.x >> 5; c < 2 * chunks; c += NT / 32) {
+    const bool v_rows = c >= chunks;
+    const int i0 = (v_rows ? c - chunks : c) * per_chunk + sub;
+    uint8_t* rows = (v_rows ? a.V : a.K)[layer] + h * a.head_bytes + col * 16;
+    int2 p[U];
+    uint4 v[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      p[u] = make_int2(-1, -1);
+      if (sub < rpi && i0 + u * rpi < moves) p[u] = plan[i0 + u * rpi];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (p[u].y >= 0) v[u] = q8_ld_stream(rows + (int64_t)p[u].y * a.row_bytes);
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (p[u].x >= 0) q8_st_stream(rows + (int64_t)p[u].x * a.row_bytes, v[u]);
+  }
+}
+
+// The largest magnitude of 16 codes (NaN does not count), as a code.
+__device__ __forceinline__ uint32_t evict_top_code(const uint4& v) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+  uint32_t top = 0;  // magnitudes order as integers
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    const uint32_t m = w[i] & 0x7F7F7F7Fu;
+    top = __vmaxu4(top, m & ~__vcmpeq4(m, 0x7F7F7F7Fu));
+  }
+  return max(max(top & 0xFFu, top >> 8 & 0xFFu), max(top >> 16 & 0xFFu, top >> 24));
+}
+__device__ __forceinline__ uint4 evict_rescale(const uint4& v, float ratio) {
+  return make_uint4(q8_rescale(v.x, ratio), q8_rescale(v.y, ratio), q8_rescale(v.z, ratio), q8_rescale(v.w, ratio));
+}
+
+// Rows of an 8-bit cache by one CTA, row by row: what the blocks need of the rows they receive, then their scales, then the rows.
+// s_scale: [2][blocks], zeroed, holes: the slots of each block that are filled.
+template <int D, int NT>
+__device__ __forceinline__ void evict_move_codes(const EvictArgs& a, const int2* plan, int moves, int layer, int h, float* s_scale,
+                                                 const uint32_t* s_holes, const float (&cut)[2]) {
+  constexpr int LPR = D / 16, RPI = 32 / LPR, U = 4, kChunk = RPI * U;
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / LPR, col = lane & (LPR - 1);
+  const int chunks = (moves + kChunk - 1) / kChunk, nblk = (a.keep + kQ8Block - 1) / kQ8Block;
+  const int cut_block = a.keep % kQ8Block ? a.keep / kQ8Block : -1;
+#pragma unroll 1
+  for (int phase = 0; phase < 2; ++phase) {
+    for (int c = warp; c < 2 * chunks; c += NT / 32) {
+      const int z = c >= chunks;
+      const int i0 = (z ? c - chunks : c) * kChunk + sub;
+      uint8_t* rows = (z ? a.V : a.K)[layer] + h * a.head_bytes + col * 16;
+      const float* scale = (z ? a.V_scale : a.K_scale)[layer] + h * a.scale_stride;
+      int2 p[U];
+      uint4 v[U];
+      float from[U];
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        p[u] = make_int2(-1, -1);
+        if (i0 + u * RPI < moves) p[u] = plan[i0 + u * RPI];
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        v[u] = make_uint4(0, 0, 0, 0);
+        from[u] = 0.f;
+        if (p[u].y >= 0) {
+          const int b = p[u].y / kQ8Block;
+          v[u] = __ldcg(reinterpret_cast<const uint4*>(rows + (int64_t)p[u].y * D));
+          from[u] = b == cut_block ? cut[z] : __ldcg(scale + b);  // (that block's scale may have grown)
+        }
+      }
+      if (phase == 0) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          float most = q8_float2(evict_top_code(v[u])).x * from[u];
+#pragma unroll
+          for (int o = 1; o < LPR; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+          if (col == 0 && p[u].x >= 0)  // (positive numbers order as integers)
+            atomicMax(reinterpret_cast<unsigned*>(s_scale) + z * nblk + p[u].x / kQ8Block, __float_as_uint(most));
+        }
+      } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+          if (p[u].x < 0) continue;
+          const float s = s_scale[z * nblk + p[u].x / kQ8Block];
+          if (from[u] != s) v[u] = evict_rescale(v[u], from[u] * q8_inverse(s));
+          *reinterpret_cast<uint4*>(rows + (int64_t)p[u].x * D) = v[u];
+        }
+      }
+    }
+    __syncthreads();
+    if (phase == 1) break;
+    // the blocks' scales; where one grows, the rows that stay
+    for (int i0 = warp * 32; i0 < 2 * nblk; i0 += NT) {
+      const int i = i0 + lane, z = i >= nblk, b = z ? i - nblk : i;
+      float old = 0.f, s = 0.f;
+      if (i < 2 * nblk && s_holes[b]) {
+        float* scale = (z ? a.V_scale : a.K_scale)[layer] + h * a.scale_stride + b;
+        old = __ldcg(scale);
+        s = fmaxf(old, q8_scale(s_scale[i]));
+        s_scale[i] = s;
+        if (old < s) *scale = s;
+      }
+      uint32_t grows = __ballot_sync(0xffffffffu, old < s);
+      while (grows) {
+        const int l = __ffs(grows) - 1, k = i0 + l, y = k >= nblk, block = y ? k - nblk : k;
+        grows &= grows - 1;
+        const float ratio = __shfl_sync(0xffffffffu, old, l) * q8_inverse(__shfl_sync(0xffffffffu, s, l));
+        const int end = min(kQ8Block, a.keep - block * kQ8Block);  // (rows at or past keep are only read)
+        const uint32_t filled = s_holes[block];
+        uint32_t* w = reinterpret_cast<uint32_t*>((y ? a.V : a.K)[layer] + h * a.head_bytes + (int64_t)block * (kQ8Block * D));
+        for (int e = lane; e < end * (D / 4); e += 32)
+          if (!(filled >> (e / (D / 4)) & 1u)) w[e] = q8_rescale(__ldcg(w + e), ratio);
+      }
+    }
+    __syncthreads();
+  }
+}
+
+// min(n, keep) of this launch's layers, where n_out is not what the launch's CTAs read n from.
+__device__ __forceinline__ void evict_counts(const EvictArgs& a, int threads) {
+  if (!a.n_out || blockIdx.x != 0) return;
+  const bool each = a.n_dev && a.n_stride;
+  for (int l = threadIdx.x; l < (each ? a.n_layers : 1); l += threads) {
+    const int at = each ? a.layer0 + l : 0;
+    const int n = a.n_dev ? __ldcg(a.n_dev + at) : a.n_host;
+    if (n >= 0 && n <= a.n_cap) a.n_out[at] = min(n, a.keep);
+  }
+}
+__global__ void evict_counts_kernel(const __grid_constant__ EvictArgs a) {
   pdl_wait();
   pdl_launch_dependents();
+  evict_counts(a, blockDim.x);
+}
+
+// DQ: 0: bf16, else the channels of a row of codes.  R: groups of 32 slots a warp holds in registers at most; 0: keys in shared
+// memory.
+template <int DQ, int NT, int R>
+__global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_select_kernel(const __grid_constant__ EvictArgs a) {
+  constexpr int NW = NT / 32, RR = R ? R : 1;
+  constexpr bool Q8 = DQ != 0;
+  extern __shared__ uint32_t s_key[];  // 8 bits: [2][blocks] scales, [blocks] holes; then keys (R = 0)
+  __shared__ uint32_t s_hist[3][2048];
+  __shared__ uint32_t s_total[2][NW];
+  __shared__ uint2 s_count[NW];
+  __shared__ uint32_t s_blocks;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
   const int pair = blockIdx.x, layer = pair / a.Hkv, h = pair - layer * a.Hkv;
+  const int keep = a.keep, nblk = Q8 ? (keep + kQ8Block - 1) / kQ8Block : 0;
+  for (int i = t; i < 3 * 2048; i += NT) s_hist[0][i] = 0;
+  for (int i = t; i < 2 * nblk; i += NT) s_key[i] = 0;
+  uint32_t* s_holes = s_key + 2 * nblk;
+  uint32_t* s_keys = s_holes + nblk;
+  if (t == 0) s_blocks = 0;
+  pdl_wait();
+  pdl_launch_dependents();
+  evict_counts(a, NT);
   int n = a.n_host;
   if (a.n_dev) {
     n = __ldcg(a.n_dev + (a.layer0 + layer) * a.n_stride);
@@ -88,120 +277,179 @@ __global__ void __launch_bounds__(kEvictThreads) evict_select_kernel(const __gri
       n = 0;
     }
   }
-  const int keep = a.keep;
   if (n <= keep) {
     if (t == 0) a.counts[pair] = make_int2(0, 0);
     return;
   }
   float* mass = a.mass[layer] + (int64_t)h * a.mass_stride;
   int32_t* pos = a.pos[layer] + (int64_t)h * a.pos_stride;
+  // warp w: groups [w per, w per + per) of 32 slots
+  const int groups = (n + 31) / 32, per = (groups + NW - 1) / NW, g0 = warp * per, rounds = max(0, min(groups - g0, per));
+  const int first = g0 * 32 + lane;
+  uint32_t keys[RR];
 
   int top = INT_MIN;
-  for (int j = t; j < n; j += kEvictThreads) top = max(top, __ldcg(pos + j));
+  if (R) {
+#pragma unroll
+    for (int r = 0; r < RR; ++r) {
+      keys[r] = (uint32_t)INT_MIN;
+      if (r < rounds && first + r * 32 < n) keys[r] = (uint32_t)__ldcg(pos + first + r * 32);
+    }
+#pragma unroll
+    for (int r = 0; r < RR; ++r) top = max(top, (int)keys[r]);
+  } else {
+    for (int r = 0; r < rounds; ++r)
+      if (first + r * 32 < n) top = max(top, __ldcg(pos + first + r * 32));
+  }
   top = __reduce_max_sync(0xffffffffu, top);
-  if (lane == 0) s_top[warp] = top;
-  if (t == 0) s_safe = s_blocks = 0;
+  if (lane == 0) s_total[0][warp] = (uint32_t)top;
   __syncthreads();
-  top = __reduce_max_sync(0xffffffffu, s_top[lane]);
+  top = __reduce_max_sync(0xffffffffu, (int)s_total[0][lane & (NW - 1)]);
   const int64_t recent = (int64_t)top - a.n_recent;
   auto make_key = [&](int j) { return evict_key(__ldcg(mass + j), __ldcg(pos + j), a.n_sink, recent); };
   uint32_t safe = 0;
-  for (int j = t; j < n; j += kEvictThreads) {
-    const uint32_t k = make_key(j);
-    if (j < a.smem_keys) s_key[j] = k;
-    safe += k == kEvictProtected;
-  }
-  safe = __reduce_add_sync(0xffffffffu, safe);
-  if (lane == 0 && safe) atomicAdd(&s_safe, safe);
-  __syncthreads();
-  auto key = [&](int j) { return j < a.smem_keys ? s_key[j] : make_key(j); };
-
-  // the key of the last retained row, and how many of those that equal it stay
-  uint32_t T = kEvictProtected, ties = keep;
-  if ((int)s_safe < keep) {
-    uint32_t mask = 0;
-    T = 0;
-    ties = keep - s_safe;
-#pragma unroll 1
-    for (int pass = 0; pass < 3; ++pass) {
-      const int shift = pass == 0 ? 21 : pass == 1 ? 10 : 0;
-      const uint32_t digits = pass == 2 ? 1023u : 2047u;
-      s_hist[t] = s_hist[t + kEvictThreads] = 0;
-      __syncthreads();
-      for (int j = t; j < n; j += kEvictThreads) {
-        const uint32_t k = key(j);
-        if ((k & mask) == T && k != kEvictProtected) atomicAdd(&s_hist[k >> shift & digits], 1u);
+  if (R) {
+    constexpr int kBatch = RR < 8 ? RR : 8;
+#pragma unroll
+    for (int r0 = 0; r0 < RR; r0 += kBatch) {
+      asm volatile("" ::: "memory");  // (a batch's loads at a time: all at once take another register a group)
+      float m[kBatch];
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r) {
+        m[r] = 0.f;
+        if (r0 + r < RR && r0 + r < rounds && first + (r0 + r) * 32 < n) m[r] = __ldcg(mass + first + (r0 + r) * 32);
       }
-      __syncthreads();
-      const uint32_t first = s_hist[2047 - 2 * t], second = s_hist[2046 - 2 * t];  // bins from the top
-      const uint32_t upto = evict_scan(first + second, s_warp), above = upto - first - second;
-      if (above < ties && ties <= upto) {
-        const bool in_first = ties <= above + first;
-        s_bin = in_first ? 2047 - 2 * t : 2046 - 2 * t;
-        s_rem = ties - above - (in_first ? 0 : first);
-      }
-      __syncthreads();
-      T |= s_bin << shift;
-      mask |= digits << shift;
-      ties = s_rem;
+#pragma unroll
+      for (int r = 0; r < kBatch; ++r)
+        if (r0 + r < RR)
+          keys[r0 + r] = first + (r0 + r) * 32 < n ? evict_key(m[r], (int)keys[r0 + r], a.n_sink, recent) : 0u;
+    }
+  } else {
+    for (int r = 0; r < rounds; ++r) {
+      const int j = first + r * 32;
+      if (j < n && j < a.smem_keys) s_keys[j] = make_key(j);
     }
   }
-
-  // rows above T and equal to it: of each warp's part of the slots, and of those below keep
-  const int groups = (n + 31) / 32, per_warp = (groups + kEvictWarps - 1) / kEvictWarps;
-  const int g0 = min(groups, warp * per_warp), g1 = min(groups, g0 + per_warp);
-  uint4 c = make_uint4(0, 0, 0, 0);
-  for (int g = g0; g < g1; ++g) {
-    const int j = g * 32 + lane;
-    const uint32_t k = j < n ? key(j) : 0u;
-    const uint32_t gt = __ballot_sync(0xffffffffu, j < n && k > T), eq = __ballot_sync(0xffffffffu, j < n && k == T);
-    const uint32_t low = __ballot_sync(0xffffffffu, j < keep);
-    c.x += __popc(gt);
-    c.y += __popc(eq);
-    c.z += __popc(gt & low);
-    c.w += __popc(eq & low);
-  }
-  if (lane == 0) s_count[warp] = c;
+  // f(key, slot) for this lane's slots below n; the whole warp at once
+  auto each = [&](auto f) {
+#pragma unroll
+    for (int r = 0; r < (R ? RR : rounds); ++r) {
+      if (r < rounds) {
+        const int j = first + r * 32;
+        const bool in = j < n;
+        uint32_t k = 0;
+        if (R) k = keys[R ? r : 0];
+        else if (in) k = j < a.smem_keys ? s_keys[j] : make_key(j);
+        f(k, j, in);
+      }
+    }
+  };
+  // the first histogram, and the protected rows
+  each([&](uint32_t k, int, bool in) {
+    const bool p = in && k == kEvictProtected;
+    safe += p;
+    if (in && !p) atomicAdd(&s_hist[0][k >> 21], 1u);
+  });
+  safe = __reduce_add_sync(0xffffffffu, safe);
+  if (lane == 0) s_total[1][warp] = safe;
   __syncthreads();
-  const uint4 mine = s_count[lane];
-  uint32_t gt0 = __reduce_add_sync(0xffffffffu, lane < warp ? mine.x : 0u);
-  uint32_t eq0 = __reduce_add_sync(0xffffffffu, lane < warp ? mine.y : 0u);
-  const uint32_t gt_low = __reduce_add_sync(0xffffffffu, mine.z), eq_low = __reduce_add_sync(0xffffffffu, mine.w);
+  safe = __reduce_add_sync(0xffffffffu, lane < NW ? s_total[1][lane] : 0u);
+
+  // the last retained row's key T under a mask, and how many of those that equal it stay
+  uint32_t T = kEvictProtected, mask = 0xFFFFFFFFu, ties = keep, count = safe;
+  if ((int)safe < keep) {
+    ties = keep - safe;
+    T = evict_bin<NT>(s_hist[0], s_total[0], ties, count) << 21;
+    mask = 0xFFE00000u;
+    if (ties < count) {
+      each([&](uint32_t k, int, bool in) {
+        if (in && (k & mask) == T) atomicAdd(&s_hist[1][k >> 10 & 2047u], 1u);
+      });
+      __syncthreads();
+      T |= evict_bin<NT>(s_hist[1], s_total[1], ties, count) << 10;
+      mask = 0xFFFFFC00u;
+    }
+    if (ties < count) {
+      each([&](uint32_t k, int, bool in) {
+        if (in && (k & mask) == T) atomicAdd(&s_hist[2][k & 1023u], 1u);
+      });
+      __syncthreads();
+      T |= evict_bin<NT>(s_hist[2], s_total[0], ties, count);
+      mask = 0xFFFFFFFFu;
+    }
+  }
+  // Rows above T, and equal to it under the mask: of each warp's slots, and of those below keep.  (No key but a protected row's
+  // reaches 0xFFE00000, so that one stays above a T under any mask.)  Where all that equal T stay, a row stays if its key is
+  // not below T, and the slots behind the last, whose keys are 0, do not count.
+  const bool all_equal = ties >= count && T != 0;
+  uint32_t here = 0, low = 0;  // above + 2^16 equal
+  each([&](uint32_t k, int j, bool in) {
+    uint32_t x;
+    if (all_equal) x = k >= T;
+    else x = in && (k & mask) > T ? 1u : in && (k & mask) == T ? 65536u : 0u;
+    here += x;
+    if (j < keep) low += x;
+  });
+  const uint32_t below = (1u << lane) - 1u;
+  here = __reduce_add_sync(0xffffffffu, here);
+  low = __reduce_add_sync(0xffffffffu, low);
+  if (lane == 0) s_count[warp] = make_uint2(here, low);
+  __syncthreads();
+  const uint2 mine = lane < NW ? s_count[lane] : make_uint2(0, 0);
+  uint32_t gt0 = __reduce_add_sync(0xffffffffu, lane < warp ? mine.x & 0xFFFFu : 0u);
+  uint32_t eq0 = __reduce_add_sync(0xffffffffu, lane < warp ? mine.x >> 16 : 0u);
+  const uint32_t gt_low = __reduce_add_sync(0xffffffffu, mine.y & 0xFFFFu), eq_low = __reduce_add_sync(0xffffffffu, mine.y >> 16);
   const int kept_low = gt_low + min(eq_low, ties), moves = keep - kept_low;
   int2* plan = a.plan + (int64_t)pair * a.plan_cap;
   int2* blocks = a.blocks + (int64_t)pair * a.block_cap;
-  for (int g = g0; g < g1; ++g) {
-    const int j = g * 32 + lane;
-    const uint32_t k = j < n ? key(j) : 0u;
-    const uint32_t gt = __ballot_sync(0xffffffffu, j < n && k > T), eq = __ballot_sync(0xffffffffu, j < n && k == T);
-    const uint32_t below = (1u << lane) - 1u;
-    const uint32_t eqb = eq0 + __popc(eq & below);
-    const bool stays = (gt >> lane & 1u) || ((eq >> lane & 1u) && eqb < ties);
-    const int R = gt0 + __popc(gt & below) + min(eqb, ties);
+  each([&](uint32_t k, int j, bool in) {
+    bool stays;
+    int kept;  // R(j)
+    if (all_equal) {
+      stays = k >= T;
+      const uint32_t ge = __ballot_sync(0xffffffffu, stays);
+      kept = gt0 + __popc(ge & below);
+      gt0 += __popc(ge);
+    } else {
+      const uint32_t gt = __ballot_sync(0xffffffffu, in && (k & mask) > T), eq = __ballot_sync(0xffffffffu, in && (k & mask) == T);
+      const uint32_t eqb = eq0 + __popc(eq & below);
+      stays = (gt >> lane & 1u) || ((eq >> lane & 1u) && eqb < ties);
+      kept = gt0 + __popc(gt & below) + min(eqb, ties);
+      gt0 += __popc(gt);
+      eq0 += __popc(eq);
+    }
     const bool hole = j < keep && !stays;
-    if (hole) plan[j - R].x = j;
-    if (j >= keep && stays) plan[R - kept_low].y = j;
+    if (hole) plan[j - kept].x = j;
+    if (j >= keep && stays) plan[kept - kept_low].y = j;
     if (Q8) {
       const uint32_t holes = __ballot_sync(0xffffffffu, hole);
-      if (lane == 0 && holes) blocks[atomicAdd(&s_blocks, 1u)] = make_int2(g, (g * 32 - R) * 64 + __popc(holes));
+      if (lane == 0 && j < keep) {
+        s_holes[j / kQ8Block] = holes;
+        if (holes && !a.moves_rows) blocks[atomicAdd(&s_blocks, 1u)] = make_int2(j / kQ8Block, (j - kept) * 64 + __popc(holes));
+      }
     }
-    gt0 += __popc(gt);
-    eq0 += __popc(eq);
+  });
+  float cut[2] = {0.f, 0.f};
+  if (Q8 && keep % kQ8Block) {
+    cut[0] = __ldcg(a.K_scale[layer] + (int64_t)h * a.scale_stride + keep / kQ8Block);
+    cut[1] = __ldcg(a.V_scale[layer] + (int64_t)h * a.scale_stride + keep / kQ8Block);
   }
   __syncthreads();
-  if (t == 0) {
+  if (t == 0 && !a.moves_rows) {
     a.counts[pair] = make_int2(moves, s_blocks);
-    if (Q8 && keep % kQ8Block)
-      a.cut[pair] = make_float2(__ldcg(a.K_scale[layer] + (int64_t)h * a.scale_stride + keep / kQ8Block),
-                                __ldcg(a.V_scale[layer] + (int64_t)h * a.scale_stride + keep / kQ8Block));
+    if (Q8) a.cut[pair] = make_float2(cut[0], cut[1]);
   }
-  for (int i = t; i < moves; i += kEvictThreads) {
+  for (int i = t; i < moves; i += NT) {
     const int2 p = plan[i];
     mass[p.x] = __ldcg(mass + p.y);
     pos[p.x] = __ldcg(pos + p.y);
   }
   __syncthreads();
-  for (int j = keep + t; j < n; j += kEvictThreads) mass[j] = 0.f;
+  for (int j = keep + t; j < n; j += NT) mass[j] = 0.f;
+  if (a.moves_rows) {
+    if constexpr (Q8) evict_move_codes<DQ, NT>(a, plan, moves, layer, h, reinterpret_cast<float*>(s_key), s_holes, cut);
+    else evict_move_rows<NT>(a, plan, moves, layer, h);
+  }
 }
 
 struct EvictMoveArgs {
@@ -224,7 +472,7 @@ struct EvictMoveArgs {
 static_assert(sizeof(EvictMoveArgs) <= 32000, "kernel parameter space");
 
 // min(n, keep) of this launch's layers.  (n_out may be n_dev: nothing else reads it here.)
-__device__ __forceinline__ void evict_counts(const EvictMoveArgs& a) {
+__device__ __forceinline__ void evict_move_counts(const EvictMoveArgs& a) {
   if (!a.n_out || blockIdx.x != 0) return;
   const bool each = a.n_dev && a.n_stride;
   for (int l = threadIdx.x; l < (each ? a.n_layers : 1); l += blockDim.x) {
@@ -240,7 +488,7 @@ constexpr int kEvictMoveUnroll = 4;
 __global__ void __launch_bounds__(kQ8Threads) evict_move_kernel(const __grid_constant__ EvictMoveArgs a) {
   pdl_wait();
   pdl_launch_dependents();
-  evict_counts(a);
+  evict_move_counts(a);
   if (a.plan_cap == 0) return;  // no head can have more than `keep`
   const int lpr = a.row_bytes >> 4, rpi = 32 / lpr;  // lanes a row, rows an instruction
   const int lane = threadIdx.x & 31, sub = lane / lpr, col = lane - sub * lpr;
@@ -276,7 +524,7 @@ __global__ void __launch_bounds__(kQ8Threads) evict_q8_move_kernel(const __grid_
   constexpr int LPR = D / 16, RPI = 32 / LPR, NI = kQ8Block / RPI;
   pdl_wait();
   pdl_launch_dependents();
-  evict_counts(a);
+  evict_move_counts(a);
   if (a.block_cap == 0) return;  // no head can have more than `keep`
   const int lane = threadIdx.x & 31, sub = lane / LPR, col = lane & (LPR - 1);
   for (Q8Chunks c(a.block_cap, a.sets); c.any(); c.next()) {
@@ -313,15 +561,7 @@ __global__ void __launch_bounds__(kQ8Threads) evict_q8_move_kernel(const __grid_
 #pragma unroll
     for (int u = 0; u < NI; ++u) {
       const float f = __shfl_sync(0xffffffffu, from, u * RPI + sub);
-      const uint32_t w[4] = {v[u].x, v[u].y, v[u].z, v[u].w};
-      uint32_t top = 0;  // magnitudes order as integers; NaN does not count
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const uint32_t m = w[i] & 0x7F7F7F7Fu;
-        top = __vmaxu4(top, m & ~__vcmpeq4(m, 0x7F7F7F7Fu));
-      }
-      top = max(max(top & 0xFFu, top >> 8 & 0xFFu), max(top >> 16 & 0xFFu, top >> 24));
-      most = fmaxf(most, q8_float2(top).x * f);
+      most = fmaxf(most, q8_float2(evict_top_code(v[u])).x * f);
     }
 #pragma unroll
     for (int o = 16; o; o >>= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
@@ -342,8 +582,7 @@ __global__ void __launch_bounds__(kQ8Threads) evict_q8_move_kernel(const __grid_
       const float f = __shfl_sync(0xffffffffu, from, u * RPI + sub);
       if (x >= 0) {
         if (f != s) {
-          const float ratio = f * q8_inverse(s);
-          v[u] = make_uint4(q8_rescale(v[u].x, ratio), q8_rescale(v[u].y, ratio), q8_rescale(v[u].z, ratio), q8_rescale(v[u].w, ratio));
+          v[u] = evict_rescale(v[u], f * q8_inverse(s));
         }
         *reinterpret_cast<uint4*>(codes + (int64_t)x * D + col * 16) = v[u];
       }
@@ -360,115 +599,137 @@ size_t evict_ws_bytes(int n_layers, int Hkv, int n_cap) {
          evict_align(pairs * sizeof(int2)) + evict_align(pairs * sizeof(float2));
 }
 
-static cudaError_t evict_launch(int nl, int l0, bool last, int Hkv, const EvictSpec& s, EvictMoveArgs& m, const float* const* K_scale,
-                                const float* const* V_scale, int64_t scale_stride, int d, bool q8, cudaStream_t stream) {
+// Whether a head's CTA moves its rows by itself: where heads fill half the machine (32 layers x 8 heads, 32768 to 8272 rows in bf16 382
+// -> 334 us, 8911 to 8272 in 8 bits 145 -> 45), or rows are few (24 x 2 heads, one row 9.4 -> 8.2).
+static bool evict_moves_rows(int pairs, int plan_cap, int n_sm) { return 2 * pairs >= n_sm || plan_cap <= 16; }
+
+// By the most rows a head can have.
+template <int DQ>
+static void (*evict_kernel(int n_most, int* threads))(EvictArgs) {
+  *threads = n_most <= kEvictShort ? kEvictShortThreads : kEvictLongThreads;
+  const int groups = (n_most + *threads - 1) / *threads;  // of 32 slots, a warp
+  if (n_most <= kEvictShort) {
+    if (groups <= 4) return evict_select_kernel<DQ, kEvictShortThreads, 4>;
+    if (groups <= 8) return evict_select_kernel<DQ, kEvictShortThreads, 8>;
+    if (groups <= 16) return evict_select_kernel<DQ, kEvictShortThreads, 16>;
+    if (groups <= 20) return evict_select_kernel<DQ, kEvictShortThreads, 20>;
+    return evict_select_kernel<DQ, kEvictShortThreads, 32>;
+  }
+  return groups <= 32 ? evict_select_kernel<DQ, kEvictLongThreads, 32> : evict_select_kernel<DQ, kEvictLongThreads, 0>;
+}
+
+// dq: 0: bf16 rows of row_bytes, else the channels of a row of codes.
+static stepkv_status_t evict_all(int n_layers, void* const* K, void* const* V, float* const* K_scale, float* const* V_scale,
+                                 int64_t head_bytes, int64_t scale_stride, int row_bytes, int Hkv, int dq, const EvictSpec& s,
+                                 cudaStream_t stream) {
   int n_sm = 0;
   cudaError_t e = device_sm_count(&n_sm);
-  if (e != cudaSuccess) return e;
-  EvictArgs a;
-  memset(&a, 0, sizeof(a));
-  for (int l = 0; l < nl; ++l) {
-    a.mass[l] = s.mass[l0 + l];
-    a.pos[l] = s.pos[l0 + l];
-    a.K_scale[l] = q8 ? K_scale[l0 + l] : nullptr;
-    a.V_scale[l] = q8 ? V_scale[l0 + l] : nullptr;
+  for (int l0 = 0; e == cudaSuccess && l0 < n_layers; l0 += kQ8Layers) {
+    const int nl = std::min(kQ8Layers, n_layers - l0), pairs = nl * Hkv;
+    const bool last = l0 + nl == n_layers;
+    EvictArgs a;
+    memset(&a, 0, sizeof(a));
+    for (int l = 0; l < nl; ++l) {
+      a.mass[l] = s.mass[l0 + l];
+      a.pos[l] = s.pos[l0 + l];
+      a.K[l] = static_cast<uint8_t*>(K[l0 + l]);
+      a.V[l] = static_cast<uint8_t*>(V[l0 + l]);
+      a.K_scale[l] = dq ? K_scale[l0 + l] : nullptr;
+      a.V_scale[l] = dq ? V_scale[l0 + l] : nullptr;
+    }
+    a.mass_stride = s.mass_stride;
+    a.pos_stride = s.pos_stride;
+    a.head_bytes = head_bytes;
+    a.scale_stride = scale_stride;
+    a.layer0 = l0;
+    a.n_layers = nl;
+    a.Hkv = Hkv;
+    a.row_bytes = row_bytes;
+    a.n_dev = s.n_dev;
+    a.n_stride = s.n_stride;
+    a.n_host = s.n_host;
+    a.n_cap = s.n_cap;
+    a.keep = s.keep;
+    a.n_sink = s.n_sink;
+    a.n_recent = s.n_recent;
+    const int n_most = s.n_dev ? s.n_cap : s.n_host;
+    a.plan_cap = std::max(0, std::min(s.keep, n_most - s.keep));
+    a.block_cap = std::min(a.plan_cap, (s.keep + kQ8Block - 1) / kQ8Block);
+    uint8_t* w = static_cast<uint8_t*>(s.ws);
+    a.plan = reinterpret_cast<int2*>(w);
+    w += evict_align((size_t)pairs * a.plan_cap * sizeof(int2));
+    a.blocks = reinterpret_cast<int2*>(w);
+    w += evict_align((size_t)pairs * a.block_cap * sizeof(int2));
+    a.counts = reinterpret_cast<int2*>(w);
+    w += evict_align((size_t)pairs * sizeof(int2));
+    a.cut = reinterpret_cast<float2*>(w);
+    a.status = s.status;
+    a.moves_rows = evict_moves_rows(pairs, a.plan_cap, n_sm);
+    // one count for all is read by every launch: replaced by the last; n itself only after all CTAs have read it
+    int32_t* const n_out = s.n_dev && s.n_stride ? s.n_out : last ? s.n_out : nullptr;
+    const bool late = n_out && n_out == s.n_dev;
+    a.n_out = late || !a.moves_rows ? nullptr : n_out;
+    int threads = 0;
+    auto select = dq == 0 ? evict_kernel<0>(n_most, &threads) : dq == 64 ? evict_kernel<64>(n_most, &threads) : evict_kernel<128>(n_most, &threads);
+    a.smem_keys = threads == kEvictLongThreads && n_most > 32 * kEvictLongThreads ? std::min(kEvictSmemKeys - (dq ? 8192 * 3 : 0), n_most) : 0;
+    const int smem = (a.smem_keys + (dq ? 3 * ((s.keep + kQ8Block - 1) / kQ8Block) : 0)) * (int)sizeof(uint32_t);
+    e = ensure_smem_attr(reinterpret_cast<const void*>(select), smem);
+    if (e == cudaSuccess) e = launch_kernel(select, dim3(pairs), dim3(threads), smem, stream, a, true);
+    if (e != cudaSuccess) break;
+    if (a.moves_rows) {
+      if (late) {
+        a.n_out = n_out;
+        e = launch_kernel(evict_counts_kernel, dim3(1), dim3(64), 0, stream, a, true);
+      }
+      continue;
+    }
+    EvictMoveArgs m;
+    memset(&m, 0, sizeof(m));
+    for (int l = 0; l < nl; ++l) {
+      m.rows[2 * l] = a.K[l];
+      m.rows[2 * l + 1] = a.V[l];
+      m.scale[2 * l] = a.K_scale[l];
+      m.scale[2 * l + 1] = a.V_scale[l];
+    }
+    m.head_bytes = head_bytes;
+    m.scale_stride = scale_stride;
+    m.by_heads = make_fastdiv(Hkv);
+    m.sets = 2 * pairs;
+    m.Hkv = Hkv;
+    m.n_layers = nl;
+    m.layer0 = l0;
+    m.row_bytes = row_bytes;
+    m.keep = s.keep;
+    m.plan_cap = a.plan_cap;
+    m.block_cap = a.block_cap;
+    m.plan = a.plan;
+    m.blocks = a.blocks;
+    m.counts = a.counts;
+    m.cut = a.cut;
+    m.n_dev = s.n_dev;
+    m.n_stride = s.n_stride;
+    m.n_host = s.n_host;
+    m.n_cap = s.n_cap;
+    m.n_out = n_out;
+    const int per_chunk = dq ? 1 : 32 / (row_bytes >> 4) * kEvictMoveUnroll;
+    const int64_t chunks = (int64_t)m.sets * (((dq ? m.block_cap : m.plan_cap) + per_chunk - 1) / per_chunk);
+    const int64_t ctas = (chunks + kQ8Threads / 32 - 1) / (kQ8Threads / 32);
+    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(n_sm * 4, ctas));
+    auto move = !dq ? evict_move_kernel : dq == 128 ? evict_q8_move_kernel<128> : evict_q8_move_kernel<64>;
+    e = launch_kernel(move, dim3(grid), dim3(kQ8Threads), 0, stream, m, true);
   }
-  a.mass_stride = s.mass_stride;
-  a.pos_stride = s.pos_stride;
-  a.scale_stride = scale_stride;
-  a.layer0 = l0;
-  a.Hkv = Hkv;
-  a.n_dev = s.n_dev;
-  a.n_stride = s.n_stride;
-  a.n_host = s.n_host;
-  a.n_cap = s.n_cap;
-  a.keep = s.keep;
-  a.n_sink = s.n_sink;
-  a.n_recent = s.n_recent;
-  const int n_most = s.n_dev ? s.n_cap : s.n_host;
-  a.smem_keys = std::min(kEvictSmemKeys, n_most);
-  const int pairs = nl * Hkv;
-  a.plan_cap = std::max(0, std::min(s.keep, n_most - s.keep));
-  a.block_cap = std::min(a.plan_cap, (s.keep + kQ8Block - 1) / kQ8Block);
-  uint8_t* w = static_cast<uint8_t*>(s.ws);
-  a.plan = reinterpret_cast<int2*>(w);
-  w += evict_align((size_t)pairs * a.plan_cap * sizeof(int2));
-  a.blocks = reinterpret_cast<int2*>(w);
-  w += evict_align((size_t)pairs * a.block_cap * sizeof(int2));
-  a.counts = reinterpret_cast<int2*>(w);
-  w += evict_align((size_t)pairs * sizeof(int2));
-  a.cut = reinterpret_cast<float2*>(w);
-  a.status = s.status;
-  auto select = q8 ? evict_select_kernel<true> : evict_select_kernel<false>;
-  const int smem = a.smem_keys * (int)sizeof(uint32_t);
-  e = ensure_smem_attr(reinterpret_cast<const void*>(select), smem);
-  if (e == cudaSuccess) e = launch_kernel(select, dim3(pairs), dim3(kEvictThreads), smem, stream, a, true);
-  if (e != cudaSuccess) return e;
-  m.by_heads = make_fastdiv(Hkv);
-  m.sets = 2 * pairs;
-  m.Hkv = Hkv;
-  m.n_layers = nl;
-  m.layer0 = l0;
-  m.keep = s.keep;
-  m.plan_cap = a.plan_cap;
-  m.block_cap = a.block_cap;
-  m.plan = a.plan;
-  m.blocks = a.blocks;
-  m.counts = a.counts;
-  m.cut = a.cut;
-  m.n_dev = s.n_dev;
-  m.n_stride = s.n_stride;
-  m.n_host = s.n_host;
-  m.n_cap = s.n_cap;
-  m.n_out = s.n_dev && s.n_stride ? s.n_out : last ? s.n_out : nullptr;  // (one count for all: read by every launch)
-  const int per_chunk = q8 ? 1 : 32 / (d >> 3) * kEvictMoveUnroll;
-  const int64_t chunks = (int64_t)m.sets * (((q8 ? m.block_cap : m.plan_cap) + per_chunk - 1) / per_chunk);
-  const int64_t ctas = (chunks + kQ8Threads / 32 - 1) / (kQ8Threads / 32);
-  const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(n_sm * 4, ctas));
-  auto move = !q8 ? evict_move_kernel : d == 128 ? evict_q8_move_kernel<128> : evict_q8_move_kernel<64>;
-  return launch_kernel(move, dim3(grid), dim3(kQ8Threads), 0, stream, m, true);
+  if (e == cudaSuccess) return STEPKV_OK;
+  set_last_cuda_error(e);
+  return STEPKV_ECUDA;
 }
 
 stepkv_status_t evict_run(int n_layers, void* const* K, void* const* V, int64_t kv_head_stride, int Hkv, int d,
                           const EvictSpec& s, cudaStream_t stream) {
-  cudaError_t e = cudaSuccess;
-  for (int l0 = 0; e == cudaSuccess && l0 < n_layers; l0 += kQ8Layers) {
-    const int nl = std::min(kQ8Layers, n_layers - l0);
-    EvictMoveArgs m;
-    memset(&m, 0, sizeof(m));
-    for (int l = 0; l < nl; ++l) {
-      m.rows[2 * l] = static_cast<uint8_t*>(K[l0 + l]);
-      m.rows[2 * l + 1] = static_cast<uint8_t*>(V[l0 + l]);
-    }
-    m.head_bytes = 2 * kv_head_stride;
-    m.row_bytes = 2 * d;
-    e = evict_launch(nl, l0, l0 + nl == n_layers, Hkv, s, m, nullptr, nullptr, 0, d, false, stream);
-  }
-  if (e == cudaSuccess) return STEPKV_OK;
-  set_last_cuda_error(e);
-  return STEPKV_ECUDA;
+  return evict_all(n_layers, K, V, nullptr, nullptr, 2 * kv_head_stride, 0, 2 * d, Hkv, 0, s, stream);
 }
 
 stepkv_status_t q8_evict_run(const stepkv_q8_cache_t& c, const EvictSpec& s, cudaStream_t stream) {
-  cudaError_t e = cudaSuccess;
-  for (int l0 = 0; e == cudaSuccess && l0 < c.n_layers; l0 += kQ8Layers) {
-    const int nl = std::min(kQ8Layers, c.n_layers - l0);
-    EvictMoveArgs m;
-    memset(&m, 0, sizeof(m));
-    for (int l = 0; l < nl; ++l) {
-      m.rows[2 * l] = static_cast<uint8_t*>(c.K[l0 + l]);
-      m.rows[2 * l + 1] = static_cast<uint8_t*>(c.V[l0 + l]);
-      m.scale[2 * l] = c.K_scale[l0 + l];
-      m.scale[2 * l + 1] = c.V_scale[l0 + l];
-    }
-    m.head_bytes = c.code_head_stride;
-    m.scale_stride = c.scale_head_stride;
-    m.row_bytes = c.d;
-    e = evict_launch(nl, l0, l0 + nl == c.n_layers, c.Hkv, s, m, c.K_scale, c.V_scale, c.scale_head_stride, c.d, true, stream);
-  }
-  if (e == cudaSuccess) return STEPKV_OK;
-  set_last_cuda_error(e);
-  return STEPKV_ECUDA;
+  return evict_all(c.n_layers, c.K, c.V, c.K_scale, c.V_scale, c.code_head_stride, c.scale_head_stride, c.d, c.Hkv, c.d, s, stream);
 }
 
 }  // namespace stepkv
