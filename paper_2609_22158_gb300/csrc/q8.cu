@@ -38,8 +38,13 @@ __device__ __forceinline__ int q8_count(const Q4Rows& r, int32_t* status) {
 
 // A warp takes a block of 32 rows: all of it in registers (64 a lane at d = 128), its largest magnitude by a reduction over
 // the warp, then the codes.  A lane has 8 consecutive channels of every 2nd (4th) row.
-template <int D, bool IDX>
-__global__ void __launch_bounds__(kQ8Threads) q8_write_kernel(const __grid_constant__ Q8Args a) {
+// CTAs an SM holds: two have the registers for all of a block's loads at once, which is faster where a warp has few blocks to take
+// (1 layer x 8 heads x 8272 rows 8.0 us, with three 10.1); with many, three (d = 64: four) keep more in flight (32 layers x
+// 8272 rows 271 -> 253 us = 6.4 TB/s, 639 rows 23.6 -> 21.1; 64 channels x 4000 rows 79 -> 65).
+constexpr int q8_write_ctas(int D, bool many) { return !many ? 2 : D == 128 ? 3 : 4; }
+constexpr int kQ8WriteFew = 3;  // blocks a warp
+template <int D, bool IDX, bool MANY>
+__global__ void __launch_bounds__(kQ8Threads, q8_write_ctas(D, MANY)) q8_write_kernel(const __grid_constant__ Q8Args a) {
   constexpr int LPR = D / 8, RPI = 32 / LPR, NI = kQ8Block / RPI;  // lanes a row, rows an instruction, instructions a block
   pdl_wait();
   pdl_launch_dependents();
@@ -141,8 +146,10 @@ __global__ void __launch_bounds__(kQ8Threads) q8_write_kernel(const __grid_const
   }
 }
 
-// A lane takes 8 codes of a row.
+// A lane takes 8 codes of a row.  32 layers x 8 heads x 8272 rows: 268 us = 6.1 TB/s, 64 layers x 4240 rows 6.2; two and eight rows of
+// a lane in flight, 3 to 16 CTAs an SM and plain stores 266-279.
 constexpr int kQ8ReadUnroll = 4;
+constexpr int kQ8ReadCtas = 4;
 
 template <int D, bool IDX>
 __global__ void __launch_bounds__(kQ8Threads) q8_read_kernel(const __grid_constant__ Q8Args a) {
@@ -243,9 +250,11 @@ static stepkv_status_t q8_rows_run(bool write, const stepkv_q8_cache_t& c, const
     const int per_chunk = write ? kQ8Block : 256 / D * kQ8ReadUnroll;
     const int64_t chunks = (int64_t)a.sets * ((rows.n + (write ? 2 * kQ8Block - 2 : per_chunk - 1)) / per_chunk);
     const int64_t ctas = (chunks + kQ8Threads / 32 - 1) / (kQ8Threads / 32);
-    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(n_sm * (write ? 2 : 4), ctas));
-    auto kern = write ? (rows.idx ? q8_write_kernel<D, true> : q8_write_kernel<D, false>)
-                      : (rows.idx ? q8_read_kernel<D, true> : q8_read_kernel<D, false>);
+    const bool many = write && ctas > kQ8WriteFew * n_sm * q8_write_ctas(D, false);
+    const int grid = (int)std::max<int64_t>(1, std::min<int64_t>(n_sm * (write ? q8_write_ctas(D, many) : kQ8ReadCtas), ctas));
+    auto kern = !write ? (rows.idx ? q8_read_kernel<D, true> : q8_read_kernel<D, false>)
+                : many ? (rows.idx ? q8_write_kernel<D, true, true> : q8_write_kernel<D, false, true>)
+                       : (rows.idx ? q8_write_kernel<D, true, false> : q8_write_kernel<D, false, false>);
     e = launch_kernel(kern, dim3(grid), dim3(kQ8Threads), 0, stream, a, true);
   }
   if (e == cudaSuccess) return STEPKV_OK;

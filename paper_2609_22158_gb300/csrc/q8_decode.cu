@@ -41,7 +41,6 @@ constexpr int kQ8DecThreads = kQ8DecWarps * 32;
 constexpr int kQ8DecCtasPerSm = 2;
 constexpr int kQ8DecMinSmem = 228 * 1024 / (kQ8DecCtasPerSm + 1);
 constexpr float kQ8WeightLog2 = 14.f;  // the largest weight is held as 2^14 (fp16 reaches 65504)
-constexpr int kQ8MassKeys = 1024;      // keys of a block of the mass pass
 static_assert(kListBlock == kQ8Block && kListLayers == kQ8Layers, "a warp step is a block of the cache");
 
 struct Q8DecodeArgs : DecodeList {
@@ -60,7 +59,7 @@ struct Q8DecodeArgs : DecodeList {
   float* logits;    // [pair][G][n_cap], log2 units, or NULL
   int whole;        // warps that take a pair, all of it: no states to join (0: the pairs are cut, list_split)
   int join_blocks;  // blocks of the second kernel that join states; those after them add to masses
-  FastDiv by_chunks;  // chunks of kQ8MassKeys of a pair
+  FastDiv by_chunks;  // chunks of keys of a pair, a block of the mass pass each
 };
 static_assert(sizeof(Q8DecodeArgs) <= 32000, "kernel parameter space");
 
@@ -171,14 +170,17 @@ struct Q8State {
     lds<8>(sc, stage + St::kScales);
     uint64_t s[4];   // key r8 + 8 i, both columns
     logits(s, stage + off, __uint_as_float(sc[0]) * c);
-    if (MASS && (GP == 8 || c4 < 2)) {
+    if constexpr (MASS) {  // (GP = 4: columns 4-7 are columns 0-3 again: their lanes keep the second half of the keys)
+      constexpr int kMine = GP == 4 ? 2 : 4;
+      const int col = GP == 4 ? 2 * (c4 & 1) : 2 * c4;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int j = kb + 8 * i + r8;
+      for (int i = 0; i < kMine; ++i) {
+        const bool second = GP == 4 && c4 >= 2;
+        const int j = kb + 8 * i + r8 + (second ? 16 : 0);
         float v[2];
-        f2_unpack(s[i], v[0], v[1]);
-        if (j < n && 2 * c4 < G) x[j] = v[0];
-        if (j < n && 2 * c4 + 1 < G) x[n_cap + j] = v[1];
+        f2_unpack(second ? s[(i + 2) & 3] : s[i], v[0], v[1]);
+        if (j < n && col < G) x[j] = v[0];
+        if (j < n && col + 1 < G) x[n_cap + j] = v[1];
       }
     }
     if (kb + kQ8Block > n) {
@@ -485,7 +487,7 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
     if (my) {
       const int n = keys_of(ci.layer), kstep = (solo ? 1 : W) * kQ8Block, k_end = ci.end * kQ8Block;
       int kb = (ci.blk + (solo ? 0 : rank)) * kQ8Block;
-      float* x = MASS ? a.logits + ((size_t)ci.pair * a.G + 2 * (lane & 3)) * a.n_cap : nullptr;
+      float* x = MASS ? a.logits + ((size_t)ci.pair * a.G + 2 * (lane & (GP == 4 ? 1 : 3))) * a.n_cap : nullptr;
       st.clear();
       if (kb < k_end) st.load_q(a.q[ci.layer] + (size_t)ci.h * a.G * D, a.G, lane);
 #pragma unroll 1
@@ -575,15 +577,33 @@ __device__ __forceinline__ Q8Slots q8_slots(const Q8DecodeArgs& a, const ListCou
   return r;
 }
 
-// The masses of a chunk of a pair's keys, from the logits and the joined (maximum, sum) of the pair's states.
-template <int D>
+// The masses of a chunk of a pair's keys, from the logits and the joined (maximum, sum) of the pair's states.  All loads of a
+// thread's keys are on their way before the states are joined.
+constexpr int q8_mass_keys(int GP) { return GP == 4 ? 8 : 4; }  // of a thread
+template <int D, int GP>
 __device__ __forceinline__ void q8_add_mass(const Q8DecodeArgs& a, const ListCounts& s, bool uniform, int chunk, float (*s_joined)[2]) {
+  constexpr int U = q8_mass_keys(GP);
   int h, part;
   const int pair = fdivmod(chunk, a.by_chunks, part), layer = fdivmod(pair, a.by_heads, h), G = a.G;
   const Q8Slots sl = q8_slots(a, s, uniform, pair, layer, h);
-  const int j0 = part * kQ8MassKeys, j1 = min(sl.n, j0 + kQ8MassKeys);
-  if (j0 >= j1) return;
+  const int j0 = part * U * (int)blockDim.x + (int)threadIdx.x;
+  if (part * U * (int)blockDim.x >= sl.n) return;  // (the whole block)
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+  const float* x = a.logits + (size_t)pair * G * a.n_cap;
+  float* mass = a.mass[layer] + (int64_t)h * a.mass_stride;
+  float y[GP][U], was[U];
+#pragma unroll
+  for (int g = 0; g < GP; ++g)
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int k = j0 + u * (int)blockDim.x;
+      y[g][u] = g < G && k < sl.n ? __ldcg(x + (size_t)g * a.n_cap + k) : 0.f;
+    }
+#pragma unroll
+  for (int u = 0; u < U; ++u) {
+    const int k = j0 + u * (int)blockDim.x;
+    was[u] = k < sl.n ? __ldcg(mass + k) : 0.f;
+  }
   for (int g = warp; g < G; g += blockDim.x >> 5) {
     float m = -INFINITY, l = 0.f;
     const float none[1] = {0.f};
@@ -603,32 +623,20 @@ __device__ __forceinline__ void q8_add_mass(const Q8DecodeArgs& a, const ListCou
     }
   }
   __syncthreads();
-  const float* x = a.logits + (size_t)pair * G * a.n_cap;
-  float* mass = a.mass[layer] + (int64_t)h * a.mass_stride;
-  constexpr int U = 4;  // keys of a thread in flight
-  for (int j = j0 + threadIdx.x; j < j1; j += U * blockDim.x) {
-    float was[U], sum[U];
+  float sum[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = j + u * blockDim.x;
-      was[u] = k < j1 ? __ldcg(mass + k) : 0.f;
-      sum[u] = 0.f;
-    }
-    for (int g = 0; g < G; ++g) {
-      float y[U];
+  for (int u = 0; u < U; ++u) sum[u] = 0.f;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        const int k = j + u * blockDim.x;
-        y[u] = k < j1 ? __ldcg(x + (size_t)g * a.n_cap + k) : 0.f;
-      }
+  for (int g = 0; g < GP; ++g) {
+    if (g >= G) break;
+    const float m = s_joined[g][0], f = s_joined[g][1];
 #pragma unroll
-      for (int u = 0; u < U; ++u) sum[u] = fmaf(ex2_approx(y[u] - s_joined[g][0]), s_joined[g][1], sum[u]);
-    }
+    for (int u = 0; u < U; ++u) sum[u] = fmaf(ex2_approx(y[g][u] - m), f, sum[u]);
+  }
 #pragma unroll
-    for (int u = 0; u < U; ++u) {
-      const int k = j + u * blockDim.x;
-      if (k < j1) mass[k] = was[u] + sum[u];
-    }
+  for (int u = 0; u < U; ++u) {
+    const int k = j0 + u * (int)blockDim.x;
+    if (k < sl.n) mass[k] = was[u] + sum[u];
   }
 }
 
@@ -636,7 +644,7 @@ __device__ __forceinline__ void q8_add_mass(const Q8DecodeArgs& a, const ListCou
 // written already; those without keys are set to zero.  Blocks from join_blocks on add to masses.
 // Which slots a pair has follows from the counts, which are final once the kernel before has passed its own wait: they are
 // read before this one's.
-template <int D, int NW>
+template <int D, int GP, int NW>
 __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q8_merge_kernel(const __grid_constant__ Q8DecodeArgs a) {
   constexpr int PER = D / 32, kInFlight = NW == 1 ? 4 : NW, kItems = NW == 1 ? 4 : 1;
   __shared__ ListCounts s_list;
@@ -652,7 +660,7 @@ __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q8_merge_kernel(const
   if ((int)blockIdx.x >= a.join_blocks) {
     pdl_wait();
     pdl_launch_dependents();
-    q8_add_mass<D>(a, s_list, uniform, blockIdx.x - a.join_blocks, s_joined);
+    q8_add_mass<D, GP>(a, s_list, uniform, blockIdx.x - a.join_blocks, s_joined);
     return;
   }
   const int item = blockIdx.x * kItems + (NW == 1 ? threadIdx.x >> 5 : 0);
@@ -741,11 +749,11 @@ static cudaError_t q8_decode_launch(Q8DecodeArgs& a, cudaStream_t stream) {
   a.join_blocks = a.whole ? 0 : nw == 1 ? (pairs * a.G + 3) / 4 : pairs * a.G;
   int64_t blocks = a.join_blocks;
   if (mass) {
-    const int chunks = (a.n_dev ? a.n_cap : a.n_host) / kQ8MassKeys + 1;
+    const int keys = q8_mass_keys(GP) * (nw == 8 ? 256 : 128), chunks = std::max(1, ((a.n_dev ? a.n_cap : a.n_host) + keys - 1) / keys);
     a.by_chunks = make_fastdiv(chunks);
     blocks += (int64_t)pairs * chunks;
   }
-  void (*merge)(Q8DecodeArgs) = nw == 8 ? q8_merge_kernel<D, 8> : nw == 4 ? q8_merge_kernel<D, 4> : q8_merge_kernel<D, 1>;
+  void (*merge)(Q8DecodeArgs) = nw == 8 ? q8_merge_kernel<D, GP, 8> : nw == 4 ? q8_merge_kernel<D, GP, 4> : q8_merge_kernel<D, GP, 1>;
   return launch_kernel(merge, dim3((unsigned)blocks), dim3(nw == 8 ? 256 : 128), 0, stream, a, true);
 }
 
