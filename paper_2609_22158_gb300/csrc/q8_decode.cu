@@ -74,6 +74,16 @@ struct Q8Stage {
   static __device__ __forceinline__ int swizzle(int row) { return D == 128 ? row & 7 : (row >> 1) & 3; }
 };
 
+// A copy of 16 bytes that leaves L2 first (masses: so that the logits stay there until they are read again).
+__device__ __forceinline__ void q8_cp_hint(uint32_t dst, const void* src, uint64_t policy) {
+  asm volatile("cp.async.cg.shared.global.L2::cache_hint [%0], [%1], 16, %2;" ::"r"(dst), "l"(src), "l"(policy) : "memory");
+}
+__device__ __forceinline__ uint64_t q8_evict_first() {
+  uint64_t policy;
+  asm volatile("createpolicy.fractional.L2::evict_first.b64 %0, 1.0;" : "=l"(policy));
+  return policy;
+}
+
 // The two pairs of codes of a word as fp16.
 __device__ __forceinline__ void q8_unpack(uint32_t w, uint32_t& lo, uint32_t& hi) {
   asm("{\n .reg .b16 a, b;\n mov.b32 {a, b}, %2;\n cvt.rn.f16x2.e4m3x2 %0, a;\n cvt.rn.f16x2.e4m3x2 %1, b;\n}\n"
@@ -433,6 +443,7 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
     if (lane == 0) is = c;
     __syncwarp();
   }
+  const uint64_t policy = MASS ? q8_evict_first() : 0ull;
   auto issue_next = [&](uint32_t dst) {
     if (ahead <= 0 && ahead > kNoMore / 2) {
       ListCursor c = is;
@@ -451,8 +462,13 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
 #pragma unroll
         for (int i = 0; i < kCopies; ++i) {
           const uint32_t to = (D == 128 && (i & 1) ? d16 ^ 64 : d16) + i * 512;
-          cp_async<16>(to, Kc + i * 512);
-          cp_async<16>(to + St::kV, Vc + i * 512);
+          if constexpr (MASS) {
+            q8_cp_hint(to, Kc + i * 512, policy);
+            q8_cp_hint(to + St::kV, Vc + i * 512, policy);
+          } else {
+            cp_async<16>(to, Kc + i * 512);
+            cp_async<16>(to + St::kV, Vc + i * 512);
+          }
         }
       } else {  // rows past the count: zeros, nothing is read
 #pragma unroll 1
