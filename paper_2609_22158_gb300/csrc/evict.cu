@@ -26,7 +26,8 @@ namespace stepkv {
 constexpr int kEvictLongThreads = 1024;    // of a head of more than kEvictShort rows
 constexpr int kEvictShortThreads = 512;
 constexpr int kEvictShort = 32 * kEvictShortThreads;
-constexpr int kEvictSmemKeys = 49152;      // heads too long for registers: keys held in shared memory (192 KB), the rest made anew
+constexpr int kEvictSmemKeys = 40960;      // heads too long for registers: keys held in shared memory (160 KB), the rest made anew
+constexpr int kEvictSmemPlan = 2048;       // moves of a head held in shared memory at most (16 KB)
 constexpr uint32_t kEvictProtected = 0xFFFFFFFFu;
 
 struct EvictArgs {
@@ -50,6 +51,7 @@ struct EvictArgs {
   int2* counts;     // (moves, blocks that receive rows)
   float2* cut;      // 8 bits: the scales (K, V) of the block that `keep` cuts
   int plan_cap, block_cap;
+  int smem_plan;    // moves held in shared memory (plan_cap), 0: in the workspace
   int32_t* status;
 };
 static_assert(sizeof(EvictArgs) <= 32000, "kernel parameter space");
@@ -149,85 +151,95 @@ __device__ __forceinline__ uint4 evict_rescale(const uint4& v, float ratio) {
   return make_uint4(q8_rescale(v.x, ratio), q8_rescale(v.y, ratio), q8_rescale(v.z, ratio), q8_rescale(v.w, ratio));
 }
 
-// Rows of an 8-bit cache by one CTA, row by row: what the blocks need of the rows they receive, then their scales, then the rows.
-// s_scale: [2][blocks], zeroed, holes: the slots of each block that are filled.
+// Rows of an 8-bit cache by one CTA: what the blocks need of the rows they receive, then their scales, then the rows.  A block
+// can only have to grow for a row of a larger scale than its own, so that few rows are looked at twice.
+// s_scale: [2][blocks], zeroed; s_holes: the slots of each block that are filled; cut: the scales of the block that `keep` cuts.
 template <int D, int NT>
 __device__ __forceinline__ void evict_move_codes(const EvictArgs& a, const int2* plan, int moves, int layer, int h, float* s_scale,
                                                  const uint32_t* s_holes, const float (&cut)[2]) {
   constexpr int LPR = D / 16, RPI = 32 / LPR, U = 4, kChunk = RPI * U;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, sub = lane / LPR, col = lane & (LPR - 1);
-  const int chunks = (moves + kChunk - 1) / kChunk, nblk = (a.keep + kQ8Block - 1) / kQ8Block;
+  const int nblk = (a.keep + kQ8Block - 1) / kQ8Block;
   const int cut_block = a.keep % kQ8Block ? a.keep / kQ8Block : -1;
+  const int tests = (moves + 31) / 32;
+  for (int c = warp; c < 2 * tests; c += NT / 32) {
+    const int z = c >= tests, i = (z ? c - tests : c) * 32 + lane;
+    uint8_t* rows = (z ? a.V : a.K)[layer] + h * a.head_bytes + col * 16;
+    const float* scale = (z ? a.V_scale : a.K_scale)[layer] + h * a.scale_stride;
+    int2 p = make_int2(0, 0);
+    float from = 0.f, old = 0.f;
+    if (i < moves) {
+      p = plan[i];
+      from = __ldcg(scale + p.y / kQ8Block);  // (no scale changes before the barrier)
+      old = __ldcg(scale + p.x / kQ8Block);
+    }
+    const uint32_t larger = __ballot_sync(0xffffffffu, from > old);
+    if (!larger) continue;
 #pragma unroll 1
-  for (int phase = 0; phase < 2; ++phase) {
-    for (int c = warp; c < 2 * chunks; c += NT / 32) {
-      const int z = c >= chunks;
-      const int i0 = (z ? c - chunks : c) * kChunk + sub;
-      uint8_t* rows = (z ? a.V : a.K)[layer] + h * a.head_bytes + col * 16;
-      const float* scale = (z ? a.V_scale : a.K_scale)[layer] + h * a.scale_stride;
-      int2 p[U];
-      uint4 v[U];
-      float from[U];
+    for (int k = 0; k < LPR; ++k) {
+      const int row = k * RPI + sub, x = __shfl_sync(0xffffffffu, p.x, row), y = __shfl_sync(0xffffffffu, p.y, row);
+      const float f = __shfl_sync(0xffffffffu, from, row);
+      float most = 0.f;
+      if (larger >> row & 1u) most = q8_float2(evict_top_code(__ldcg(reinterpret_cast<const uint4*>(rows + (int64_t)y * D)))).x * f;
 #pragma unroll
-      for (int u = 0; u < U; ++u) {
-        p[u] = make_int2(-1, -1);
-        if (i0 + u * RPI < moves) p[u] = plan[i0 + u * RPI];
-      }
-#pragma unroll
-      for (int u = 0; u < U; ++u) {
-        v[u] = make_uint4(0, 0, 0, 0);
-        from[u] = 0.f;
-        if (p[u].y >= 0) {
-          const int b = p[u].y / kQ8Block;
-          v[u] = __ldcg(reinterpret_cast<const uint4*>(rows + (int64_t)p[u].y * D));
-          from[u] = b == cut_block ? cut[z] : __ldcg(scale + b);  // (that block's scale may have grown)
-        }
-      }
-      if (phase == 0) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          float most = q8_float2(evict_top_code(v[u])).x * from[u];
-#pragma unroll
-          for (int o = 1; o < LPR; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-          if (col == 0 && p[u].x >= 0)  // (positive numbers order as integers)
-            atomicMax(reinterpret_cast<unsigned*>(s_scale) + z * nblk + p[u].x / kQ8Block, __float_as_uint(most));
-        }
-      } else {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-          if (p[u].x < 0) continue;
-          const float s = s_scale[z * nblk + p[u].x / kQ8Block];
-          if (from[u] != s) v[u] = evict_rescale(v[u], from[u] * q8_inverse(s));
-          *reinterpret_cast<uint4*>(rows + (int64_t)p[u].x * D) = v[u];
-        }
-      }
+      for (int o = 1; o < LPR; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+      if (col == 0 && (larger >> row & 1u))  // (positive numbers order as integers)
+        atomicMax(reinterpret_cast<unsigned*>(s_scale) + z * nblk + x / kQ8Block, __float_as_uint(most));
     }
-    __syncthreads();
-    if (phase == 1) break;
-    // the blocks' scales; where one grows, the rows that stay
-    for (int i0 = warp * 32; i0 < 2 * nblk; i0 += NT) {
-      const int i = i0 + lane, z = i >= nblk, b = z ? i - nblk : i;
-      float old = 0.f, s = 0.f;
-      if (i < 2 * nblk && s_holes[b]) {
-        float* scale = (z ? a.V_scale : a.K_scale)[layer] + h * a.scale_stride + b;
-        old = __ldcg(scale);
-        s = fmaxf(old, q8_scale(s_scale[i]));
-        s_scale[i] = s;
-        if (old < s) *scale = s;
-      }
-      uint32_t grows = __ballot_sync(0xffffffffu, old < s);
-      while (grows) {
-        const int l = __ffs(grows) - 1, k = i0 + l, y = k >= nblk, block = y ? k - nblk : k;
-        grows &= grows - 1;
-        const float ratio = __shfl_sync(0xffffffffu, old, l) * q8_inverse(__shfl_sync(0xffffffffu, s, l));
-        const int end = min(kQ8Block, a.keep - block * kQ8Block);  // (rows at or past keep are only read)
-        const uint32_t filled = s_holes[block];
-        uint32_t* w = reinterpret_cast<uint32_t*>((y ? a.V : a.K)[layer] + h * a.head_bytes + (int64_t)block * (kQ8Block * D));
-        for (int e = lane; e < end * (D / 4); e += 32)
-          if (!(filled >> (e / (D / 4)) & 1u)) w[e] = q8_rescale(__ldcg(w + e), ratio);
-      }
+  }
+  __syncthreads();
+  // the blocks' scales; where one grows, the rows that stay
+  for (int i0 = warp * 32; i0 < 2 * nblk; i0 += NT) {
+    const int i = i0 + lane, z = i >= nblk, b = z ? i - nblk : i;
+    float old = 0.f, s = 0.f;
+    if (i < 2 * nblk && s_holes[b]) {
+      float* scale = (z ? a.V_scale : a.K_scale)[layer] + h * a.scale_stride + b;
+      old = __ldcg(scale);
+      s = fmaxf(old, q8_scale(s_scale[i]));
+      s_scale[i] = s;
+      if (old < s) *scale = s;
     }
-    __syncthreads();
+    uint32_t grows = __ballot_sync(0xffffffffu, old < s);
+    while (grows) {
+      const int l = __ffs(grows) - 1, k = i0 + l, y = k >= nblk, block = y ? k - nblk : k;
+      grows &= grows - 1;
+      const float ratio = __shfl_sync(0xffffffffu, old, l) * q8_inverse(__shfl_sync(0xffffffffu, s, l));
+      const int end = min(kQ8Block, a.keep - block * kQ8Block);  // (rows at or past keep are only read)
+      const uint32_t filled = s_holes[block];
+      uint32_t* w = reinterpret_cast<uint32_t*>((y ? a.V : a.K)[layer] + h * a.head_bytes + (int64_t)block * (kQ8Block * D));
+      for (int e = lane; e < end * (D / 4); e += 32)
+        if (!(filled >> (e / (D / 4)) & 1u)) w[e] = q8_rescale(__ldcg(w + e), ratio);
+    }
+  }
+  __syncthreads();
+  const int chunks = (moves + kChunk - 1) / kChunk;
+  for (int c = warp; c < 2 * chunks; c += NT / 32) {
+    const int z = c >= chunks;
+    const int i0 = (z ? c - chunks : c) * kChunk + sub;
+    uint8_t* rows = (z ? a.V : a.K)[layer] + h * a.head_bytes + col * 16;
+    const float* scale = (z ? a.V_scale : a.K_scale)[layer] + h * a.scale_stride;
+    int2 p[U];
+    uint4 v[U];
+    float from[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      p[u] = make_int2(-1, -1);
+      if (i0 + u * RPI < moves) p[u] = plan[i0 + u * RPI];
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p[u].y < 0) continue;
+      const int b = p[u].y / kQ8Block;
+      v[u] = q8_ld_stream(rows + (int64_t)p[u].y * D);
+      from[u] = b == cut_block ? cut[z] : __ldcg(scale + b);  // (that block's scale may have grown)
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (p[u].x < 0) continue;
+      const float s = s_scale[z * nblk + p[u].x / kQ8Block];
+      if (from[u] != s) v[u] = evict_rescale(v[u], from[u] * q8_inverse(s));
+      *reinterpret_cast<uint4*>(rows + (int64_t)p[u].x * D) = v[u];
+    }
   }
 }
 
@@ -253,7 +265,7 @@ template <int DQ, int NT, int R>
 __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_select_kernel(const __grid_constant__ EvictArgs a) {
   constexpr int NW = NT / 32, RR = R ? R : 1;
   constexpr bool Q8 = DQ != 0;
-  extern __shared__ uint32_t s_key[];  // 8 bits: [2][blocks] scales, [blocks] holes; then keys (R = 0)
+  extern __shared__ __align__(8) uint32_t s_dyn[];  // moves; 8 bits: [2][blocks] scales, [blocks] holes; keys (R = 0)
   __shared__ uint32_t s_hist[3][2048];
   __shared__ uint32_t s_total[2][NW];
   __shared__ uint2 s_count[NW];
@@ -262,8 +274,9 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
   const int pair = blockIdx.x, layer = pair / a.Hkv, h = pair - layer * a.Hkv;
   const int keep = a.keep, nblk = Q8 ? (keep + kQ8Block - 1) / kQ8Block : 0;
   for (int i = t; i < 3 * 2048; i += NT) s_hist[0][i] = 0;
-  for (int i = t; i < 2 * nblk; i += NT) s_key[i] = 0;
-  uint32_t* s_holes = s_key + 2 * nblk;
+  uint32_t* s_scale = s_dyn + 2 * a.smem_plan;
+  for (int i = t; i < 2 * nblk; i += NT) s_scale[i] = 0;
+  uint32_t* s_holes = s_scale + 2 * nblk;
   uint32_t* s_keys = s_holes + nblk;
   if (t == 0) s_blocks = 0;
   pdl_wait();
@@ -400,7 +413,7 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
   uint32_t eq0 = __reduce_add_sync(0xffffffffu, lane < warp ? mine.x >> 16 : 0u);
   const uint32_t gt_low = __reduce_add_sync(0xffffffffu, mine.y & 0xFFFFu), eq_low = __reduce_add_sync(0xffffffffu, mine.y >> 16);
   const int kept_low = gt_low + min(eq_low, ties), moves = keep - kept_low;
-  int2* plan = a.plan + (int64_t)pair * a.plan_cap;
+  int2* plan = a.smem_plan ? reinterpret_cast<int2*>(s_dyn) : a.plan + (int64_t)pair * a.plan_cap;
   int2* blocks = a.blocks + (int64_t)pair * a.block_cap;
   each([&](uint32_t k, int j, bool in) {
     bool stays;
@@ -447,7 +460,7 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
   __syncthreads();
   for (int j = keep + t; j < n; j += NT) mass[j] = 0.f;
   if (a.moves_rows) {
-    if constexpr (Q8) evict_move_codes<DQ, NT>(a, plan, moves, layer, h, reinterpret_cast<float*>(s_key), s_holes, cut);
+    if constexpr (Q8) evict_move_codes<DQ, NT>(a, plan, moves, layer, h, reinterpret_cast<float*>(s_scale), s_holes, cut);
     else evict_move_rows<NT>(a, plan, moves, layer, h);
   }
 }
@@ -672,7 +685,8 @@ static stepkv_status_t evict_all(int n_layers, void* const* K, void* const* V, f
     int threads = 0;
     auto select = dq == 0 ? evict_kernel<0>(n_most, &threads) : dq == 64 ? evict_kernel<64>(n_most, &threads) : evict_kernel<128>(n_most, &threads);
     a.smem_keys = threads == kEvictLongThreads && n_most > 32 * kEvictLongThreads ? std::min(kEvictSmemKeys - (dq ? 8192 * 3 : 0), n_most) : 0;
-    const int smem = (a.smem_keys + (dq ? 3 * ((s.keep + kQ8Block - 1) / kQ8Block) : 0)) * (int)sizeof(uint32_t);
+    a.smem_plan = a.moves_rows && a.plan_cap <= kEvictSmemPlan ? a.plan_cap : 0;
+    const int smem = (2 * a.smem_plan + a.smem_keys + (dq ? 3 * ((s.keep + kQ8Block - 1) / kQ8Block) : 0)) * (int)sizeof(uint32_t);
     e = ensure_smem_attr(reinterpret_cast<const void*>(select), smem);
     if (e == cudaSuccess) e = launch_kernel(select, dim3(pairs), dim3(threads), smem, stream, a, true);
     if (e != cudaSuccess) break;
