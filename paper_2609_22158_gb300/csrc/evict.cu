@@ -12,6 +12,7 @@
 // of 11, 11 and 10 bits, as many as it takes; with R(j) = min(rows below j that equal T, those of them that stay) + rows below
 // j above T, the retained rows below slot j,
 //   a slot j < keep that goes is number j - R(j) of those, a slot j >= keep that stays number R(j) - R(keep).
+#include <cooperative_groups.h>
 #include <limits.h>
 
 #include <algorithm>
@@ -25,8 +26,10 @@ namespace stepkv {
 
 constexpr int kEvictLongThreads = 1024;    // of a head of more than kEvictShort rows
 constexpr int kEvictShortThreads = 512;
-constexpr int kEvictShort = 32 * kEvictShortThreads;
-constexpr int kEvictSmemKeys = 40960;      // heads too long for registers: keys held in shared memory (160 KB), the rest made anew
+constexpr int kEvictShort = 32 * kEvictShortThreads;  // (a thread holds 32 keys at most)
+constexpr int kEvictLong = 32 * kEvictLongThreads;
+constexpr int kEvictCluster = 8;           // CTAs of a head at most
+static_assert(kEvictCluster * kEvictLong >= kEvictMaxRows, "every key has a register");
 constexpr int kEvictSmemPlan = 2048;       // moves of a head held in shared memory at most (16 KB)
 constexpr uint32_t kEvictProtected = 0xFFFFFFFFu;
 
@@ -42,7 +45,7 @@ struct EvictArgs {
   int row_bytes;
   const int32_t* n_dev;
   int n_stride, n_host, n_cap, keep, n_sink, n_recent;
-  int smem_keys;
+  int cluster;      // CTAs of a head
   int moves_rows;   // this launch moves keys and values
   int32_t* n_out;   // NULL: not this launch
   // workspace, per (layer, head):
@@ -259,25 +262,30 @@ __global__ void evict_counts_kernel(const __grid_constant__ EvictArgs a) {
   evict_counts(a, blockDim.x);
 }
 
-// DQ: 0: bf16, else the channels of a row of codes.  R: groups of 32 slots a warp holds in registers at most; 0: keys in shared
-// memory.
-template <int DQ, int NT, int R>
+namespace cg = cooperative_groups;
+
+// DQ: 0: bf16, else the channels of a row of codes.  R: groups of 32 slots that a warp has at most.  CL: a cluster of CTAs takes the
+// head, each a part of its slots; maxima, histograms and counts meet through distributed shared memory.
+template <int DQ, int NT, int R, bool CL>
 __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_select_kernel(const __grid_constant__ EvictArgs a) {
-  constexpr int NW = NT / 32, RR = R ? R : 1;
+  constexpr int NW = NT / 32;
   constexpr bool Q8 = DQ != 0;
-  extern __shared__ __align__(8) uint32_t s_dyn[];  // moves; 8 bits: [2][blocks] scales, [blocks] holes; keys (R = 0)
+  extern __shared__ __align__(8) uint32_t s_dyn[];  // moves; 8 bits: [2][blocks] scales, [blocks] holes
   __shared__ uint32_t s_hist[3][2048];
+  __shared__ uint32_t s_sum[CL ? 2048 : 1];         // a histogram of all the cluster's CTAs
   __shared__ uint32_t s_total[2][NW];
   __shared__ uint2 s_count[NW];
   __shared__ uint32_t s_blocks;
+  __shared__ uint32_t s_top, s_safe;                // CL: what this CTA tells the others, each written once
+  __shared__ uint4 s_part;
   const int t = threadIdx.x, lane = t & 31, warp = t >> 5;
-  const int pair = blockIdx.x, layer = pair / a.Hkv, h = pair - layer * a.Hkv;
-  const int keep = a.keep, nblk = Q8 ? (keep + kQ8Block - 1) / kQ8Block : 0;
+  const int C = CL ? a.cluster : 1, pair = CL ? blockIdx.x / C : blockIdx.x, rank = blockIdx.x - pair * C;
+  const int layer = pair / a.Hkv, h = pair - layer * a.Hkv;
+  const int keep = a.keep, nblk = Q8 && a.moves_rows ? (keep + kQ8Block - 1) / kQ8Block : 0;
   for (int i = t; i < 3 * 2048; i += NT) s_hist[0][i] = 0;
   uint32_t* s_scale = s_dyn + 2 * a.smem_plan;
   for (int i = t; i < 2 * nblk; i += NT) s_scale[i] = 0;
   uint32_t* s_holes = s_scale + 2 * nblk;
-  uint32_t* s_keys = s_holes + nblk;
   if (t == 0) s_blocks = 0;
   pdl_wait();
   pdl_launch_dependents();
@@ -290,72 +298,79 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
       n = 0;
     }
   }
-  if (n <= keep) {
-    if (t == 0) a.counts[pair] = make_int2(0, 0);
+  if (n <= keep) {  // (the whole cluster)
+    if (t == 0 && rank == 0) a.counts[pair] = make_int2(0, 0);
     return;
   }
+  auto meet = [&] {
+    if constexpr (CL) cg::this_cluster().sync();
+    else __syncthreads();
+  };
+  auto peer = [&](auto* p, int r) { return cg::this_cluster().map_shared_rank(p, r); };
   float* mass = a.mass[layer] + (int64_t)h * a.mass_stride;
   int32_t* pos = a.pos[layer] + (int64_t)h * a.pos_stride;
-  // warp w: groups [w per, w per + per) of 32 slots
-  const int groups = (n + 31) / 32, per = (groups + NW - 1) / NW, g0 = warp * per, rounds = max(0, min(groups - g0, per));
+  // groups of 32 slots: this CTA's, of which warp w has `per` from g0 on
+  const int all = (n + 31) / 32, part = (all + C - 1) / C, c0 = rank * part, c1 = min(all, c0 + part);
+  const int per = (part + NW - 1) / NW, g0 = c0 + warp * per, rounds = max(0, min(c1 - g0, per));
   const int first = g0 * 32 + lane;
-  uint32_t keys[RR];
+  uint32_t keys[R];
 
   int top = INT_MIN;
-  if (R) {
 #pragma unroll
-    for (int r = 0; r < RR; ++r) {
-      keys[r] = (uint32_t)INT_MIN;
-      if (r < rounds && first + r * 32 < n) keys[r] = (uint32_t)__ldcg(pos + first + r * 32);
-    }
-#pragma unroll
-    for (int r = 0; r < RR; ++r) top = max(top, (int)keys[r]);
-  } else {
-    for (int r = 0; r < rounds; ++r)
-      if (first + r * 32 < n) top = max(top, __ldcg(pos + first + r * 32));
+  for (int r = 0; r < R; ++r) {
+    keys[r] = (uint32_t)INT_MIN;
+    if (r < rounds && first + r * 32 < n) keys[r] = (uint32_t)__ldcg(pos + first + r * 32);
   }
+#pragma unroll
+  for (int r = 0; r < R; ++r) top = max(top, (int)keys[r]);
   top = __reduce_max_sync(0xffffffffu, top);
   if (lane == 0) s_total[0][warp] = (uint32_t)top;
   __syncthreads();
   top = __reduce_max_sync(0xffffffffu, (int)s_total[0][lane & (NW - 1)]);
-  const int64_t recent = (int64_t)top - a.n_recent;
-  auto make_key = [&](int j) { return evict_key(__ldcg(mass + j), __ldcg(pos + j), a.n_sink, recent); };
-  uint32_t safe = 0;
-  if (R) {
-    constexpr int kBatch = RR < 8 ? RR : 8;
-#pragma unroll
-    for (int r0 = 0; r0 < RR; r0 += kBatch) {
-      asm volatile("" ::: "memory");  // (a batch's loads at a time: all at once take another register a group)
-      float m[kBatch];
-#pragma unroll
-      for (int r = 0; r < kBatch; ++r) {
-        m[r] = 0.f;
-        if (r0 + r < RR && r0 + r < rounds && first + (r0 + r) * 32 < n) m[r] = __ldcg(mass + first + (r0 + r) * 32);
-      }
-#pragma unroll
-      for (int r = 0; r < kBatch; ++r)
-        if (r0 + r < RR)
-          keys[r0 + r] = first + (r0 + r) * 32 < n ? evict_key(m[r], (int)keys[r0 + r], a.n_sink, recent) : 0u;
-    }
-  } else {
-    for (int r = 0; r < rounds; ++r) {
-      const int j = first + r * 32;
-      if (j < n && j < a.smem_keys) s_keys[j] = make_key(j);
-    }
+  if constexpr (CL) {
+    if (t == 0) s_top = (uint32_t)top;
+    meet();
+    top = __reduce_max_sync(0xffffffffu, lane < C ? (int)*peer(&s_top, lane) : INT_MIN);
   }
-  // f(key, slot) for this lane's slots below n; the whole warp at once
+  const int64_t recent = (int64_t)top - a.n_recent;
+  uint32_t safe = 0;
+  constexpr int kBatch = R < 8 ? R : 8;
+#pragma unroll
+  for (int r0 = 0; r0 < R; r0 += kBatch) {
+    asm volatile("" ::: "memory");  // (a batch's loads at a time: all at once take another register a group)
+    float m[kBatch];
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r) {
+      m[r] = 0.f;
+      if (r0 + r < R && r0 + r < rounds && first + (r0 + r) * 32 < n) m[r] = __ldcg(mass + first + (r0 + r) * 32);
+    }
+#pragma unroll
+    for (int r = 0; r < kBatch; ++r)
+      if (r0 + r < R) keys[r0 + r] = first + (r0 + r) * 32 < n ? evict_key(m[r], (int)keys[r0 + r], a.n_sink, recent) : 0u;
+  }
+  // f(key, slot, slot < n) for this lane's slots, the whole warp at once; keys of slots behind the last are 0
   auto each = [&](auto f) {
 #pragma unroll
-    for (int r = 0; r < (R ? RR : rounds); ++r) {
+    for (int r = 0; r < R; ++r) {
       if (r < rounds) {
         const int j = first + r * 32;
-        const bool in = j < n;
-        uint32_t k = 0;
-        if (R) k = keys[R ? r : 0];
-        else if (in) k = j < a.smem_keys ? s_keys[j] : make_key(j);
-        f(k, j, in);
+        f(keys[r], j, j < n);
       }
     }
+  };
+  // a histogram of all the head's keys, complete and counted in
+  auto counted = [&](uint32_t* hist) -> const uint32_t* {
+    meet();
+    if constexpr (CL) {
+      for (int i = t; i < 2048; i += NT) {
+        uint32_t x = 0;
+        for (int r = 0; r < C; ++r) x += peer(hist, r)[i];
+        s_sum[i] = x;
+      }
+      __syncthreads();
+      return s_sum;
+    }
+    return hist;
   };
   // the first histogram, and the protected rows
   each([&](uint32_t k, int, bool in) {
@@ -365,29 +380,35 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
   });
   safe = __reduce_add_sync(0xffffffffu, safe);
   if (lane == 0) s_total[1][warp] = safe;
-  __syncthreads();
-  safe = __reduce_add_sync(0xffffffffu, lane < NW ? s_total[1][lane] : 0u);
+  if constexpr (CL) {
+    __syncthreads();
+    safe = __reduce_add_sync(0xffffffffu, lane < NW ? s_total[1][lane] : 0u);
+    if (t == 0) s_safe = safe;
+  }
+  const uint32_t* hist = counted(s_hist[0]);
+  if constexpr (CL) safe = __reduce_add_sync(0xffffffffu, lane < C ? *peer(&s_safe, lane) : 0u);
+  else safe = __reduce_add_sync(0xffffffffu, lane < NW ? s_total[1][lane] : 0u);
 
   // the last retained row's key T under a mask, and how many of those that equal it stay
   uint32_t T = kEvictProtected, mask = 0xFFFFFFFFu, ties = keep, count = safe;
   if ((int)safe < keep) {
     ties = keep - safe;
-    T = evict_bin<NT>(s_hist[0], s_total[0], ties, count) << 21;
+    T = evict_bin<NT>(hist, s_total[0], ties, count) << 21;
     mask = 0xFFE00000u;
     if (ties < count) {
       each([&](uint32_t k, int, bool in) {
         if (in && (k & mask) == T) atomicAdd(&s_hist[1][k >> 10 & 2047u], 1u);
       });
-      __syncthreads();
-      T |= evict_bin<NT>(s_hist[1], s_total[1], ties, count) << 10;
+      hist = counted(s_hist[1]);
+      T |= evict_bin<NT>(hist, s_total[1], ties, count) << 10;
       mask = 0xFFFFFC00u;
     }
     if (ties < count) {
       each([&](uint32_t k, int, bool in) {
         if (in && (k & mask) == T) atomicAdd(&s_hist[2][k & 1023u], 1u);
       });
-      __syncthreads();
-      T |= evict_bin<NT>(s_hist[2], s_total[0], ties, count);
+      hist = counted(s_hist[2]);
+      T |= evict_bin<NT>(hist, s_total[0], ties, count);
       mask = 0xFFFFFFFFu;
     }
   }
@@ -411,7 +432,17 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
   const uint2 mine = lane < NW ? s_count[lane] : make_uint2(0, 0);
   uint32_t gt0 = __reduce_add_sync(0xffffffffu, lane < warp ? mine.x & 0xFFFFu : 0u);
   uint32_t eq0 = __reduce_add_sync(0xffffffffu, lane < warp ? mine.x >> 16 : 0u);
-  const uint32_t gt_low = __reduce_add_sync(0xffffffffu, mine.y & 0xFFFFu), eq_low = __reduce_add_sync(0xffffffffu, mine.y >> 16);
+  uint32_t gt_low = __reduce_add_sync(0xffffffffu, mine.y & 0xFFFFu), eq_low = __reduce_add_sync(0xffffffffu, mine.y >> 16);
+  if constexpr (CL) {
+    const uint32_t gt = __reduce_add_sync(0xffffffffu, mine.x & 0xFFFFu), eq = __reduce_add_sync(0xffffffffu, mine.x >> 16);
+    if (t == 0) s_part = make_uint4(gt, eq, gt_low, eq_low);
+    meet();
+    const uint4 other = lane < C ? *peer(&s_part, lane) : make_uint4(0, 0, 0, 0);
+    gt0 += __reduce_add_sync(0xffffffffu, lane < rank ? other.x : 0u);
+    eq0 += __reduce_add_sync(0xffffffffu, lane < rank ? other.y : 0u);
+    gt_low = __reduce_add_sync(0xffffffffu, other.z);
+    eq_low = __reduce_add_sync(0xffffffffu, other.w);
+  }
   const int kept_low = gt_low + min(eq_low, ties), moves = keep - kept_low;
   int2* plan = a.smem_plan ? reinterpret_cast<int2*>(s_dyn) : a.plan + (int64_t)pair * a.plan_cap;
   int2* blocks = a.blocks + (int64_t)pair * a.block_cap;
@@ -437,8 +468,9 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
     if (Q8) {
       const uint32_t holes = __ballot_sync(0xffffffffu, hole);
       if (lane == 0 && j < keep) {
-        s_holes[j / kQ8Block] = holes;
-        if (holes && !a.moves_rows) blocks[atomicAdd(&s_blocks, 1u)] = make_int2(j / kQ8Block, (j - kept) * 64 + __popc(holes));
+        if (a.moves_rows) s_holes[j / kQ8Block] = holes;
+        else if (holes)
+          blocks[atomicAdd(CL ? peer(&s_blocks, 0) : &s_blocks, 1u)] = make_int2(j / kQ8Block, (j - kept) * 64 + __popc(holes));
       }
     }
   });
@@ -447,19 +479,19 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
     cut[0] = __ldcg(a.K_scale[layer] + (int64_t)h * a.scale_stride + keep / kQ8Block);
     cut[1] = __ldcg(a.V_scale[layer] + (int64_t)h * a.scale_stride + keep / kQ8Block);
   }
-  __syncthreads();
-  if (t == 0 && !a.moves_rows) {
+  meet();
+  if (t == 0 && rank == 0 && !a.moves_rows) {
     a.counts[pair] = make_int2(moves, s_blocks);
     if (Q8) a.cut[pair] = make_float2(cut[0], cut[1]);
   }
-  for (int i = t; i < moves; i += NT) {
-    const int2 p = plan[i];
+  for (int i = rank * NT + t; i < moves; i += C * NT) {
+    const int2 p = CL ? __ldcg(plan + i) : plan[i];
     mass[p.x] = __ldcg(mass + p.y);
     pos[p.x] = __ldcg(pos + p.y);
   }
-  __syncthreads();
-  for (int j = keep + t; j < n; j += NT) mass[j] = 0.f;
-  if (a.moves_rows) {
+  meet();
+  for (int j = keep + rank * NT + t; j < n; j += C * NT) mass[j] = 0.f;
+  if (!CL && a.moves_rows) {
     if constexpr (Q8) evict_move_codes<DQ, NT>(a, plan, moves, layer, h, reinterpret_cast<float*>(s_scale), s_holes, cut);
     else evict_move_rows<NT>(a, plan, moves, layer, h);
   }
@@ -616,19 +648,30 @@ size_t evict_ws_bytes(int n_layers, int Hkv, int n_cap) {
 // -> 334 us, 8911 to 8272 in 8 bits 145 -> 45), or rows are few (24 x 2 heads, one row 9.4 -> 8.2).
 static bool evict_moves_rows(int pairs, int plan_cap, int n_sm) { return 2 * pairs >= n_sm || plan_cap <= 16; }
 
-// By the most rows a head can have.
-template <int DQ>
-static void (*evict_kernel(int n_most, int* threads))(EvictArgs) {
-  *threads = n_most <= kEvictShort ? kEvictShortThreads : kEvictLongThreads;
-  const int groups = (n_most + *threads - 1) / *threads;  // of 32 slots, a warp
-  if (n_most <= kEvictShort) {
-    if (groups <= 4) return evict_select_kernel<DQ, kEvictShortThreads, 4>;
-    if (groups <= 8) return evict_select_kernel<DQ, kEvictShortThreads, 8>;
-    if (groups <= 16) return evict_select_kernel<DQ, kEvictShortThreads, 16>;
-    if (groups <= 20) return evict_select_kernel<DQ, kEvictShortThreads, 20>;
-    return evict_select_kernel<DQ, kEvictShortThreads, 32>;
+// By the most rows a CTA can have.
+template <int DQ, bool CL>
+static void (*evict_kernel(int rows, int* threads))(EvictArgs) {
+  *threads = rows <= kEvictShort && !CL ? kEvictShortThreads : kEvictLongThreads;
+  const int groups = (rows + *threads - 1) / *threads;  // of 32 slots, a warp
+  if constexpr (CL) {
+    return groups <= 8 ? evict_select_kernel<DQ, kEvictLongThreads, 8, true> : evict_select_kernel<DQ, kEvictLongThreads, 32, true>;
+  } else {
+    if (rows > kEvictShort) return evict_select_kernel<DQ, kEvictLongThreads, 32, false>;
+    if (groups <= 4) return evict_select_kernel<DQ, kEvictShortThreads, 4, false>;
+    if (groups <= 8) return evict_select_kernel<DQ, kEvictShortThreads, 8, false>;
+    if (groups <= 16) return evict_select_kernel<DQ, kEvictShortThreads, 16, false>;
+    if (groups <= 20) return evict_select_kernel<DQ, kEvictShortThreads, 20, false>;
+    return evict_select_kernel<DQ, kEvictShortThreads, 32, false>;
   }
-  return groups <= 32 ? evict_select_kernel<DQ, kEvictLongThreads, 32> : evict_select_kernel<DQ, kEvictLongThreads, 0>;
+}
+
+// CTAs of a head: as many as its keys need, and, where heads leave SMs idle, more while each has kEvictPart rows.
+constexpr int kEvictPart = 4096;
+static int evict_cluster(int pairs, int n_most, int n_sm) {
+  int c = 1;
+  while (c * kEvictLong < n_most) c *= 2;
+  while (c < kEvictCluster && 2 * c * pairs <= n_sm && n_most >= 2 * c * kEvictPart) c *= 2;
+  return c;
 }
 
 // dq: 0: bf16 rows of row_bytes, else the channels of a row of codes.
@@ -677,18 +720,25 @@ static stepkv_status_t evict_all(int n_layers, void* const* K, void* const* V, f
     w += evict_align((size_t)pairs * sizeof(int2));
     a.cut = reinterpret_cast<float2*>(w);
     a.status = s.status;
-    a.moves_rows = evict_moves_rows(pairs, a.plan_cap, n_sm);
+    a.cluster = 1;
+    a.moves_rows = n_most <= kEvictLong && evict_moves_rows(pairs, a.plan_cap, n_sm);
+    if (!a.moves_rows) a.cluster = evict_cluster(pairs, n_most, n_sm);
     // one count for all is read by every launch: replaced by the last; n itself only after all CTAs have read it
     int32_t* const n_out = s.n_dev && s.n_stride ? s.n_out : last ? s.n_out : nullptr;
     const bool late = n_out && n_out == s.n_dev;
     a.n_out = late || !a.moves_rows ? nullptr : n_out;
     int threads = 0;
-    auto select = dq == 0 ? evict_kernel<0>(n_most, &threads) : dq == 64 ? evict_kernel<64>(n_most, &threads) : evict_kernel<128>(n_most, &threads);
-    a.smem_keys = threads == kEvictLongThreads && n_most > 32 * kEvictLongThreads ? std::min(kEvictSmemKeys - (dq ? 8192 * 3 : 0), n_most) : 0;
+    const int rows = (n_most + a.cluster - 1) / a.cluster;
+    auto select = a.cluster > 1 ? (dq == 0 ? evict_kernel<0, true>(rows, &threads) : evict_kernel<64, true>(rows, &threads))
+                  : dq == 0     ? evict_kernel<0, false>(rows, &threads)
+                  : dq == 64    ? evict_kernel<64, false>(rows, &threads)
+                                : evict_kernel<128, false>(rows, &threads);
     a.smem_plan = a.moves_rows && a.plan_cap <= kEvictSmemPlan ? a.plan_cap : 0;
-    const int smem = (2 * a.smem_plan + a.smem_keys + (dq ? 3 * ((s.keep + kQ8Block - 1) / kQ8Block) : 0)) * (int)sizeof(uint32_t);
+    const int smem = (2 * a.smem_plan + (dq && a.moves_rows ? 3 * ((s.keep + kQ8Block - 1) / kQ8Block) : 0)) * (int)sizeof(uint32_t);
     e = ensure_smem_attr(reinterpret_cast<const void*>(select), smem);
-    if (e == cudaSuccess) e = launch_kernel(select, dim3(pairs), dim3(threads), smem, stream, a, true);
+    if (e == cudaSuccess)
+      e = a.cluster > 1 ? launch_cluster(select, dim3(pairs * a.cluster), dim3(threads), a.cluster, smem, stream, a, true)
+                        : launch_kernel(select, dim3(pairs), dim3(threads), smem, stream, a, true);
     if (e != cudaSuccess) break;
     if (a.moves_rows) {
       if (late) {

@@ -99,7 +99,8 @@ CASES = [  # L, Hkv, d, rows, n, keep, n_sink, n_recent
     (1, 1, 8, 2, 2, 1, 0, 0), (1, 1, 128, 1, 1, 1, 0, 0), (2, 2, 64, 33, 33, 32, 1, 2), (1, 3, 128, 40, 37, 5, 2, 3), (2, 2, 96, 100, 100, 31, 4, 8),
     (1, 2, 256, 70, 65, 64, 0, 64), (3, 2, 80, 200, 199, 198, 7, 90), (1, 4, 128, 1500, 1400, 700, 16, 100), (2, 1, 64, 4097, 4097, 1, 0, 1),
     (70, 1, 64, 50, 49, 20, 2, 2), (1, 2, 64, 2049, 2049, 2048, 4, 500), (2, 3, 128, 5000, 4999, 1024, 1024, 0), (1, 8, 128, 8911, 8911, 8272, 16, 32),
-    (33, 8, 64, 90, 90, 45, 0, 0), (20, 4, 128, 3000, 2999, 1001, 4, 300), (1, 2, 8, 40000, 39999, 39990, 10, 3000), (1, 1, 8, 60000, 60000, 30001, 100, 5000), (1, 2, 8, 50000, 49500, 400, 0, 0)]
+    (33, 8, 64, 90, 90, 45, 0, 0), (20, 4, 128, 3000, 2999, 1001, 4, 300), (1, 2, 8, 40000, 39999, 39990, 10, 3000), (1, 1, 8, 262144, 262144, 100001, 4, 9000),
+    (2, 2, 16, 17000, 16999, 9000, 3, 700), (1, 1, 8, 60000, 60000, 30001, 100, 5000), (1, 2, 8, 50000, 49500, 400, 0, 0)]
 
 
 @pytest.mark.parametrize("kind", MASSES)
@@ -123,7 +124,7 @@ def test_evict_matches_oracle(B, L, Hkv, d, rows, n, keep, sink, recent, kind):
 Q8_CASES = [(1, 1, 64, 2, 2, 1, 0, 0), (1, 2, 128, 40, 37, 5, 2, 3), (2, 2, 64, 33, 33, 32, 1, 2), (1, 3, 128, 100, 99, 40, 4, 8),
             (2, 1, 64, 640, 640, 320, 16, 64), (1, 2, 128, 1500, 1401, 700, 16, 100), (70, 1, 64, 70, 69, 33, 2, 2),
             (1, 2, 64, 2049, 2049, 2048, 4, 500), (3, 2, 128, 301, 300, 299, 0, 20), (1, 1, 128, 1000, 1000, 31, 0, 10),
-            (20, 4, 64, 200, 199, 77, 2, 8), (39, 2, 128, 400, 390, 300, 2, 30), (76, 1, 128, 700, 700, 352, 0, 50), (10, 8, 64, 1300, 1300, 700, 8, 100)]
+            (20, 4, 64, 200, 199, 77, 2, 8), (39, 2, 128, 400, 390, 300, 2, 30), (76, 1, 128, 700, 700, 352, 0, 50), (10, 8, 64, 1300, 1300, 700, 8, 100), (1, 2, 64, 17000, 16999, 6001, 16, 2000)]
 
 
 @pytest.mark.parametrize("spread", [0, 3, 14])
