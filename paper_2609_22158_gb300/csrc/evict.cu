@@ -115,7 +115,7 @@ __device__ __forceinline__ uint32_t evict_bin(const uint32_t* hist, uint32_t* s_
 // Rows of bf16 by one CTA, 16 bytes a lane.
 template <int NT>
 __device__ __forceinline__ void evict_move_rows(const EvictArgs& a, const int2* plan, int moves, int layer, int h) {
-  constexpr int U = 6;
+  constexpr int U = 4;
   const int lpr = a.row_bytes >> 4, rpi = 32 / lpr;  // lanes a row, rows an instruction
   const int lane = threadIdx.x & 31, sub = lane / lpr, col = lane - sub * lpr;
   const int per_chunk = rpi * U, chunks = (moves + per_chunk - 1) / per_chunk;
