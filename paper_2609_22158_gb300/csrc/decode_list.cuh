@@ -45,12 +45,15 @@ __device__ __forceinline__ int list_keys(const DecodeList& a, int layer, bool te
 
 // Keys of every cache and the first block of each in the list of all pairs' blocks; first[n_layers]: all blocks.  By the
 // first warp of a CTA; the caller synchronises.  Not used where all caches have one count.
+// PAD: blocks without keys that each pair has behind its own in the list, for what a pair costs whatever its length: ranges of
+// the same length then take the same time, whether they hold a few long pairs or many short ones.
 struct ListCounts {
   int n[kListLayers];
   int first[kListLayers + 1];
 };
 __device__ __forceinline__ int list_blocks(int n) { return (n + kListBlock - 1) / kListBlock; }
 __device__ __forceinline__ bool list_uniform(const DecodeList& a) { return !a.n_dev || a.n_stride == 0 || a.n_layers == 1; }
+template <int PAD = 0>
 __device__ __forceinline__ void list_counts(const DecodeList& a, ListCounts& s, bool tell) {
   const int lane = threadIdx.x & 31;
   int sum[2];
@@ -59,7 +62,7 @@ __device__ __forceinline__ void list_counts(const DecodeList& a, ListCounts& s, 
     const int l = 2 * lane + i;
     const int n = l < a.n_layers ? list_keys(a, l, tell) : 0;
     s.n[l] = n;
-    sum[i] = list_blocks(n) * a.Hkv;
+    sum[i] = n > 0 ? (list_blocks(n) + PAD) * a.Hkv : 0;
   }
   int total = sum[0] + sum[1];
 #pragma unroll

@@ -41,6 +41,10 @@ constexpr int kQ8DecThreads = kQ8DecWarps * 32;
 constexpr int kQ8DecCtasPerSm = 2;
 constexpr int kQ8DecMinSmem = 228 * 1024 / (kQ8DecCtasPerSm + 1);
 constexpr float kQ8WeightLog2 = 14.f;  // the largest weight is held as 2^14 (fp16 reaches 65504)
+// Blocks that a pair of a ragged batch counts besides its own (list_counts): what its query, its state and the join with the CTA's
+// other warps cost.  64 caches x 16 heads of 0 to 4096 rows, d = 64: 85 us without, 60 with 8, 51 with 16, 49 with 32; 32 x 8 heads,
+// lengths spread over their logarithm up to 8192 46, 22, 21, 23; one of 8192 among 64 rows 17, 12.6, 12.3, 12.7.
+constexpr int kQ8Pad = 16;
 static_assert(kListBlock == kQ8Block && kListLayers == kQ8Layers, "a warp step is a block of the cache");
 
 struct Q8DecodeArgs : DecodeList {
@@ -327,12 +331,13 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
     n_all = list_keys(a, 0, blockIdx.x == 0 && threadIdx.x == 0);
     total = list_blocks(n_all) * a.n_layers * a.Hkv;
   } else {
-    if (warp == 0) list_counts(a, s_list, blockIdx.x == 0);
+    if (warp == 0) list_counts<kQ8Pad>(a, s_list, blockIdx.x == 0);
     __syncthreads();
     total = s_list.first[a.n_layers];
   }
   auto keys_of = [&](int layer) { return RAGGED ? s_list.n[layer] : n_all; };
   auto blocks_of = [&](int layer) { return list_blocks(keys_of(layer)); };
+  constexpr int kPad = RAGGED ? kQ8Pad : 0;
   const ListSplit sp = list_split(a, !RAGGED, list_blocks(n_all), total);
   const int W = a.whole ? a.whole : sp.W, rank = warp & (W - 1);
   const int group = W == 1 ? blockIdx.x * kQ8DecWarps + warp : blockIdx.x;
@@ -378,19 +383,17 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
         while (s_list.first[ci.layer + 1] <= lo) ++ci.layer;
         nb = blocks_of(ci.layer);
         at = lo - s_list.first[ci.layer];
-        ci.h = (unsigned)at / (unsigned)nb;
+        ci.h = (unsigned)at / (unsigned)(nb + kPad);
         ci.pair = ci.layer * a.Hkv + ci.h;
-        at -= ci.h * nb;
+        at -= ci.h * (nb + kPad);
       }
       ci.blk = at;
       ci.left = hi - lo + at;
       ci.end = min(nb, ci.left);
     }
   }
-  if (ci.layer == a.n_layers) return;  // whole groups
-  if (lane == 0) s_here[warp] = ci;
   auto next_pair = [&](ListCursor& c) {
-    c.left -= c.end;
+    c.left -= blocks_of(c.layer) + kPad;
     if (c.left <= 0) {
       c.layer = a.n_layers;
       return;
@@ -407,6 +410,10 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
     c.blk = 0;
     c.end = min(blocks_of(c.layer), c.left);
   };
+
+  if (RAGGED && ci.layer < a.n_layers && ci.blk >= ci.end) next_pair(ci);  // (the range begins behind a pair's own blocks)
+  if (ci.layer == a.n_layers) return;  // whole groups
+  if (lane == 0) s_here[warp] = ci;
 
   // copies: kStages blocks ahead of the arithmetic, across pairs
   constexpr int kVecRow = D / 16, kRows = 32 / kVecRow, kCopies = kQ8Block / kRows;  // vectors a row, rows an instruction, instructions
@@ -573,7 +580,7 @@ __device__ __forceinline__ Q8Slots q8_slots(const Q8DecodeArgs& a, const ListCou
     first = s.first[layer];
     total = s.first[a.n_layers];
   }
-  const int nb = list_blocks(r.n);
+  const int nb = list_blocks(r.n), pad = uniform ? 0 : kQ8Pad;
   r.slot = r.count = 0;
   if (nb == 0) return r;
   if (a.whole) {
@@ -586,7 +593,7 @@ __device__ __forceinline__ Q8Slots q8_slots(const Q8DecodeArgs& a, const ListCou
     r.slot = pair * sp.k;
     r.count = sp.k;
   } else {
-    const int b0 = first + h * nb, g0 = (unsigned)b0 / (unsigned)sp.per;
+    const int b0 = first + h * (nb + pad), g0 = (unsigned)b0 / (unsigned)sp.per;
     r.slot = g0 + pair;
     r.count = (unsigned)(b0 + nb - 1) / (unsigned)sp.per - g0 + 1;
   }
@@ -670,7 +677,7 @@ __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q8_merge_kernel(const
   const int warp = NW == 1 ? 0 : threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool uniform = list_uniform(a);
   if (!uniform) {
-    if (threadIdx.x < 32) list_counts(a, s_list, false);
+    if (threadIdx.x < 32) list_counts<kQ8Pad>(a, s_list, false);
     __syncthreads();
   }
   if ((int)blockIdx.x >= a.join_blocks) {
@@ -731,10 +738,11 @@ __global__ void __launch_bounds__(NW == 1 ? 128 : NW * 32) q8_merge_kernel(const
   }
 }
 
-// Partial states: a pair of n rows leaves at most one slot per block, and all pairs together at most one per group and pair.
+// Partial states: a pair of n rows leaves at most one slot per block of the list, and all pairs together at most one per group
+// and pair.
 // Behind them, for masses, the logits.
 static size_t q8_part_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap) {
-  const int64_t pairs = (int64_t)n_layers * Hkv, blocks = pairs * (((int64_t)n_cap + kQ8Block - 1) / kQ8Block);
+  const int64_t pairs = (int64_t)n_layers * Hkv, blocks = pairs * (((int64_t)n_cap + kQ8Block - 1) / kQ8Block + kQ8Pad);
   const size_t b = (size_t)(std::min<int64_t>(kListMaxGroups, blocks) + pairs) * (Hq / Hkv) * (d + 4) * sizeof(float);
   return (b + 255) & ~(size_t)255;
 }
