@@ -40,6 +40,9 @@ constexpr int kQ8DecWarps = kListWarps;
 constexpr int kQ8DecThreads = kQ8DecWarps * 32;
 constexpr int kQ8DecCtasPerSm = 2;
 constexpr int kQ8DecMinSmem = 228 * 1024 / (kQ8DecCtasPerSm + 1);
+// Rounds of blocks up to which a pair taken whole has its masses added by its own warps, in the same launch (1 layer x 8 heads x
+// 512 rows 8.7 -> 7.2 us, 32 layers 12.0 -> 9.5; at 8 rounds 10.9, by the second kernel's blocks 7.2).
+constexpr int kQ8FewRounds = 4;
 constexpr float kQ8WeightLog2 = 14.f;  // the largest weight is held as 2^14 (fp16 reaches 65504)
 // Blocks that a pair of a ragged batch counts besides its own (list_counts): what its query, its state and the join with the CTA's
 // other warps cost.  64 caches x 16 heads of 0 to 4096 rows, d = 64: 85 us without, 60 with 8, 51 with 16, 49 with 32; 32 x 8 heads,
@@ -61,7 +64,8 @@ struct Q8DecodeArgs : DecodeList {
   float c;          // log2(e) / sqrt(d)
   float* part;      // [slot][G][d + 4]: m, l, -, -, values
   float* logits;    // [pair][G][n_cap], log2 units, or NULL
-  int whole;        // warps that take a pair, all of it: no states to join (0: the pairs are cut, list_split)
+  int whole;        // warps of a CTA that take a pair, all of it: one launch (0: the pairs are cut, list_split)
+  int mass_here;    // whole pairs: the first kernel adds to the masses
   int join_blocks;  // blocks of the second kernel that join states; those after them add to masses
   FastDiv by_chunks;  // chunks of keys of a pair, a block of the mass pass each
 };
@@ -313,7 +317,7 @@ struct Q8State {
   }
 };
 
-// RAGGED: a count for each cache.  MASS: logits are kept, and the state of every pair.
+// RAGGED: a count for each cache.  MASS: logits are kept, and the state of every pair, unless its masses are added here.
 template <int D, int GP, bool RAGGED, bool MASS>
 __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kernel(const __grid_constant__ Q8DecodeArgs a) {
   using State = Q8State<D, GP>;
@@ -322,6 +326,7 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
   extern __shared__ __align__(128) uint8_t q8_smem[];  // per-warp rings, then per-warp states
   __shared__ ListCounts s_list;  // RAGGED
   __shared__ float s_ml[kQ8DecWarps][2 * GP];
+  __shared__ float s_joined[kQ8DecWarps][2 * GP];     // MASS, whole pairs: of each head m and 1 / (G l)
   __shared__ ListCursor s_cursor[kQ8DecWarps], s_here[kQ8DecWarps];  // where each warp's copies and its arithmetic are, out of its registers
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   pdl_wait();
@@ -545,7 +550,12 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
         if (all)
           *reinterpret_cast<float4*>(a.out[ci.layer] + (size_t)(ci.h * G + g) * D + e0) =
               make_float4(v[0] / ll, v[1] / ll, v[2] / ll, v[3] / ll);
-        if (!all || MASS) {
+        if (MASS && a.mass_here) {
+          if (e0 == 0) {
+            s_joined[w0][2 * g] = mm;
+            s_joined[w0][2 * g + 1] = 1.f / (ll * (float)G);
+          }
+        } else if (!all || MASS) {
           const int slot = a.whole ? ci.pair : !RAGGED && sp.k > 0 ? group : group + ci.pair;
           float* dst = a.part + ((size_t)slot * G + g) * (D + 4);
           if (e0 == 0) {
@@ -553,6 +563,37 @@ __global__ void __launch_bounds__(kQ8DecThreads, kQ8DecCtasPerSm) q8_decode_kern
             dst[1] = ll;
           }
           if (!all) *reinterpret_cast<float4*>(dst + 4 + e0) = make_float4(v[0], v[1], v[2], v[3]);
+        }
+      }
+      sync_group();
+      if (MASS && a.mass_here) {  // this warp's blocks, whose logits it wrote
+        const float* lg = a.logits + (size_t)ci.pair * G * a.n_cap;
+        float* mass = a.mass[ci.layer] + (int64_t)ci.h * a.mass_stride;
+        const float* joined = s_joined[w0];
+        constexpr int U = 4;  // blocks in flight
+        for (int b = solo ? 0 : rank; b < ci.end; b += U * (solo ? 1 : W)) {
+          float was[U], sum[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int j = (b + u * (solo ? 1 : W)) * kQ8Block + lane;
+            was[u] = j < n ? __ldcg(mass + j) : 0.f;
+            sum[u] = 0.f;
+          }
+#pragma unroll
+          for (int g = 0; g < GP; ++g) {
+            if (g >= G) break;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+              const int j = (b + u * (solo ? 1 : W)) * kQ8Block + lane;
+              const float y = j < n ? __ldcg(lg + (size_t)g * a.n_cap + j) : 0.f;
+              sum[u] = fmaf(ex2_approx(y - joined[2 * g]), joined[2 * g + 1], sum[u]);
+            }
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const int j = (b + u * (solo ? 1 : W)) * kQ8Block + lane;
+            if (j < n) mass[j] = was[u] + sum[u];
+          }
         }
       }
       sync_group();
@@ -750,8 +791,10 @@ size_t q8_decode_ws_bytes(int n_layers, int Hkv, int Hq, int d, int n_cap, bool 
   return q8_part_bytes(n_layers, Hkv, Hq, d, n_cap) + (mass ? (size_t)n_layers * Hq * n_cap * sizeof(float) : 0);
 }
 
-// Warps that take a pair whole, which needs no partial states and, without masses, no second kernel, or 0; by the most blocks a pair can
-// have (where the counts are on the device: by n_cap).
+// Warps that take a pair whole, which needs no partial states and no second kernel, or 0; by the most blocks a pair can have (where
+// the counts are on the device: by n_cap).  A warp each where pairs are many and short (64 layers x 8 heads, G = 1, 32 rows 3.9 us, a CTA
+// each 6.8, cut 5.4), else a CTA, while what its last wave leaves idle costs less than that kernel (1 layer x 8 heads x 512 rows 5.9
+// us, cut 7.0; 32 x 8 heads x 2048 rows 24.7, cut 27.5).
 static int q8_whole(int pairs, int slots, int nb, bool ragged) {
   if (pairs > slots && nb <= 12) return 1;
   const int64_t rounds = (nb + kQ8DecWarps - 1) / kQ8DecWarps, idle = pairs % slots ? slots - pairs % slots : 0;
@@ -768,7 +811,7 @@ static cudaError_t q8_decode_launch(Q8DecodeArgs& a, cudaStream_t stream) {
   cudaError_t e = ensure_smem_attr(reinterpret_cast<const void*>(kern), smem);
   const int pairs = a.n_layers * a.Hkv;
   if (e == cudaSuccess) e = launch_kernel(kern, dim3(a.n_groups), dim3(kQ8DecThreads), smem, stream, a, true);
-  if (e != cudaSuccess || (a.whole && !mass)) return e;
+  if (e != cudaSuccess || (a.whole && (!mass || a.mass_here))) return e;
   const int nw = a.whole ? 1 : a.n_groups >= 16 * pairs ? 8 : a.n_groups > 5 * pairs ? 4 : 1;
   a.join_blocks = a.whole ? 0 : nw == 1 ? (pairs * a.G + 3) / 4 : pairs * a.G;
   int64_t blocks = a.join_blocks;
@@ -810,7 +853,10 @@ stepkv_status_t q8_decode_run(const stepkv_q8_cache_t& c, const void* const* q, 
     const int64_t blocks = (int64_t)nl * c.Hkv * ((n_cap + kQ8Block - 1) / kQ8Block);
     const int slots = std::min(kListMaxGroups / kQ8DecWarps, n_sm * kQ8DecCtasPerSm);
     a.n_groups = (int)std::min<int64_t>(slots, blocks);
-    a.whole = q8_whole(nl * c.Hkv, slots, ((n_dev ? n_cap : n_host) + kQ8Block - 1) / kQ8Block, n_dev && n_stride && nl > 1);
+    const bool ragged = n_dev && n_stride && nl > 1;
+    const int nb = ((n_dev ? n_cap : n_host) + kQ8Block - 1) / kQ8Block;
+    a.whole = q8_whole(nl * c.Hkv, slots, nb, ragged);
+    a.mass_here = mass && a.whole && nb <= kQ8FewRounds * a.whole;
     if (a.whole) a.n_groups = (nl * c.Hkv * a.whole + kQ8DecWarps - 1) / kQ8DecWarps;
     for (int i = 0; i < 2; ++i) {
       const int groups = a.n_groups * (i ? kQ8DecWarps : 1);
