@@ -9,6 +9,7 @@ import pytest
 from oracle import stepkv_oracle as O
 from paper_2609_22158_gb300 import workload as wl
 import stepkv_testlib as TL
+import test_gpu_q8 as Q
 
 pytestmark = pytest.mark.gpu
 
@@ -278,9 +279,10 @@ def _attended(rng, steps, L, Hkv, G, d):
 @pytest.mark.parametrize("q8", [True, False])
 @pytest.mark.parametrize("captured", [False, True])
 def test_decoding_at_a_budget(B, q8, captured):
-    """The operators as they are used together: a prompt, then tokens appended, attended with their weights accumulated, and
-    evicted whenever the cache has `slack` rows more than its budget, eagerly or as one captured step replayed.  The oracle
-    follows the device's masses (a sum's last bits decide between rows that are near one another), and all else is its own."""
+    """The operators as they are used together: a prompt brought to its budget, then tokens appended, attended with their weights
+    accumulated, and one row of each head evicted, eagerly or as one captured step replayed, in 8 bits and in bf16.  The
+    oracle follows the device's masses (a sum's last bits decide between rows that are near one another), and all else is its
+    own."""
     import torch
     rng = np.random.default_rng(7)
     L, Hkv, G, d, prompt, keep, sink, recent, steps = 2, 2, 4, 64, 70, 60, 4, 20, 12
@@ -301,6 +303,7 @@ def test_decoding_at_a_budget(B, q8, captured):
     else:
         K, V = (torch.zeros((L, Hkv, rows, d), dtype=torch.bfloat16, device="cuda") for _ in "kv")
         K[:, :, :prompt], V[:, :, :prompt] = TL.bf16_dev(X[0]), TL.bf16_dev(X[1])
+        ws = torch.zeros(B.load_library().stepkv_decode_h2o_workspace_size(L, Hkv, Hkv * G, d, rows) + 512, dtype=torch.uint8, device="cuda")
     ews, masses = B.evict_workspace(mass), torch.zeros_like(mass)
 
     def evict():
@@ -321,6 +324,8 @@ def test_decoding_at_a_budget(B, q8, captured):
         now.add_(1)
         if q8:
             B.stepkv_q8_decode(q, cache, n, out=out, mass=mass, ws=ws, status=st)
+        else:
+            B.stepkv_decode_h2o(list(q), list(K), list(V), n, list(mass), out=list(out), ws=ws, status=st)
         evict()
 
     # the oracle's side
@@ -376,13 +381,15 @@ def test_decoding_at_a_budget(B, q8, captured):
                 append(0, l, h, k[l, h], keep)
                 append(1, l, h, val[l, h], keep)
                 at[l][h][keep] = prompt + i
+            Kv, Vv = (np.stack([v[t][l][h][:keep + 1] for h in range(Hkv)]) for t in range(2))
+            want, weights = O.q4_decode_attention(qq[l], Kv, Vv), O.attention_weights(qq[l], Kv)
+            got, was, now_ = (x[l].cpu().numpy().astype(np.float64) for x in (out, before, masses))
             if q8:
-                Kv, Vv = (np.stack([v[t][l][h][:keep + 1] for h in range(Hkv)]) for t in range(2))
-                want = O.q4_decode_attention(qq[l], Kv, Vv)
-                # 2^-17: test_gpu_q8's bound at 61 rows of logits below 32, of max |V| < 8
-                assert np.abs(out[l].cpu().numpy() - want).max() < 8 * 2.0 ** -17
-                added = (masses - before)[l, :, :keep + 1].cpu().numpy()
-                assert np.abs(added - O.attention_weights(qq[l], Kv)).max() < 2.0 ** -17 + 2.0 ** -20
+                assert (np.abs(got - want) <= Q._decode_bound(qq[l], Kv, Vv)).all()
+                assert (np.abs((now_ - was)[:, :keep + 1] - weights) <= Q._mass_bound(qq[l], Kv, was[:, :keep + 1])).all()
+            else:  # as the decode and its masses are tested: 2e-3, of the terms' magnitude where they cancel
+                assert (np.abs(got - want) <= 2e-3 * np.maximum(np.abs(want), 1e-3 * O.q4_decode_attention(qq[l], Kv, np.abs(Vv)))).all()
+                assert (np.abs((now_ - was)[:, :keep + 1] - weights) <= 2e-3 * weights + 2.0 ** -22 * (was[:, :keep + 1] + 1)).all()
         follow(keep + 1)
         for l in range(L):
             for h in range(Hkv):

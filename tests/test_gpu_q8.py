@@ -611,6 +611,62 @@ def test_two_streams_at_once(B):
         assert abs(mass.sum().item() / (20 * 4) - 1) < 1e-4  # (each call adds 1 a head)
 
 
+def test_captured_steps_replay_with_new_counts(B):
+    """Two captured steps (append a token, attend with masses) of one cache that share nothing but it, replayed in turn as it grows
+    across blocks; the counts are on the device."""
+    import torch
+    rng = np.random.default_rng(17)
+    L, Hkv, G, d, n0, steps = 2, 2, 4, 128, 25, 50
+    rows = n0 + steps
+    K, V = ([_bits(rng, (Hkv, rows, d)) for _ in range(L)] for _ in "kv")
+    q = [_bits(rng, (Hkv * G, d)) for _ in range(L)]
+    Kd, Vd = torch.stack([TL.bf16_dev(x) for x in K]), torch.stack([TL.bf16_dev(x) for x in V])
+    cache, st = B.Q8Cache.allocate(L, Hkv, rows, d), B.new_status()
+    B.stepkv_q8_write(cache, Kd[:, :, :n0], Vd[:, :, :n0], 0, status=st)
+    row, count = (torch.zeros(1, dtype=torch.int32, device="cuda") for _ in "rn")
+    row.fill_(n0), count.fill_(n0)
+    tk, tv = (torch.zeros((L, Hkv, 1, d), dtype=torch.bfloat16, device="cuda") for _ in "kv")
+    qd = torch.stack([TL.bf16_dev(x) for x in q])
+    graphs, outs, masses = [], [], []
+    for _ in range(2):
+        out, mass, ws = torch.zeros((L, Hkv * G, d), device="cuda"), torch.zeros((L, Hkv, rows), device="cuda"), B.q8_decode_workspace(cache, Hkv * G, True)
+
+        def step():
+            B.stepkv_q8_write(cache, tk, tv, row, status=st)
+            B.stepkv_q8_decode(qd, cache, count, out=out, mass=mass, ws=ws, status=st)
+
+        tk.copy_(Kd[:, :, n0:n0 + 1]), tv.copy_(Vd[:, :, n0:n0 + 1])
+        step()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            step()
+        mass.zero_()
+        graphs.append(graph), outs.append(out), masses.append(mass)
+    v = [[[np.zeros((rows, d)), np.zeros(-(-rows // 32))] for h in range(Hkv)] for l in range(L)]
+    vv = [[[np.zeros((rows, d)), np.zeros(-(-rows // 32))] for h in range(Hkv)] for l in range(L)]
+    want, bound = np.zeros((2, L, Hkv, rows)), np.zeros((2, L, Hkv, rows))
+    for t in range(n0, rows):
+        row.fill_(t), count.fill_(t + 1)
+        tk.copy_(Kd[:, :, t:t + 1]), tv.copy_(Vd[:, :, t:t + 1])
+        graphs[t & 1].replay()
+        for l in range(L):
+            for h in range(Hkv):
+                for x, src in ((v, K), (vv, V)):
+                    if t == n0:
+                        O.q8_append(*x[l][h], src[l][h][:n0], 0)
+                    O.q8_append(*x[l][h], src[l][h][t:t + 1], t)
+        torch.cuda.synchronize()
+        for l in range(L):
+            Kv, Vv = (np.stack([x[l][h][0][:t + 1] for h in range(Hkv)]) for x in (v, vv))
+            want[t & 1, l, :, :t + 1] += O.attention_weights(q[l], Kv)
+            bound[t & 1, l, :, :t + 1] += _mass_bound(q[l], Kv, want[t & 1, l, :, :t + 1])
+            if t % 7 == 0 or t == rows - 1:
+                _check(outs[t & 1][l], q[l], Kv, Vv, t + 1, f"token {t}, layer {l}")
+    assert st.item() == 0
+    for i in range(2):
+        assert (np.abs(masses[i].cpu().numpy() - want[i]) <= 1.001 * bound[i]).all()  # (a mass that is off rounds like one that is not)
+
+
 def test_what_a_call_makes_belongs_to_its_stream(B):
     """Calls on a stream while the current one is busy: the status, rows and workspace that they make are neither cleared nor
     handed out again by what the current stream does late."""
