@@ -150,8 +150,10 @@ __device__ __forceinline__ uint32_t evict_top_code(const uint4& v) {
   }
   return max(max(top & 0xFFu, top >> 8 & 0xFFu), max(top >> 16 & 0xFFu, top >> 24));
 }
-__device__ __forceinline__ uint4 evict_rescale(const uint4& v, float ratio) {
-  return make_uint4(q8_rescale(v.x, ratio), q8_rescale(v.y, ratio), q8_rescale(v.z, ratio), q8_rescale(v.w, ratio));
+// The rows of a block that lie below keep (those at or past it are only read), a bit each.
+__device__ __forceinline__ uint32_t evict_rows_below(int keep, int block) {
+  const int rows = keep - block * kQ8Block;
+  return rows >= kQ8Block ? 0xFFFFFFFFu : (1u << rows) - 1u;
 }
 
 // Rows of an 8-bit cache by one CTA: what the blocks need of the rows they receive, then their scales, then the rows.  A block
@@ -179,15 +181,23 @@ __device__ __forceinline__ void evict_move_codes(const EvictArgs& a, const int2*
     const uint32_t larger = __ballot_sync(0xffffffffu, from > old);
     if (!larger) continue;
 #pragma unroll 1
-    for (int k = 0; k < LPR; ++k) {
-      const int row = k * RPI + sub, x = __shfl_sync(0xffffffffu, p.x, row), y = __shfl_sync(0xffffffffu, p.y, row);
-      const float f = __shfl_sync(0xffffffffu, from, row);
-      float most = 0.f;
-      if (larger >> row & 1u) most = q8_float2(evict_top_code(__ldcg(reinterpret_cast<const uint4*>(rows + (int64_t)y * D)))).x * f;
+    for (int k0 = 0; k0 < LPR; k0 += U) {  // (LPR instructions cover the 32 rows)
+      uint4 v[U];
 #pragma unroll
-      for (int o = 1; o < LPR; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
-      if (col == 0 && (larger >> row & 1u))  // (positive numbers order as integers)
-        atomicMax(reinterpret_cast<unsigned*>(s_scale) + z * nblk + x / kQ8Block, __float_as_uint(most));
+      for (int u = 0; u < U; ++u) {
+        const int row = (k0 + u) * RPI + sub, y = __shfl_sync(0xffffffffu, p.y, row);
+        v[u] = make_uint4(0, 0, 0, 0);
+        if (larger >> row & 1u) v[u] = __ldcg(reinterpret_cast<const uint4*>(rows + (int64_t)y * D));
+      }
+#pragma unroll
+      for (int u = 0; u < U; ++u) {
+        const int row = (k0 + u) * RPI + sub, x = __shfl_sync(0xffffffffu, p.x, row);
+        float most = q8_float2(evict_top_code(v[u])).x * __shfl_sync(0xffffffffu, from, row);
+#pragma unroll
+        for (int o = 1; o < LPR; o <<= 1) most = fmaxf(most, __shfl_xor_sync(0xffffffffu, most, o));
+        if (col == 0 && (larger >> row & 1u))  // (positive numbers order as integers)
+          atomicMax(reinterpret_cast<unsigned*>(s_scale) + z * nblk + x / kQ8Block, __float_as_uint(most));
+      }
     }
   }
   __syncthreads();
@@ -207,11 +217,8 @@ __device__ __forceinline__ void evict_move_codes(const EvictArgs& a, const int2*
       const int l = __ffs(grows) - 1, k = i0 + l, y = k >= nblk, block = y ? k - nblk : k;
       grows &= grows - 1;
       const float ratio = __shfl_sync(0xffffffffu, old, l) * q8_inverse(__shfl_sync(0xffffffffu, s, l));
-      const int end = min(kQ8Block, a.keep - block * kQ8Block);  // (rows at or past keep are only read)
-      const uint32_t filled = s_holes[block];
-      uint32_t* w = reinterpret_cast<uint32_t*>((y ? a.V : a.K)[layer] + h * a.head_bytes + (int64_t)block * (kQ8Block * D));
-      for (int e = lane; e < end * (D / 4); e += 32)
-        if (!(filled >> (e / (D / 4)) & 1u)) w[e] = q8_rescale(__ldcg(w + e), ratio);
+      q8_rescale_rows<D>((y ? a.V : a.K)[layer] + h * a.head_bytes + (int64_t)block * (kQ8Block * D),
+                         evict_rows_below(a.keep, block) & ~s_holes[block], ratio);
     }
   }
   __syncthreads();
@@ -240,7 +247,7 @@ __device__ __forceinline__ void evict_move_codes(const EvictArgs& a, const int2*
     for (int u = 0; u < U; ++u) {
       if (p[u].x < 0) continue;
       const float s = s_scale[z * nblk + p[u].x / kQ8Block];
-      if (from[u] != s) v[u] = evict_rescale(v[u], from[u] * q8_inverse(s));
+      if (from[u] != s) v[u] = q8_rescale(v[u], from[u] * q8_inverse(s));
       *reinterpret_cast<uint4*>(rows + (int64_t)p[u].x * D) = v[u];
     }
   }
@@ -614,11 +621,7 @@ __global__ void __launch_bounds__(kQ8Threads) evict_q8_move_kernel(const __grid_
     float s = q8_scale(most);
     if (old >= s) s = old;
     if (old < s) {  // the rows that stay (those at or past keep are only read now)
-      const float ratio = old * q8_inverse(s);
-      const int end = min(kQ8Block, a.keep - block * kQ8Block);
-      uint32_t* w = reinterpret_cast<uint32_t*>(codes + (int64_t)block * (kQ8Block * D));
-      for (int i = lane; i < end * (D / 4); i += 32)
-        if (!(filled >> (i / (D / 4)) & 1u)) w[i] = q8_rescale(__ldcg(w + i), ratio);
+      q8_rescale_rows<D>(codes + (int64_t)block * (kQ8Block * D), evict_rows_below(a.keep, block) & ~filled, old * q8_inverse(s));
     }
     __syncwarp();  // every lane has read the old scale
 #pragma unroll
@@ -627,7 +630,7 @@ __global__ void __launch_bounds__(kQ8Threads) evict_q8_move_kernel(const __grid_
       const float f = __shfl_sync(0xffffffffu, from, u * RPI + sub);
       if (x >= 0) {
         if (f != s) {
-          v[u] = evict_rescale(v[u], f * q8_inverse(s));
+          v[u] = q8_rescale(v[u], f * q8_inverse(s));
         }
         *reinterpret_cast<uint4*>(codes + (int64_t)x * D + col * 16) = v[u];
       }

@@ -124,9 +124,7 @@ __global__ void __launch_bounds__(kQ8Threads, q8_write_ctas(D, MANY)) q8_write_k
       if (old > s) {
         s = old;
       } else if (old < s) {
-        const float ratio = old * q8_inverse(s);
-        uint32_t* w = reinterpret_cast<uint32_t*>(codes);
-        for (int i = lane; i < lead * (D / 4); i += 32) w[i] = q8_rescale(__ldcg(w + i), ratio);
+        q8_rescale_rows<D>(codes, (1u << lead) - 1u, old * q8_inverse(s));
       }
       __syncwarp();  // every lane has read the old scale
     }
