@@ -14,6 +14,7 @@
 //   a slot j < keep that goes is number j - R(j) of those, a slot j >= keep that stays number R(j) - R(keep).
 #include <cooperative_groups.h>
 #include <limits.h>
+#include <math.h>
 
 #include <algorithm>
 
@@ -647,9 +648,18 @@ size_t evict_ws_bytes(int n_layers, int Hkv, int n_cap) {
          evict_align(pairs * sizeof(int2)) + evict_align(pairs * sizeof(float2));
 }
 
-// Whether a head's CTA moves its rows by itself: where heads fill half the machine (32 layers x 8 heads, 32768 to 8272 rows in bf16 382
-// -> 334 us, 8911 to 8272 in 8 bits 145 -> 45), or rows are few (24 x 2 heads, one row 9.4 -> 8.2).
-static bool evict_moves_rows(int pairs, int plan_cap, int n_sm) { return 2 * pairs >= n_sm || plan_cap <= 16; }
+// Whether a head's CTA moves its rows by itself, by what either way is to take at most (in ns; 152 SMs).  By itself: 12 a row of
+// 256 bytes (4 that do not go by its bytes), 20 a row of codes, heads beyond the number of SMs in a second turn.  By a second kernel: its
+// launch, and the bytes at the rate of scattered rows, or a turn of 6 us for the blocks that its warps take at once.
+// Measured, by itself against a second kernel, us: 8 heads 8911 to 8272 rows bf16 18.5, 15.4, codes 26, 20.5; 32 heads 19.0, 18.1
+// and 27, 34; 64 heads 19.4, 22.0 and 29, 54; 8 heads 2100 to 2048 6.7, 8.2; 64 heads 16384 to 8272 105, 77 and 127, 75; 256 heads 32768 to
+// 8272 334, 382.
+static bool evict_moves_rows(int pairs, int plan_cap, int block_cap, int row_bytes, bool q8, int n_sm) {
+  const double turns = (pairs + n_sm - 1) / n_sm, rows = (double)pairs * plan_cap;
+  const double itself = turns * plan_cap * (q8 ? 20.0 : 4.0 + row_bytes / 32.0);
+  const double second = 4000.0 + (q8 ? 6000.0 * ceil(2.0 * pairs * block_cap / (n_sm * 32)) : rows * 4 * row_bytes / 6500.0);
+  return itself <= second;
+}
 
 // By the most rows a CTA can have.
 template <int DQ, bool CL>
@@ -724,7 +734,7 @@ static stepkv_status_t evict_all(int n_layers, void* const* K, void* const* V, f
     a.cut = reinterpret_cast<float2*>(w);
     a.status = s.status;
     a.cluster = 1;
-    a.moves_rows = n_most <= kEvictLong && evict_moves_rows(pairs, a.plan_cap, n_sm);
+    a.moves_rows = n_most <= kEvictLong && evict_moves_rows(pairs, a.plan_cap, a.block_cap, row_bytes, dq != 0, n_sm);
     if (!a.moves_rows) a.cluster = evict_cluster(pairs, n_most, n_sm);
     // one count for all is read by every launch: replaced by the last; n itself only after all CTAs have read it
     int32_t* const n_out = s.n_dev && s.n_stride ? s.n_out : last ? s.n_out : nullptr;
