@@ -218,7 +218,7 @@ __device__ __forceinline__ void evict_move_codes(const EvictArgs& a, const int2*
       const int l = __ffs(grows) - 1, k = i0 + l, y = k >= nblk, block = y ? k - nblk : k;
       grows &= grows - 1;
       const float ratio = __shfl_sync(0xffffffffu, old, l) * q8_inverse(__shfl_sync(0xffffffffu, s, l));
-      q8_rescale_rows<D>((y ? a.V : a.K)[layer] + h * a.head_bytes + (int64_t)block * (kQ8Block * D),
+      q8_rescale_rows<D, 4>((y ? a.V : a.K)[layer] + h * a.head_bytes + (int64_t)block * (kQ8Block * D),
                          evict_rows_below(a.keep, block) & ~s_holes[block], ratio);
     }
   }
@@ -622,7 +622,7 @@ __global__ void __launch_bounds__(kQ8Threads) evict_q8_move_kernel(const __grid_
     float s = q8_scale(most);
     if (old >= s) s = old;
     if (old < s) {  // the rows that stay (those at or past keep are only read now)
-      q8_rescale_rows<D>(codes + (int64_t)block * (kQ8Block * D), evict_rows_below(a.keep, block) & ~filled, old * q8_inverse(s));
+      q8_rescale_rows<D, 4>(codes + (int64_t)block * (kQ8Block * D), evict_rows_below(a.keep, block) & ~filled, old * q8_inverse(s));
     }
     __syncwarp();  // every lane has read the old scale
 #pragma unroll
@@ -649,15 +649,15 @@ size_t evict_ws_bytes(int n_layers, int Hkv, int n_cap) {
 }
 
 // Whether a head's CTA moves its rows by itself, by what either way is to take at most (in ns; 152 SMs).  By itself: 12 a row of
-// 256 bytes (4 that do not go by its bytes), 20 a row of codes, heads beyond the number of SMs in a second turn.  By a second kernel: its
-// launch, and the bytes at the rate of scattered rows, or a turn of 6 us for the blocks that its warps take at once.
+// 256 bytes (4 that do not go by its bytes), 20 a row of codes, heads beyond those that run at once in a second turn.  By a second kernel:
+// its launch, and the bytes at the rate of scattered rows, or a turn of 8 us for the blocks that its warps take at once.
 // Measured, by itself against a second kernel, us: 8 heads 8911 to 8272 rows bf16 18.5, 15.4, codes 26, 20.5; 32 heads 19.0, 18.1
-// and 27, 34; 64 heads 19.4, 22.0 and 29, 54; 8 heads 2100 to 2048 6.7, 8.2; 64 heads 16384 to 8272 105, 77 and 127, 75; 256 heads 32768 to
-// 8272 334, 382.
-static bool evict_moves_rows(int pairs, int plan_cap, int block_cap, int row_bytes, bool q8, int n_sm) {
-  const double turns = (pairs + n_sm - 1) / n_sm, rows = (double)pairs * plan_cap;
+// and 27, 34; 64 heads 19.4, 22.0 and 29, 54; 8 heads 2100 to 2048 6.7, 8.2; 64 heads 16384 to 8272 105, 77 and 127, 75; 256 heads 176, 270
+// (codes), 32768 to 8272 334, 382.
+static bool evict_moves_rows(int pairs, int plan_cap, int block_cap, int row_bytes, bool q8, int at_once, int n_sm) {
+  const double turns = (pairs + at_once - 1) / at_once, rows = (double)pairs * plan_cap;
   const double itself = turns * plan_cap * (q8 ? 20.0 : 4.0 + row_bytes / 32.0);
-  const double second = 4000.0 + (q8 ? 6000.0 * ceil(2.0 * pairs * block_cap / (n_sm * 32)) : rows * 4 * row_bytes / 6500.0);
+  const double second = 4000.0 + (q8 ? 8000.0 * ceil(2.0 * pairs * block_cap / (n_sm * 32)) : rows * 4 * row_bytes / 6500.0);
   return itself <= second;
 }
 
@@ -734,7 +734,7 @@ static stepkv_status_t evict_all(int n_layers, void* const* K, void* const* V, f
     a.cut = reinterpret_cast<float2*>(w);
     a.status = s.status;
     a.cluster = 1;
-    a.moves_rows = n_most <= kEvictLong && evict_moves_rows(pairs, a.plan_cap, a.block_cap, row_bytes, dq != 0, n_sm);
+    a.moves_rows = n_most <= kEvictLong && evict_moves_rows(pairs, a.plan_cap, a.block_cap, row_bytes, dq != 0, n_most <= kEvictShort ? 2 * n_sm : n_sm, n_sm);
     if (!a.moves_rows) a.cluster = evict_cluster(pairs, n_most, n_sm);
     // one count for all is read by every launch: replaced by the last; n itself only after all CTAs have read it
     int32_t* const n_out = s.n_dev && s.n_stride ? s.n_out : last ? s.n_out : nullptr;

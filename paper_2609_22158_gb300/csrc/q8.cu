@@ -123,8 +123,20 @@ __global__ void __launch_bounds__(kQ8Threads, q8_write_ctas(D, MANY)) q8_write_k
       const float old = __ldcg(scale);
       if (old > s) {
         s = old;
-      } else if (old < s) {
-        q8_rescale_rows<D>(codes, (1u << lead) - 1u, old * q8_inverse(s));
+      } else if (old < s) {  // (some words of a lane at a time: the new rows are in registers)
+        constexpr int kAt = MANY ? 2 : 8;
+        const float ratio = old * q8_inverse(s);
+        uint32_t* w = reinterpret_cast<uint32_t*>(codes) + lane;
+        const int words = lead * (D / 4);
+#pragma unroll 1
+        for (int i = 0; i < words; i += kAt * 32) {
+          uint32_t x[kAt];
+#pragma unroll
+          for (int k = 0; k < kAt; ++k) x[k] = i + k * 32 + lane < words ? __ldcg(w + i + k * 32) : 0u;
+#pragma unroll
+          for (int k = 0; k < kAt; ++k)
+            if (i + k * 32 + lane < words) w[i + k * 32] = q8_rescale(x[k], ratio);
+        }
       }
       __syncwarp();  // every lane has read the old scale
     }

@@ -49,19 +49,22 @@ __device__ __forceinline__ uint4 q8_rescale(const uint4& v, float ratio) {
   return make_uint4(q8_rescale(v.x, ratio), q8_rescale(v.y, ratio), q8_rescale(v.z, ratio), q8_rescale(v.w, ratio));
 }
 
-// A warp brings the rows of `rows` (a bit each) of a block to a scale `ratio` times as fine, 16 bytes a lane, all loads ahead.
-template <int D>
+// A warp brings the rows of `rows` (a bit each) of a block to a scale `ratio` times as fine, 16 bytes a lane, AT loads ahead.
+template <int D, int AT>
 __device__ __forceinline__ void q8_rescale_rows(uint8_t* block, uint32_t rows, float ratio) {
   constexpr int LPR = D / 16, RPI = 32 / LPR, NI = kQ8Block / RPI;
   const int lane = threadIdx.x & 31, sub = lane / LPR;
   uint4* p = reinterpret_cast<uint4*>(block) + lane;
-  uint4 v[NI];
+#pragma unroll 1
+  for (int u0 = 0; u0 < NI; u0 += AT) {
+    uint4 v[AT];
 #pragma unroll
-  for (int u = 0; u < NI; ++u)
-    if (rows >> (u * RPI + sub) & 1u) v[u] = __ldcg(p + u * 32);
+    for (int u = 0; u < AT; ++u)
+      if (rows >> ((u0 + u) * RPI + sub) & 1u) v[u] = __ldcg(p + (u0 + u) * 32);
 #pragma unroll
-  for (int u = 0; u < NI; ++u)
-    if (rows >> (u * RPI + sub) & 1u) p[u * 32] = q8_rescale(v[u], ratio);
+    for (int u = 0; u < AT; ++u)
+      if (rows >> ((u0 + u) * RPI + sub) & 1u) p[(u0 + u) * 32] = q8_rescale(v[u], ratio);
+  }
 }
 
 constexpr int kQ8Threads = 256;  // of a CTA of the kernels that move rows
