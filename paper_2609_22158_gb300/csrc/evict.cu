@@ -12,6 +12,11 @@
 // of 11, 11 and 10 bits, as many as it takes; with R(j) = min(rows below j that equal T, those of them that stay) + rows below
 // j above T, the retained rows below slot j,
 //   a slot j < keep that goes is number j - R(j) of those, a slot j >= keep that stays number R(j) - R(keep).
+//
+// 32 layers x 8 heads: 8273 to 8272 rows 13 us (positions 1.6, masses and the first histogram 3.1, its bin 0.7, counts 0.8, moves
+// listed 1.6, done 1.2, of a CTA's 9), where the 16 MB that are read take 2.5; 32768 to 8272 in bf16 332 us, of which the moves of 1.7 GB
+// are 254 at the copy rate: one CTA an SM, so that 104 heads wait for the first 152, and their search leaves DRAM idle.  Keys in shared
+// memory instead of registers, with every pass over all of them: 24 and 393 us.
 #include <cooperative_groups.h>
 #include <limits.h>
 #include <math.h>

@@ -21,8 +21,16 @@
 // its warps' states in shared memory, and writes the output where it had the whole pair, or else leaves a partial state, which a second
 // kernel joins with the others in key order.
 //
-// Masses need the sums over all keys: the logits go to the workspace, and blocks of the second kernel join the (maximum, sum)
-// of a pair's states and add exp2(x - m) / l to its keys' masses.
+// 441 instructions a block of 32 keys (G <= 4, d = 128), issued at a third of the rate that the schedulers have: the reads bound it.
+// 64 layers x 8 heads x 16417 rows, G = 5: 300 us = 7.2 TB/s; 32 layers x 8272 rows 86 us = 6.3 (the first rows and the join are 6 of
+// them); one layer 9.1 us (17 MB; launch, first rows, two rounds of blocks, join). On CUDA cores, a lane's share of the channels
+// per key, 5393, 1190 and 796 us.  Eight warps of up to 255 registers on an SM with three stages of 8 KB each (d = 128, G <= 4).
+// Clusters of 2 to 16 CTAs a pair, joined through distributed shared memory in one launch: 1 layer x 8 heads x 1024 rows 6.4 -> 6.2
+// us, 4096 8.2 -> 8.3, 8272 9.1 -> 10.7, with masses 7.2 -> 8.2: not kept, nor a dry run of the second kernel before its wait (9.2).
+//
+// Masses need the sums over all keys: the logits go to the workspace (keys and values leave L2 first, so that they stay there: 32
+// layers x 8272 rows 115 -> 107 us), and blocks of the second kernel join the (maximum, sum) of a pair's states and add
+// exp2(x - m) / l to its keys' masses; short pairs taken whole do that themselves (kQ8FewRounds).
 #include <cuda_fp16.h>
 #include <math.h>
 
