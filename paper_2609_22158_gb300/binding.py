@@ -194,9 +194,16 @@ def default_params() -> Params:
 
 
 # ----------------------------------------------------------------------------- helpers
+_torch_module = None
+
+
 def _torch():
-    import torch
-    return torch
+    """torch, imported with the first call (a call of the library asks several times: an import statement each took 0.3 us)."""
+    global _torch_module
+    if _torch_module is None:
+        import torch
+        _torch_module = torch
+    return _torch_module
 
 
 def _ptr(t) -> Optional[int]:
@@ -1232,9 +1239,10 @@ def _evict(where, call, front, L, Hkv, rows, dev, mass, pos, n, keep, n_sink, n_
     m, ms = _per_row(mass, torch.float32, L, Hkv, rows, dev, "mass")
     p, ps = _per_row(pos, torch.int32, L, Hkv, rows, dev, "pos")
     n_dev, stride, n_host = _counts_arg(n, L, dev)
-    for x, name in ((rows, "rows"), (keep, "keep"), (n_sink, "n_sink"), (n_recent, "n_recent")):
-        _int32(x, name)
-    counts = n_dev.numel() if stride else 1
+    if not (0 <= keep < 2 ** 31 and 0 <= n_sink < 2 ** 31 and 0 <= n_recent < 2 ** 31 and rows < 2 ** 31):
+        for x, name in ((rows, "rows"), (keep, "keep"), (n_sink, "n_sink"), (n_recent, "n_recent")):
+            _int32(x, name)
+    counts = L if stride else 1
     if n_out is None:
         with _made_on(stream):
             n_out = torch.zeros(counts, dtype=torch.int32, device=dev)
@@ -1261,7 +1269,7 @@ def stepkv_evict(K, V, mass, pos, n, keep: int, n_sink: int = 0, n_recent: int =
     layer.  Rows [0, keep) are the retained ones afterwards, with their masses and positions; masses behind them
     are zero.  Returns n_out, min(n, keep) on the device, as many as n has (n itself may be given)."""
     torch = _torch()
-    k, v = (_PerLayer(x, torch.bfloat16, 3, name) for x, name in ((K, "K"), (V, "V")))
+    k, v = _PerLayer(K, torch.bfloat16, 3, "K"), _PerLayer(V, torch.bfloat16, 3, "V")
     Hkv, rows, d = k.shape
     if not k.like(v) or k.strides[2] != 1 or (rows > 1 and k.strides[1] != d):
         raise ValueError("stepkv_evict: K and V must be laid out alike, with dense rows")
