@@ -243,7 +243,7 @@ def test_positions_at_the_ends_of_32_bits(B):
     import torch
     lo, hi = -2 ** 31, 2 ** 31 - 1
     for pos, sink, recent in (([hi, hi - 1, lo, 0, 5, hi - 2], 0, 2), ([lo, lo + 1, lo + 2, lo + 3, lo + 4, lo + 5], 0, 2),
-                              ([3, 1, 2, hi, 0, lo], 2, 1)):
+                              ([3, 1, 2, hi, 0, lo], 2, 1), ([7] * 6, 0, 1), ([lo] * 6, 1, 0), ([hi] * 6, 3, 0)):
         mass = np.array([0.1, 0.2, 0.9, 0.8, 0.7, 0.3], np.float32)
         K = torch.arange(6 * 8, dtype=torch.float32).reshape(1, 1, 6, 8).cuda().bfloat16()
         V, md, pd = K.clone(), _dev(mass)[None, None], _dev(np.array(pos, np.int32))[None, None]
@@ -253,6 +253,25 @@ def test_positions_at_the_ends_of_32_bits(B):
         want[to] = want[start]
         np.testing.assert_array_equal(pd[0, 0].cpu().numpy()[:3], want[:3])
         assert (K[0, 0, :3, 0] / 8).tolist() == [dict(zip(to, start)).get(j, j) for j in range(3)]
+
+
+@pytest.mark.parametrize("rows", [20000, 70000])
+def test_long_capacities_and_short_counts(B, rows):
+    """What is launched goes by the capacity (here several CTAs a head), what is done by the counts on the device."""
+    import torch
+    rng = np.random.default_rng(8)
+    L, Hkv, d, keep = 5, 1, 8, 32
+    n = np.array([33, 5, rows, 2000, 0])
+    c = _Case(rng, L, Hkv, d, rows, n, keep, 2, 9, "special", False)
+    K = rng.integers(0, 65536, (L, Hkv, rows, d), dtype=np.uint16)
+    Kd, Vd = TL.bf16_dev(K), TL.bf16_dev(K)
+    count, st = _dev(n.astype(np.int32)), B.new_status()
+    left = B.stepkv_evict(Kd, Vd, c.md, c.pd, count, keep, 2, 9, status=st)
+    torch.cuda.synchronize()
+    assert st.item() == 0 and left.tolist() == np.minimum(n, keep).tolist()
+    c.check_book()
+    np.testing.assert_array_equal(TL.bits_of(Kd), c.moved(K))
+    np.testing.assert_array_equal(TL.bits_of(Vd), c.moved(K))
 
 
 def test_two_streams_at_once(B):
