@@ -36,7 +36,9 @@ constexpr int kEvictShort = 32 * kEvictShortThreads;  // (a thread holds 32 keys
 constexpr int kEvictLong = 32 * kEvictLongThreads;
 constexpr int kEvictCluster = 8;           // CTAs of a head at most
 static_assert(kEvictCluster * kEvictLong >= kEvictMaxRows, "every key has a register");
-constexpr int kEvictSmemPlan = 2048;       // moves of a head held in shared memory at most (16 KB)
+// Moves of a head held in shared memory at most (16 KB).  48 heads 2200 to 2048 rows: 7.6 us, 8.6 listed in the workspace; 256 heads
+// 8911 to 8272 38.6 and 39.5, codes 45.7 and 47.8.  More would cost the second CTA of an SM.
+constexpr int kEvictSmemPlan = 2048;
 constexpr uint32_t kEvictProtected = 0xFFFFFFFFu;
 
 struct EvictArgs {
@@ -666,7 +668,8 @@ static bool evict_moves_rows(int pairs, int plan_cap, int block_cap, int row_byt
   return itself <= second;
 }
 
-// By the most rows a CTA can have.
+// By the most rows a CTA can have: a loop over slots is unrolled to its limit.  48 heads 1025 rows 5.7 us, 11.8 with the kernel of 32
+// groups; 2200 rows 7.7, 13.0; 256 heads 8273 rows 12.0, 18.5; a cluster's 8 heads 16384 rows 23, 38.
 template <int DQ, bool CL>
 static void (*evict_kernel(int rows, int* threads))(EvictArgs) {
   *threads = rows <= kEvictShort && !CL ? kEvictShortThreads : kEvictLongThreads;
@@ -683,7 +686,9 @@ static void (*evict_kernel(int rows, int* threads))(EvictArgs) {
   }
 }
 
-// CTAs of a head: as many as its keys need, and, where heads leave SMs idle, more while each has kEvictPart rows.
+// CTAs of a head: as many as its keys need, and, where heads leave SMs idle, more while each has kEvictPart rows.  Against as many as
+// its keys need: 2 heads 8911 to 2048 rows 15.2 us, 14.8 (codes 17.9, 20.1); 8 heads 16384 to 8272 23, 30 (24, 35), 32768 28, 39
+// (27, 52), 65536 31, 49.
 constexpr int kEvictPart = 4096;
 static int evict_cluster(int pairs, int n_most, int n_sm) {
   int c = 1;
