@@ -14,7 +14,7 @@
 //   a slot j < keep that goes is number j - R(j) of those, a slot j >= keep that stays number R(j) - R(keep).
 //
 // 32 layers x 8 heads: 8273 to 8272 rows 13 us (positions 1.6, masses and the first histogram 3.1, its bin 0.7, counts 0.8, moves
-// listed 1.6, done 1.2, of a CTA's 9), where the 16 MB that are read take 2.5; 32768 to 8272 in bf16 332 us, of which the moves of 1.7 GB
+// listed 1.6, done 1.2, of a CTA's 9), where the 16 MB that are read take 2.5; 32768 to 8272 in bf16 313 us, of which the moves of 1.7 GB
 // are 254 at the copy rate: one CTA an SM, so that 104 heads wait for the first 152, and their search leaves DRAM idle.  Keys in shared
 // memory instead of registers, with every pass over all of them: 24 and 393 us.
 #include <cooperative_groups.h>
@@ -365,10 +365,15 @@ __global__ void __launch_bounds__(NT, NT == kEvictShortThreads ? 2 : 1) evict_se
   }
   // f(key, slot, slot < n) for this lane's slots, the whole warp at once; keys of slots behind the last are 0
   auto each = [&](auto f) {
+    int at = first;
 #pragma unroll
     for (int r = 0; r < R; ++r) {
       if (r < rounds) {
-        const int j = first + r * 32;
+        if (R > 20 && r) {  // (slots known ahead push keys out of the registers: 32768 to 8272 rows 332 us)
+          at += 32;
+          asm volatile("" : "+r"(at));
+        }
+        const int j = R > 20 ? at : first + r * 32;
         f(keys[r], j, j < n);
       }
     }
@@ -660,7 +665,7 @@ size_t evict_ws_bytes(int n_layers, int Hkv, int n_cap) {
 // its launch, and the bytes at the rate of scattered rows, or a turn of 8 us for the blocks that its warps take at once.
 // Measured, by itself against a second kernel, us: 8 heads 8911 to 8272 rows bf16 18.5, 15.4, codes 26, 20.5; 32 heads 19.0, 18.1
 // and 27, 34; 64 heads 19.4, 22.0 and 29, 54; 8 heads 2100 to 2048 6.7, 8.2; 64 heads 16384 to 8272 105, 77 and 127, 75; 256 heads 176, 270
-// (codes), 32768 to 8272 334, 382.
+// (codes), 32768 to 8272 313, 355.
 static bool evict_moves_rows(int pairs, int plan_cap, int block_cap, int row_bytes, bool q8, int at_once, int n_sm) {
   const double turns = (pairs + at_once - 1) / at_once, rows = (double)pairs * plan_cap;
   const double itself = turns * plan_cap * (q8 ? 20.0 : 4.0 + row_bytes / 32.0);
@@ -668,8 +673,8 @@ static bool evict_moves_rows(int pairs, int plan_cap, int block_cap, int row_byt
   return itself <= second;
 }
 
-// By the most rows a CTA can have: a loop over slots is unrolled to its limit.  48 heads 1025 rows 5.7 us, 11.8 with the kernel of 32
-// groups; 2200 rows 7.7, 13.0; 256 heads 8273 rows 12.0, 18.5; a cluster's 8 heads 16384 rows 23, 38.
+// By the most rows a CTA can have: a loop over slots is unrolled to its limit.  48 heads 1025 rows 5.4 us, 10.7 with the kernel of 32
+// groups; 2200 rows 7.0, 12.2; 256 heads 8273 rows 12.3, 16.4; a cluster's 8 heads 16384 rows 21, 32.
 template <int DQ, bool CL>
 static void (*evict_kernel(int rows, int* threads))(EvictArgs) {
   *threads = rows <= kEvictShort && !CL ? kEvictShortThreads : kEvictLongThreads;
@@ -687,8 +692,8 @@ static void (*evict_kernel(int rows, int* threads))(EvictArgs) {
 }
 
 // CTAs of a head: as many as its keys need, and, where heads leave SMs idle, more while each has kEvictPart rows.  Against as many as
-// its keys need: 2 heads 8911 to 2048 rows 15.2 us, 14.8 (codes 17.9, 20.1); 8 heads 16384 to 8272 23, 30 (24, 35), 32768 28, 39
-// (27, 52), 65536 31, 49.
+// its keys need: 2 heads 8911 to 2048 rows 15.2 us, 14.8 (codes 17.8, 20.3); 8 heads 16384 to 8272 21, 26 (26, 33), 32768 28, 31
+// (29, 48), 65536 32, 43 (32, 58).
 constexpr int kEvictPart = 4096;
 static int evict_cluster(int pairs, int n_most, int n_sm) {
   int c = 1;
