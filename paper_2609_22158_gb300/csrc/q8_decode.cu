@@ -114,7 +114,7 @@ struct Q8State {
   static constexpr int NV = D / 16;     // 16-channel tiles of a row
   static constexpr int NB = GP == 4 ? 2 : 4;
   float m[2];                           // largest logit so far (log2 units)
-  uint64_t nm;                          // 14 - m, 0 before the first key
+  uint64_t nm;                          // -m, 0 before the first key
   uint64_t l;
   uint64_t acc[NV][2];
   uint32_t q[NV][2];                    // B operand of the k-steps
@@ -231,7 +231,7 @@ struct Q8State {
         const float mn = fmaxf(m[e], t[e]);
         was[e] = m[e] == mn ? 1.f : ex2_approx(m[e] - mn);
         m[e] = mn;
-        k[e] = mn == -INFINITY ? 0.f : kQ8WeightLog2 - mn;
+        k[e] = mn == -INFINITY ? 0.f : -mn;
       }
       nm = f2_pack(k[0], k[1]);
       const uint64_t was2 = f2_pack(was[0], was[1]);
@@ -242,13 +242,16 @@ struct Q8State {
         acc[v][1] = f2_mul(acc[v][1], was2);
       }
     }
+    // (14 is added to the difference: 14 - m would round to a multiple of 4 or more once a logit reaches 2^25, with weights of 2^16
+    // and masses off by powers of two)
+    const uint64_t top = f2_pack(kQ8WeightLog2, kQ8WeightLog2);
     const float take = GP == 4 && c4 < 2 ? 0.f : -1.f;
     const uint64_t minus_hi = f2_pack(take, take);
     uint32_t b[2][NB];  // B operand of P: [16 keys][b0, b1 (GP = 8: of both terms)]
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
       float p[2];
-      f2_unpack(f2_add(s[i], nm), p[0], p[1]);
+      f2_unpack(f2_add(f2_add(s[i], nm), top), p[0], p[1]);
       p[0] = ex2_approx(p[0]);
       p[1] = ex2_approx(p[1]);
       const uint64_t p2 = f2_pack(p[0], p[1]);

@@ -454,6 +454,34 @@ def test_decode_keys_queries_and_values_of_any_magnitude(B, magnitude):
     _check(out, q, _values(K), _values(V), 300, "")
 
 
+@pytest.mark.parametrize("G,d,n", [(4, 64, 1), (8, 128, 45), (3, 128, 33), (4, 128, 3000), (5, 64, 700)])
+@pytest.mark.parametrize("e", [20, 24, 25, 26, 27, 28, 31, 60, 100])
+def test_decode_logits_beyond_a_unit_of_32_bits(B, e, G, d, n):
+    """Logits of some 2^e (the heavy keys of one head) and -2^e (of the other), whose neighbours in 32 bits are 2^(e - 23) apart:
+    keys that are the same have the same logit whatever it is rounded to, and share all the weight where the others' lie 2^e
+    below.  What then rounds are the weights (2^-20 relative), their sum and the weighted sum, as in _decode_bound and
+    _mass_bound."""
+    import torch
+    rng = np.random.default_rng(19)
+    half, Hkv = e // 2, 2
+    heavy = np.arange(n) % 3 != 1 if n > 1 else np.ones(1, bool)
+    K = np.stack([np.where(heavy, 1.0, -1.0), np.where(heavy, -1.0, -2.0)])[:, :, None] * np.full(d, 2.0 ** (e - half - int(math.log2(d)) // 2))
+    q = np.tile(np.repeat(2.0 ** half * (1 + np.arange(G) / 8), d).reshape(G, d), (Hkv, 1))
+    K, V, q = wl.f32_to_bf16_bits(K.astype(np.float32)), _bits(rng, (Hkv, n, d)), wl.f32_to_bf16_bits(q.astype(np.float32))
+    mass, st = torch.zeros((1, Hkv, n), device="cuda"), B.new_status()
+    cache = _filled(B, [K], [V])
+    out = B.stepkv_q8_decode([TL.bf16_dev(q)], cache, n, mass=mass, status=st)[0].cpu().numpy()
+    torch.cuda.synchronize()
+    assert st.item() == 0
+    some = heavy.sum()
+    for h in range(Hkv):
+        v = _values(V)[h, heavy]
+        bound = 2 * (2.0 ** -20 + (n / 16 + 64) * 2.0 ** -24) * np.abs(v).mean(0) + 2.0 ** -38 * np.abs(v).sum(0)
+        assert (np.abs(out[h * G:(h + 1) * G] - v.mean(0)) <= bound).all()
+        m = mass[0, h].cpu().numpy()
+        assert (np.abs(m - heavy / some) <= (2.0 ** -19 + (n / 8 + 128 + G + 3) * 2.0 ** -24) / some).all()
+
+
 def test_decode_blocks_of_different_magnitude(B):
     """Blocks whose scales differ by up to 2^40, keys and values alike."""
     import torch
