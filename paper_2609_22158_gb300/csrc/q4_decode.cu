@@ -243,6 +243,9 @@ struct Q4State {
         sc[e] = m[e] == mn ? 1.f : ex2_approx(m[e] - mn);
         m[e] = mn;
         k[e] = mn == -INFINITY ? 0.f : kQ4WeightLog2 - mn;
+        // (from 2^25 on this rounds to a multiple of 4 or more: up, the largest weight would be 2^16, which fp16 does not hold; down,
+        // this state counts for less against others by no more than a unit in the last place of its logits does)
+        if (mn + k[e] > kQ4WeightLog2 + 1.f) k[e] = __fsub_rd(kQ4WeightLog2, mn);
       }
       nm = f2_pack(k[0], k[1]);
       const uint64_t sc2 = f2_pack(sc[0], sc[1]);

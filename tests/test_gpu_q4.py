@@ -636,6 +636,26 @@ def test_decode_keys_of_any_magnitude(B, magnitude):
     _check(out, q, K, V, 300, "")
 
 
+@pytest.mark.parametrize("G,d,n", [(4, 64, 1), (8, 128, 45), (3, 128, 33), (4, 128, 3000), (5, 64, 700)])
+@pytest.mark.parametrize("e", [20, 24, 25, 26, 27, 28, 31, 60, 100])
+def test_decode_logits_beyond_a_unit_of_32_bits(B, e, G, d, n):
+    """Logits of some 2^e (the heavy keys of one head) and -2^e (of the other), whose neighbours in 32 bits are 2^(e - 23) apart:
+    keys that are the same have the same logit whatever it is rounded to, and share all the weight where the others' lie 2^e
+    below.  What then rounds are the weights (2^-20 relative), their sum and the weighted sum, as in _decode_bound."""
+    import torch
+    rng = np.random.default_rng(19)
+    Hkv = 2
+    heavy = np.arange(n) % 3 != 1 if n > 1 else np.ones(1, bool)
+    K = np.stack([np.where(heavy, 1.0, -1.0), np.where(heavy, -1.0, -2.0)])[:, :, None] * np.full(d, 2.0 ** (7 - int(math.log2(d)) // 2))
+    q = np.tile(np.repeat(2.0 ** (e - 7) * (1 + np.arange(G) / 8), d).reshape(G, d), (Hkv, 1))
+    K, V, q = wl.f32_to_bf16_bits(K.astype(np.float32)), _bits(rng, (Hkv, n, d)), wl.f32_to_bf16_bits(q.astype(np.float32))
+    out = B.stepkv_q4_decode([TL.bf16_dev(q)], _filled(B, [K], [V]), n)[0].cpu().numpy()
+    for h in range(Hkv):
+        v = _values(V)[h, heavy]
+        bound = 2 * (2.0 ** -20 + (n / 16 + 64) * 2.0 ** -24) * np.abs(v).mean(0) + 2.0 ** -38 * np.abs(v).sum(0)
+        assert (np.abs(out[h * G:(h + 1) * G] - v.mean(0)) <= bound).all()
+
+
 def _weights_bound(q, K, V, e):
     """_decode_bound's, of logits that are off by e[head] at most."""
     G, out = q.shape[0] // K.shape[0], np.zeros((q.shape[0], K.shape[2]))
