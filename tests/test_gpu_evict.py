@@ -197,6 +197,84 @@ def test_counts_of_their_own(B):
                         np.testing.assert_array_equal(got[l, h, :m], O.q8_evict(v, s, *c.moves[l][h])[0][:m])
 
 
+LENGTHS = [  # L, Hkv, d, rows, n, keep, n_sink, n_recent: every number of rows a thread holds, few rows let go and many
+    (2, 2, 128, 5010, 5000, 4900, 4, 100), (2, 2, 64, 8000, 8000, 7800, 0, 32), (1, 3, 128, 8273, 8273, 8272, 4, 256), (24, 1, 64, 8911, 8911, 8272, 16, 32),
+    (3, 1, 64, 10240, 10240, 10100, 16, 1000), (1, 2, 128, 10241, 10241, 10000, 0, 0), (2, 2, 64, 12000, 11999, 11900, 4, 64), (1, 2, 128, 16384, 16384, 16300, 1, 1),
+    (3, 1, 64, 16385, 16385, 16300, 4, 10), (2, 1, 128, 20000, 20000, 19900, 9, 500), (1, 2, 64, 32768, 32768, 32700, 4, 32), (11, 1, 64, 32700, 32700, 30720, 4, 2000)]
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("L,Hkv,d,rows,n,keep,sink,recent", LENGTHS)
+def test_heads_of_every_length(B, L, Hkv, d, rows, n, keep, sink, recent, q8):
+    if q8:
+        test_q8_evict_matches_oracle(B, L, Hkv, d, rows, n, keep, sink, recent, 3 if keep % 8 else 14)
+    else:
+        test_evict_matches_oracle(B, L, Hkv, d, rows, n, keep, sink, recent, "ties" if keep % 8 else "special")
+
+
+@pytest.mark.parametrize("L,Hkv,d,n,keep", [(2, 3, 96, 1400, 700), (2, 3, 80, 1400, 650), (5, 2, 48, 1300, 700), (1, 2, 24, 2000, 999), (1, 1, 8, 3000, 1500),
+                                            (1, 2, 256, 1500, 700), (1, 3, 200, 1500, 700)])
+def test_many_moves_of_rows_of_any_width(B, L, Hkv, d, n, keep):
+    """Rows that a warp's instruction takes 1 to 32 of, with lanes left over where their 16-byte pieces do not divide 32."""
+    test_evict_matches_oracle(B, L, Hkv, d, n + 1, n, keep, 4, 50, "long tail")
+
+
+@pytest.mark.parametrize("q8", [False, True])
+@pytest.mark.parametrize("L,Hkv,d,rows,keep,each", [
+    (3, 2, 64, 1600, 700, True), (3, 2, 128, 1600, 701, False), (70, 1, 128, 4300, 2100, True), (70, 1, 128, 4250, 2100, False),
+    (66, 1, 64, 1500, 733, True), (66, 1, 64, 33000, 16500, False)])
+def test_many_moves_with_the_count_replaced(B, L, Hkv, d, rows, keep, each, q8):
+    """Calls that move rows by a launch of their own, more than 64 layers (two of either launch, which share the workspace) among
+    them; n_out is n, one for all or one each, of which some are zero, at `keep` or out of range."""
+    import torch
+    rng = np.random.default_rng(L + rows + each)
+    d = 8 if rows > 30000 and not q8 else d
+    n = rng.integers(rows // 2, rows + 1, L) if each else np.array([rows - 3])
+    code = 0
+    if each:
+        n[:2] = keep, rows
+        n[-1] = rows + 1
+        code = B.STEPKV_ENOSPACE
+        if L > 3:
+            n[[5, 40, 64]] = 0, keep + 1, rows
+    used = np.broadcast_to(np.where(n > rows, 0, n), (L,))
+    c = _Case(rng, L, Hkv, d, rows, used, keep, 4, 30, "long tail", False)
+    few = 3  # caches that differ
+    if q8:
+        X = [_bits(rng, (few, Hkv, rows, d)) for _ in "kv"]
+        for x in X:
+            x[:, :, rng.integers(0, rows, rows // 50)] += 5 << 7  # rows 32 times as large
+    else:
+        X = [rng.integers(0, 65536, (few, Hkv, rows, d), dtype=np.uint16) for _ in "kv"]
+    Kd, Vd = (TL.bf16_dev(x)[[l % few for l in range(L)]] for x in X)
+    count, st = _dev(n.astype(np.int32)), B.new_status()
+    if q8:
+        cache = B.Q8Cache.allocate(L, Hkv, rows, d)
+        B.stepkv_q8_write(cache, Kd, Vd, 0, status=st)
+        B.stepkv_q8_evict(cache, c.md, c.pd, count, keep, 4, 30, n_out=count, status=st)
+        got = B.stepkv_q8_read(cache)
+    else:
+        B.stepkv_evict(Kd, Vd, c.md, c.pd, count, keep, 4, 30, n_out=count, status=st)
+        got = (Kd, Vd)
+    torch.cuda.synchronize()
+    assert st.item() == code
+    assert count.tolist() == [x if x > rows else min(x, keep) for x in n.tolist()]
+    c.check_book()
+    want = [O.q8_quantise(x) for x in X] if q8 else None
+    for l in sorted({0, 1, 2, 5, 40, 63, 64, L - 1} & set(range(L))) if q8 else range(L):
+        for t in range(2):
+            for h in range(Hkv):
+                to, start = c.moves[l][h]
+                if q8:
+                    m = min(int(used[l]), keep)
+                    v, s = want[t][0][l % few, h], want[t][1][l % few, h]
+                    np.testing.assert_array_equal(_f64(got[t][l, h])[:m], O.q8_evict(v, s, to, start)[0][:m])
+                else:
+                    x = X[t][l % few, h].copy()
+                    x[to] = x[start]
+                    np.testing.assert_array_equal(TL.bits_of(got[t][l, h].contiguous()), x)
+
+
 @pytest.mark.parametrize("L", [3, 130])
 def test_one_count_on_the_device_for_all(B, L):
     """130 layers take three launches, which all read the one count before it is replaced."""

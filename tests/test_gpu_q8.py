@@ -279,6 +279,39 @@ def test_bad_data(B, kind):
         assert (back[0, :, [4, 9]] == 7).all() if kind == "index" else (back[1] == 7).all() or kind == "row0 above"
 
 
+@pytest.mark.parametrize("row0", [31, 60, 2 ** 31 - 1, -1, -2 ** 31])
+def test_rows_outside_the_cache_leave_a_layer_alone(B, row0):
+    """One layer of three begins where 30 rows do not fit: its codes and scales, keys and values, and the rows read from it keep
+    every byte; the others are written and read."""
+    import torch
+    rng = np.random.default_rng(18)
+    L, Hkv, d, n, rows = 3, 2, 64, 30, 60
+    X = [[_bits(rng, (Hkv, n, d)) for _ in range(L)] for _ in "kv"]
+    cache = B.Q8Cache.allocate(L, Hkv, rows, d)
+    was = _stale(cache, rng)
+    at = np.array([0, row0, 30], np.int32)
+    cache.K_scale[:, :, 0], cache.V_scale[:, :, 0] = 2.0 ** -100, 2.0 ** -100  # (of the rows before 30)
+    scales = [x.clone() for x in (cache.K_scale, cache.V_scale)]
+    st = B.stepkv_q8_write(cache, *[torch.stack([TL.bf16_dev(b) for b in x]) for x in X], _dev(at))
+    torch.cuda.synchronize()
+    assert st.item() == B.STEPKV_ENOSPACE
+    back = [torch.full((L, Hkv, n, d), 7.0, dtype=torch.bfloat16, device="cuda") for _ in "kv"]
+    st = B.new_status()
+    B.stepkv_q8_read(cache, _dev(at), n, K=back[0], V=back[1], status=st)
+    torch.cuda.synchronize()
+    assert st.item() == B.STEPKV_EDATA
+    for t, (codes, scale) in enumerate(((cache.K, cache.K_scale), (cache.V, cache.V_scale))):
+        assert torch.equal(codes.view(torch.uint8)[1], was[t][1]) and torch.equal(scale[1].view(torch.int32), scales[t][1].view(torch.int32))
+        assert (back[t][1] == 7).all()
+        assert torch.equal(codes.view(torch.uint8)[0, :, n:], was[t][0, :, n:])
+        np.testing.assert_array_equal(_f64(back[t])[0], _values(X[t][0]))
+        for h in range(Hkv):
+            v, s = O.e4m3_values(was[t][2, h].cpu().numpy()) * 2.0 ** -100, np.array([2.0 ** -100, 0.0])
+            O.q8_append(v, s, X[t][2][h], 30)
+            np.testing.assert_array_equal(_f64(back[t])[2, h], v[30:])
+            np.testing.assert_array_equal(scale.cpu().numpy()[2, h], s)
+
+
 @pytest.mark.parametrize("order", ["lhnd", "nlhd", "hlnd", "lnhd"])
 def test_read_into_any_order_of_axes(B, order):
     import torch
@@ -441,6 +474,34 @@ def test_decode_forms_and_counts(B, L, Hkv, G, d, rows):
                 assert all(((mass[l] - mass[same[0]])[:, :m].abs() <= bound).all() for l in same)
             else:
                 assert not out[same].any()
+
+
+@pytest.mark.parametrize("L,Hkv,G,d,rows,some", [(64, 8, 4, 128, 1700, [1700, 33, 1, 300]), (64, 8, 8, 64, 1600, [5, 1600, 64, 65, 1, 31]),
+                                                 (60, 16, 1, 64, 2000, [2000]), (64, 32, 2, 64, 1700, [1, 2, 3, 1, 200, 64, 30, 1699])])
+def test_decode_batches_of_mostly_empty_caches(B, L, Hkv, G, d, rows, some):
+    """More pairs than CTAs of which few have keys, where the caches might all be long: single warps take the ranges."""
+    import torch
+    rng = np.random.default_rng(L + rows + G)
+    K, V, q = _keys(rng, (Hkv, rows, d)), _bits(rng, (Hkv, rows, d)), _bits(rng, (Hkv * G, d))
+    Kv, Vv = _values(K), _values(V)
+    cache, st = B.Q8Cache.allocate(L, Hkv, rows, d), B.new_status()
+    B.stepkv_q8_write(cache, *[TL.bf16_dev(x)[None].expand(L, -1, -1, -1) for x in (K, V)], 0, status=st)
+    qd = TL.bf16_dev(q).expand(L, -1, -1).contiguous()
+    n = np.zeros(L, np.int32)
+    n[rng.permutation(L)[:len(some)]] = some
+    for counts in (n, np.sort(n), np.sort(n)[::-1]):
+        nd = _dev(counts.copy())
+        mass0 = torch.rand((L, Hkv, rows), device="cuda")
+        mass, out = mass0.clone(), torch.full((L, Hkv * G, d), 7.0, device="cuda")
+        B.stepkv_q8_decode(qd, cache, nd, out=out, status=st)
+        again = B.stepkv_q8_decode(qd, cache, nd, mass=mass, status=st)
+        torch.cuda.synchronize()
+        assert st.item() == 0 and torch.equal(out, again)
+        for l in range(L):
+            if counts[l]:
+                _check(out[l], q, Kv, Vv, int(counts[l]), f"cache {l} of {counts[l]}", mass[l], mass0[l])
+        empty = torch.from_numpy(counts == 0)
+        assert not out[empty].any() and torch.equal(mass[empty], mass0[empty])
 
 
 @pytest.mark.parametrize("magnitude", [2.0 ** -110, 2.0 ** -90, 1e-20, 1e-3, 1.0, 1e3, 1e20, 2.0 ** 90, 2.0 ** 118])
