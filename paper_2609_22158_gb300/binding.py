@@ -1225,12 +1225,16 @@ def stepkv_q8_decode(q, cache: Q8Cache, n, out=None, mass=None, ws=None, status=
 
 
 # ----------------------------------------------------------------------------- eviction by accumulated attention
+EVICT_MAX_ROWS = 1 << 18  # rows of a head that an eviction ranks at most; a cache may have room for more
+
+
 def evict_workspace(mass, rows: Optional[int] = None):
     """A workspace for evictions from a cache of `rows` rows (default: as many as mass has) whose accumulated attention is
     `mass` (one call at a time may use it)."""
     torch = _torch()
     p = _PerLayer(mass, torch.float32, 2, "mass")
-    need = load_library().stepkv_evict_workspace_size(p.n, p.shape[0], _int32(p.shape[1] if rows is None else rows, "rows"))
+    rows = _int32(p.shape[1] if rows is None else rows, "rows")
+    need = load_library().stepkv_evict_workspace_size(p.n, p.shape[0], min(rows, EVICT_MAX_ROWS))
     return torch.empty(need + 512, dtype=torch.uint8, device=p.device)
 
 
@@ -1254,8 +1258,8 @@ def _evict(where, call, front, L, Hkv, rows, dev, mass, pos, n, keep, n_sink, n_
     wp, wn = _aligned_ws(ws)
     status = _status_on(dev, status, stream)
     _on(dev, ws, "ws")
-    _call_on(dev, stream, where, call, *front, _ptr(n_dev), stride, n_host, rows, keep, n_sink, n_recent, m.ptrs, ms, p.ptrs,
-             ps, n_out.data_ptr(), wp, wn, status.data_ptr())
+    _call_on(dev, stream, where, call, *front, _ptr(n_dev), stride, n_host, min(rows, EVICT_MAX_ROWS), keep, n_sink, n_recent,
+             m.ptrs, ms, p.ptrs, ps, n_out.data_ptr(), wp, wn, status.data_ptr())
     return n_out
 
 
@@ -1266,7 +1270,7 @@ def stepkv_evict(K, V, mass, pos, n, keep: int, n_sink: int = 0, n_recent: int =
 
     K, V: per layer [Hkv, rows, d] bf16; mass: per layer [Hkv, >= rows] float32 (stepkv_decode_h2o's); pos: per layer
     [Hkv, >= rows] int32, the position of each row's token; n: an int, or a device int32 tensor of one count or one per
-    layer.  Rows [0, keep) are the retained ones afterwards, with their masses and positions; masses behind them
+    layer, at most 262144 (EVICT_MAX_ROWS) however many rows there are.  Rows [0, keep) are the retained ones afterwards, with their masses and positions; masses behind them
     are zero.  Returns n_out, min(n, keep) on the device, as many as n has (n itself may be given)."""
     torch = _torch()
     k, v = _PerLayer(K, torch.bfloat16, 3, "K"), _PerLayer(V, torch.bfloat16, 3, "V")

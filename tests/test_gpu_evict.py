@@ -352,6 +352,44 @@ def test_long_capacities_and_short_counts(B, rows):
     np.testing.assert_array_equal(TL.bits_of(Vd), c.moved(K))
 
 
+@pytest.mark.parametrize("q8", [False, True])
+def test_caches_with_room_for_more_rows_than_are_ranked(B, q8):
+    """Heads of 300000 rows with short counts, given on the host and on the device; counts above 262144 are refused or told, and
+    leave their layers alone."""
+    import torch
+    rng = np.random.default_rng(9)
+    L, Hkv, d, rows, keep, limit = 3, 1, 64 if q8 else 8, 300000, 1000, B.EVICT_MAX_ROWS
+    K = _bits(rng, (L, Hkv, rows, d))
+    for n in (np.full(L, 1777), np.array([1500, 900, 1234]), np.array([limit + 1, 1300, rows])):
+        used = np.where(n > limit, 0, n)
+        c = _Case(rng, L, Hkv, d, rows, used, keep, 4, 40, "long tail", False)
+        Kd, Vd, st = TL.bf16_dev(K), TL.bf16_dev(K), B.new_status()
+        if q8:
+            front = (B.Q8Cache.allocate(L, Hkv, rows, d),)
+            B.stepkv_q8_write(front[0], Kd, Vd, 0, n=2000, status=st)
+        else:
+            front = (Kd, Vd)
+        call = B.stepkv_q8_evict if q8 else B.stepkv_evict
+        with pytest.raises(B.StepKVError):
+            call(*front, c.md, c.pd, limit + 1, keep, 4, 40)
+        ws = B.evict_workspace(c.md)
+        left = call(*front, c.md, c.pd, int(n[0]) if n[0] == n[1] else _dev(n.astype(np.int32)), keep, 4, 40, ws=ws, status=st)
+        torch.cuda.synchronize()
+        assert st.item() == (B.STEPKV_ENOSPACE if n.max() > limit else 0)
+        assert left.tolist() == ([keep] if n[0] == n[1] else [0 if x > limit else min(x, keep) for x in n.tolist()])
+        c.check_book()
+        got = _f64(B.stepkv_q8_read(front[0], 0, keep)[0]) if q8 else O.bf16_to_f64(TL.bits_of(Kd))
+        for l in range(L):
+            to, start = c.moves[l][0]
+            if q8:
+                v, s = O.q8_quantise(K[l, 0, :2000])
+                np.testing.assert_array_equal(got[l, 0], O.q8_evict(v, s, to, start)[0][:keep])
+            else:
+                x = K[l, 0].copy()
+                x[to] = x[start]
+                np.testing.assert_array_equal(got[l, 0], O.bf16_to_f64(x))
+
+
 def test_two_streams_at_once(B):
     import torch
     rng = np.random.default_rng(6)
