@@ -479,8 +479,10 @@ STEPKV_API stepkv_status_t stepkv_q4_decode(const stepkv_q4_cache_t* cache, cons
 
 /* ---------------------------------------------------------------------------------------------
  * A cache held in 8 bits: e4m3 codes, with one scale for each block of STEPKV_Q8_BLOCK rows (tokens) of a KV head.  Half the
- * bytes of bf16.  A value is off by at most 2^-4 of itself, and channels much larger than the others take nothing from them
- * (e4m3 keeps its 4 significant bits down to 2^-14 of the block's largest value).
+ * bytes of bf16.  A value x is off by at most 2^-4 max(|x|, 2^-6 s), s its block's scale: by 2^-4 of itself where it is at least
+ * 2^-6 s, which is 2^-13.8 (largest value just above 224 s) to 2^-14.8 (448 s) of the block's largest value, so that channels much
+ * larger than the others take nothing from them; below that e4m3 is subnormal, and below 2^-10 s it is zero.  Each time a block's
+ * scale grows, what it has below 2^-6 of the new scale rounds once more, by at most 2^-10 of that scale.
  *
  * Format.  A block's scale is s = 2^k with k the smallest integer for which every finite value of the rows written to it has
  * |x| <= 448 s, at least -100 and at most 119; a value's code is e4m3(x / s), ties to even; NaN and infinities get the code of
@@ -578,7 +580,8 @@ STEPKV_API stepkv_status_t stepkv_q8_decode(const stepkv_q8_cache_t* cache, cons
  *  n_out       device, laid out as n_dev (without it, or with stride 0: one value), or NULL: min(n, keep).  May be n_dev itself.
  *  ws          scratch of stepkv_evict_workspace_size bytes (256-byte aligned); 0 for what is not supported.
  *  Nothing that is written may share memory with another tensor of the call (STEPKV_EINVAL; n_out may be n_dev).
- *  Supported: n_cap <= 262144, Hkv <= 65535.
+ *  Supported: n_cap <= 262144 (of a longer cache, too: n_cap bounds the counts, not the rows that heads have room for), Hkv <=
+ *  65535.
  *  stepkv_q8_evict: the same over a cache held in 8 bits (n_cap <= cache->rows).  The scale of a block that receives rows becomes
  *  the larger of what it was and what those rows need; the codes of rows that stay in it become e4m3(code s_old / s_new), those
  *  of rows received e4m3(code s_source / s_new).

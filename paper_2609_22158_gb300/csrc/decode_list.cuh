@@ -78,7 +78,9 @@ __device__ __forceinline__ void list_counts(const DecodeList& a, ListCounts& s, 
 // How the list of blocks is cut, where pairs are.  Ranges of `per` blocks of the list, one after another; or (k > 0: one count
 // for all, and ranges that each lie in one pair, k in each, are nearly as even) these, which spares a second start and end to
 // those that would reach over.  Groups are single warps where there are more pairs than CTAs and the pairs are short: a warp
-// then takes a range by itself instead of waiting for three others at its end.
+// then takes a range by itself instead of waiting for three others at its end.  (`total` is the list's, blocks without keys
+// included: where every pair has 16 of these, as in the 8-bit decode of a ragged batch, it passes 16 * pairs unless a part of the
+// caches is empty, so that only batches of mostly empty caches go to single warps there.)
 struct ListSplit {
   int W, per, k;
 };

@@ -8,7 +8,8 @@
 // else a second kernel moves them over the whole machine.  In 8 bits a block that receives rows may have to take a larger scale.
 //
 // A row's rank is a 32-bit key: all ones where it is protected, else the mass as an integer that orders like the number (0 for
-// a NaN).  Keys stay in registers, a warp's being consecutive slots.  The key T of the last retained row comes from histograms
+// a NaN).  Keys stay in registers, a warp's being consecutive slots (of 64 a thread: the 8-bit kernels of 20 and 32 keys a thread
+// spill 2 to 5 words, the cluster kernels of 32 keys 17, in bf16 1).  The key T of the last retained row comes from histograms
 // of 11, 11 and 10 bits, as many as it takes; with R(j) = min(rows below j that equal T, those of them that stay) + rows below
 // j above T, the retained rows below slot j,
 //   a slot j < keep that goes is number j - R(j) of those, a slot j >= keep that stays number R(j) - R(keep).
@@ -34,10 +35,12 @@ constexpr int kEvictLongThreads = 1024;    // of a head of more than kEvictShort
 constexpr int kEvictShortThreads = 512;
 constexpr int kEvictShort = 32 * kEvictShortThreads;  // (a thread holds 32 keys at most)
 constexpr int kEvictLong = 32 * kEvictLongThreads;
-constexpr int kEvictCluster = 8;           // CTAs of a head at most
-static_assert(kEvictCluster * kEvictLong >= kEvictMaxRows, "every key has a register");
+constexpr int kEvictCluster = 8;           // CTAs of a head at most: as many as a cluster has without asking the device for more
+static_assert(kEvictCluster * kEvictLong >= kEvictMaxRows, "every key has a place");
 // Moves of a head held in shared memory at most (16 KB).  48 heads 2200 to 2048 rows: 7.6 us, 8.6 listed in the workspace; 256 heads
-// 8911 to 8272 38.6 and 39.5, codes 45.7 and 47.8.  More would cost the second CTA of an SM.
+// 8911 to 8272 38.6 and 39.5, codes 45.7 and 47.8.  Two CTAs of an SM have room for some 10000; of longer lists the moves themselves are
+// most of the time: 256 heads 11172 to 8272 109 us, 109 with 4096 and with 6144, codes 98, 94, 95; 14272 to 8272 169, 170, 168 and 140, 139,
+// 130.
 constexpr int kEvictSmemPlan = 2048;
 constexpr uint32_t kEvictProtected = 0xFFFFFFFFu;
 
@@ -666,6 +669,8 @@ size_t evict_ws_bytes(int n_layers, int Hkv, int n_cap) {
 // Measured, by itself against a second kernel, us: 8 heads 8911 to 8272 rows bf16 18.5, 15.4, codes 26, 20.5; 32 heads 19.0, 18.1
 // and 27, 34; 64 heads 19.4, 22.0 and 29, 54; 8 heads 2100 to 2048 6.7, 8.2; 64 heads 16384 to 8272 105, 77 and 127, 75; 256 heads 176, 270
 // (codes), 32768 to 8272 313, 355.
+// Where the count is on the device this, the kernel's number of keys and the place of the list go by the rows there may be.  8273 to 8272
+// rows in caches of 8273, 8337 and 12369 rows: 8 heads 10.5, 10.5, 14.4 us (codes 10.8, 12.7, 14.4), 256 heads 12.4, 12.4, 16.5 (16.6, 16.4, 22.7).
 static bool evict_moves_rows(int pairs, int plan_cap, int block_cap, int row_bytes, bool q8, int at_once, int n_sm) {
   const double turns = (pairs + at_once - 1) / at_once, rows = (double)pairs * plan_cap;
   const double itself = turns * plan_cap * (q8 ? 20.0 : 4.0 + row_bytes / 32.0);
@@ -674,7 +679,8 @@ static bool evict_moves_rows(int pairs, int plan_cap, int block_cap, int row_byt
 }
 
 // By the most rows a CTA can have: a loop over slots is unrolled to its limit.  48 heads 1025 rows 5.4 us, 10.7 with the kernel of 32
-// groups; 2200 rows 7.0, 12.2; 256 heads 8273 rows 12.3, 16.4; a cluster's 8 heads 16384 rows 21, 32.
+// groups; 2200 rows 7.0, 12.2; 256 heads 8273 rows 12.3, 16.4; a cluster's 8 heads 16384 rows 21, 32.  A kernel of 24 groups in place of
+// that of 20: 256 heads 8273 rows 12.6 -> 14.5 (codes 16.5 -> 18.5), 10240 to 8272 81 -> 82 (74 -> 76), 12288 to 8272 133 -> 131 (114 -> 111).
 template <int DQ, bool CL>
 static void (*evict_kernel(int rows, int* threads))(EvictArgs) {
   *threads = rows <= kEvictShort && !CL ? kEvictShortThreads : kEvictLongThreads;

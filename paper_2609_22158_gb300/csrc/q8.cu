@@ -37,10 +37,12 @@ __device__ __forceinline__ int q8_count(const Q4Rows& r, int32_t* status) {
 }
 
 // A warp takes a block of 32 rows: all of it in registers (64 a lane at d = 128), its largest magnitude by a reduction over
-// the warp, then the codes.  A lane has 8 consecutive channels of every 2nd (4th) row.
+// the warp, then the codes.  A lane has 8 consecutive channels of every 2nd (4th) row.  (With three CTAs an SM, d = 128, 15 words
+// of a lane's 80 go through local memory, which is L1's: still the faster of the two.)
 // CTAs an SM holds: two have the registers for all of a block's loads at once, which is faster where a warp has few blocks to take
 // (1 layer x 8 heads x 8272 rows 8.0 us, with three 10.1); with many, three (d = 64: four) keep more in flight (32 layers x
-// 8272 rows 271 -> 253 us = 6.4 TB/s, 639 rows 23.6 -> 21.1; 64 channels x 4000 rows 79 -> 65).
+// 8272 rows 271 -> 253 us = 6.4 TB/s, 639 rows 23.6 -> 21.1; 64 channels x 4000 rows 79 -> 65).  By index, 8272 of 32768 rows: 259
+// us of 32 layers; of one layer, out of DRAM, 19.6, and 16.6 in order.
 constexpr int q8_write_ctas(int D, bool many) { return !many ? 2 : D == 128 ? 3 : 4; }
 constexpr int kQ8WriteFew = 3;  // blocks a warp
 template <int D, bool IDX, bool MANY>
@@ -156,8 +158,11 @@ __global__ void __launch_bounds__(kQ8Threads, q8_write_ctas(D, MANY)) q8_write_k
   }
 }
 
-// A lane takes 8 codes of a row.  32 layers x 8 heads x 8272 rows: 268 us = 6.1 TB/s, 64 layers x 4240 rows 6.2; two and eight rows of
+// A lane takes 8 codes of a row.  32 layers x 8 heads x 8272 rows: 265 us = 6.1 TB/s, 64 layers x 4240 rows 6.2; two and eight rows of
 // a lane in flight, 3 to 16 CTAs an SM and plain stores 266-279.
+// Right behind a call of this library it takes longer: its CTAs are launched while that one's still fill the SMs, gather on those that
+// are free first, up to eight on one, and each keeps its share of the rows.  After an eviction of 256 heads (38 us) the two take 373
+// us, launched in ordinary order 303; 639 rows written and read back 47 us, 37.
 constexpr int kQ8ReadUnroll = 4;
 constexpr int kQ8ReadCtas = 4;
 
